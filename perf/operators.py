@@ -196,8 +196,8 @@ def prepare(case, seed):
             s["plan"] = da.decode_attn_plan(s["shape"], da.make_policy(track_weights=1), lens)
         elif op == "prompt":
             s["plan"] = da.decode_attn_prompt_plan(s["shape"], da.make_policy(window_tokens=window, sink_tokens=sinks), news, lens)
-        need = s["plan"].workspace_bytes if "plan" in s else da.decode_attn_evict_workspace_bytes(s["shape"], case["budget"])
-        s["ws"] = torch.empty(max(need, 256), dtype=torch.uint8, device="cuda")
+        if "plan" in s:
+            s["ws"] = torch.empty(max(s["plan"].workspace_bytes, 256), dtype=torch.uint8, device="cuda")
     return s
 
 
@@ -223,7 +223,7 @@ def _own_weights(s):
 def _own_evict(s):
     c = s["case"]
     s["da"].decode_attn_evict(s["shape"], c["budget"], c["sinks"], c["recent"], s["seq_lens"], s["block_table"], s["dst_table"],
-                              s["k"], s["v"], s["weights"], s["weights_out"], s["kept"], s["lens_out"], s["ws"])
+                              s["k"], s["v"], s["weights"], s["weights_out"], s["kept"], s["lens_out"])
     return {"kept": s["kept"], "lens": s["lens_out"], "weights": s["weights_out"], "k": s["k"], "v": s["v"]}
 
 
