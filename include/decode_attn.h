@@ -108,7 +108,17 @@ typedef struct {
                                sequences instead of once per sequence.  Tensor-core kernels only
                                (MMA_TMA: groups of up to 4 heads; UMMA_PREFIX: head_dim 128, groups of
                                up to 16), separate combine, no capacity plan, not FIXED_COUNT.         */
-    int32_t reserved[5];
+    int32_t window_tokens;  /* > 0: sliding window.  The step's query, at position seq_len - 1, attends the
+                               last window_tokens positions (its own among them) and the first
+                               sink_tokens ones.  Block-table entries of pages that hold neither are
+                               never read: an engine may give such pages back.  The plan's units then
+                               count visible positions: whole 16-token tiles of the gap are left out.
+                               Tensor-core kernel MMA_TMA, no shared prefix.                          */
+    int32_t sink_tokens;    /* with window_tokens: first positions that stay visible (0: none)         */
+    int32_t track_weights;  /* 1: the launch also leaves every logit in the workspace, from which
+                               decode_attn_add_weights adds each cached token's attention weight to a
+                               running total.  Tensor-core kernel MMA_TMA, no shared prefix.           */
+    int32_t reserved[2];
 } decode_attn_policy_t;
 
 typedef struct {
@@ -348,6 +358,30 @@ int decode_attn_merge_shards(const decode_attn_shape_t *shape, int32_t n_shards,
  * valid: it recomputes the same bits. */
 int decode_attn_combine(const decode_attn_plan_t *plan, const void *workspace, void *out,
                         float *lse_or_null, cudaStream_t stream);
+
+/* Running totals of attention weights, what an eviction by attention weight
+ * ranks a cache by (decode_attn_evict).  For plans made with
+ * policy.track_weights (DA_ERR_UNSUPPORTED otherwise), behind
+ * decode_attn_run and decode_attn_combine of the step, with the workspace and
+ * the lse they wrote:
+ *   weights_out[b][g][t] = weights[b][g][t] + sum over the query heads h of KV head g of softmax weight of t in row (b, h)
+ * for t < seq_len; what lies behind a sequence's end is neither read nor
+ * written.  Rows that attended nothing (a RUN mask of 0) and tokens a window
+ * hides add nothing.  The prompt's own attention can be counted the same way:
+ * its last n tokens are n rows of a batch that share one row of pages, with
+ * lengths seq_len - n + 1 .. seq_len and totals of their own to be summed.
+ *   lse          device, fp32 [batch, num_q_heads]
+ *   weights, weights_out  device, fp32; the row of (b, g) starts at
+ *                b * stride_seq + g * stride_head and holds `tokens` values, at
+ *                least the longest sequence (of a capacity plan: the longest it
+ *                can hold); both strides are at least `tokens`.  The two may be
+ *                the same buffer, and must not overlap otherwise.
+ * A log-sum-exp of magnitude x carries an fp32 rounding of about 6e-8 x, and
+ * the weights that relative error.  One launch on `stream`, nothing is allocated,
+ * capture-safe. */
+int decode_attn_add_weights(const decode_attn_plan_t *plan, const void *workspace, const float *lse,
+                            const int32_t *seq_lens, const float *weights, float *weights_out, int64_t tokens,
+                            int64_t stride_seq, int64_t stride_head, cudaStream_t stream);
 
 /* Synchronises `stream`, returns the worst condition the kernels recorded
  * since the last call (DA_OK, DA_ERR_STALE_PLAN, DA_ERR_BAD_PAGE,

@@ -56,6 +56,7 @@ EXPORTED = [
     "decode_attn_step_static", "decode_attn_append_kv", "decode_attn_breakeven_tokens",
     "decode_attn_switch_thresholds", "decode_attn_switch_next", "decode_attn_validate_shared_prefix",
     "decode_attn_merge_shards", "decode_attn_append_kv_checked", "decode_attn_debug_expire_wait",
+    "decode_attn_add_weights",
 ]
 
 
@@ -65,7 +66,8 @@ class Policy(ctypes.Structure):
                 ("sm_count", ctypes.c_int32), ("kernel", ctypes.c_int32),
                 ("fuse_combine", ctypes.c_int32), ("capacity_batch", ctypes.c_int32),
                 ("capacity_tokens", ctypes.c_int32), ("ctas_per_sm", ctypes.c_int32),
-                ("shared_prefix_tokens", ctypes.c_int32), ("reserved", ctypes.c_int32 * 5)]
+                ("shared_prefix_tokens", ctypes.c_int32), ("window_tokens", ctypes.c_int32),
+                ("sink_tokens", ctypes.c_int32), ("track_weights", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
 
 
 class Shape(ctypes.Structure):
@@ -131,6 +133,7 @@ _lib.decode_attn_append_kv.argtypes = [ctypes.POINTER(Shape), _vp, _vp, _vp, _vp
 _lib.decode_attn_append_kv_checked.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.decode_attn_debug_expire_wait.argtypes = [_vp, ctypes.POINTER(RunArgs), ctypes.c_int64, _vp]
 _lib.decode_attn_merge_shards.argtypes = [ctypes.POINTER(Shape), ctypes.c_int32, _vp, _vp, _vp, _vp, _vp]
+_lib.decode_attn_add_weights.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp] + [ctypes.c_int64] * 3 + [_vp]
 _lib.decode_attn_breakeven_tokens.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int32,
                                               ctypes.c_double, ctypes.POINTER(ctypes.c_double)]
 _lib.decode_attn_switch_thresholds.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double),
@@ -188,12 +191,14 @@ def _host_i32(x) -> np.ndarray:
 def make_policy(split_mode: int = DA_SPLIT_AUTO, fixed_count: int = 0, chunk_tokens: int = 0,
                 max_splits: int = 0, sm_count: int = 0, kernel: int = DA_KERNEL_AUTO, fuse_combine: int = 0,
                 capacity_batch: int = 0, capacity_tokens: int = 0, ctas_per_sm: int = 0,
-                shared_prefix_tokens: int = 0) -> Policy:
+                shared_prefix_tokens: int = 0, window_tokens: int = 0, sink_tokens: int = 0,
+                track_weights: int = 0) -> Policy:
     p = Policy()
     p.split_mode, p.fixed_count, p.chunk_tokens, p.max_splits = split_mode, fixed_count, chunk_tokens, max_splits
     p.sm_count, p.kernel, p.fuse_combine = sm_count, kernel, fuse_combine
     p.capacity_batch, p.capacity_tokens, p.ctas_per_sm = capacity_batch, capacity_tokens, ctas_per_sm
     p.shared_prefix_tokens = shared_prefix_tokens
+    p.window_tokens, p.sink_tokens, p.track_weights = window_tokens, sink_tokens, track_weights
     return p
 
 
@@ -327,6 +332,22 @@ def decode_attn_combine(plan: Plan, workspace, out, lse=None, stream=None, check
     rc = _lib.decode_attn_combine(plan.handle, _ptr(workspace), _ptr(out), _ptr(lse), _stream(stream))
     if check:
         _check(rc, "decode_attn_combine")
+    return rc
+
+
+def decode_attn_add_weights(plan: Plan, workspace, lse, seq_lens, weights, weights_out=None, stream=None,
+                            check: bool = True) -> int:
+    """weights, weights_out: fp32 [batch, num_kv_heads, tokens], innermost axis contiguous, other strides equal;
+    weights_out None: in place."""
+    if weights_out is None:
+        weights_out = weights
+    if weights.shape != weights_out.shape or weights.stride() != weights_out.stride() or weights.stride(2) != 1 or \
+            weights.shape[0] < plan.shape.batch or weights.shape[1] != plan.shape.num_kv_heads:
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_add_weights")
+    rc = _lib.decode_attn_add_weights(plan.handle, _ptr(workspace), _ptr(lse), _ptr(seq_lens), _ptr(weights),
+                                      _ptr(weights_out), weights.shape[2], weights.stride(0), weights.stride(1), _stream(stream))
+    if check:
+        _check(rc, "decode_attn_add_weights")
     return rc
 
 

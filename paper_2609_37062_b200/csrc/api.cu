@@ -19,6 +19,7 @@
 #include "kernel_umma.cuh"
 #include "kernel_simt.cuh"
 #include "planner.h"
+#include "weights.cuh"
 
 using namespace da;
 
@@ -50,6 +51,7 @@ struct decode_attn_plan {
     int64_t grid = 0;        // blocks launched by run: work_grid attending blocks (+ merge blocks when fused)
     int64_t work_grid = 0;
     size_t workspace_bytes = 0;
+    size_t off_logits = 0;   // in the workspace, behind the partial records (plans that track weights)
     // device buffer (views into the cached allocation the plan holds)
     char* dev = nullptr;
     char* pinned = nullptr;
@@ -226,7 +228,7 @@ int pick_kernel(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
 
 // Resident blocks per SM of the kernel a plan will launch (the uncached query; it also opts the
 // kernel in to its dynamic shared memory).
-int query_occupancy_uncached(int kernel, int D, int G, int* block_threads, int* dyn_smem, bool prefix)
+int query_occupancy_uncached(int kernel, int D, int G, int* block_threads, int* dyn_smem, bool prefix, bool ext)
 {
     int n = 0;
     if (kernel == DA_KERNEL_SIMT) {
@@ -240,19 +242,19 @@ int query_occupancy_uncached(int kernel, int D, int G, int* block_threads, int* 
         }
         return n;
     }
-    return mma_query_occupancy(D, G, block_threads, dyn_smem, prefix);
+    return mma_query_occupancy(D, G, block_threads, dyn_smem, prefix, false, ext);
 }
 
 // Plans are made every decode step: the answers that depend only on (device, kernel variant) are
 // kept after the first query.
 struct OccEntry {
-    int device, kernel, D, G, prefix, occ, block_threads, dyn_smem;
+    int device, kernel, D, G, prefix, ext, occ, block_threads, dyn_smem;
 };
 std::mutex g_occ_mu;
 std::vector<OccEntry> g_occ;
 std::vector<std::pair<int, int>> g_sm_counts;   // (device, multiprocessors)
 
-int query_occupancy(int kernel, int D, int G, int* block_threads, int* dyn_smem, bool prefix = false)
+int query_occupancy(int kernel, int D, int G, int* block_threads, int* dyn_smem, bool prefix = false, bool ext = false)
 {
     int dev = -1;
     if (cudaGetDevice(&dev) != cudaSuccess) {
@@ -262,16 +264,16 @@ int query_occupancy(int kernel, int D, int G, int* block_threads, int* dyn_smem,
     {
         std::lock_guard<std::mutex> lock(g_occ_mu);
         for (const OccEntry& e : g_occ)
-            if (e.device == dev && e.kernel == kernel && e.D == D && e.G == G && e.prefix == (int)prefix) {
+            if (e.device == dev && e.kernel == kernel && e.D == D && e.G == G && e.prefix == (int)prefix && e.ext == (int)ext) {
                 *block_threads = e.block_threads;
                 *dyn_smem = e.dyn_smem;
                 return e.occ;
             }
     }
-    const int occ = query_occupancy_uncached(kernel, D, G, block_threads, dyn_smem, prefix);
+    const int occ = query_occupancy_uncached(kernel, D, G, block_threads, dyn_smem, prefix, ext);
     if (occ > 0) {
         std::lock_guard<std::mutex> lock(g_occ_mu);
-        g_occ.push_back({dev, kernel, D, G, (int)prefix, occ, *block_threads, *dyn_smem});
+        g_occ.push_back({dev, kernel, D, G, (int)prefix, (int)ext, occ, *block_threads, *dyn_smem});
     }
     return occ;
 }
@@ -318,7 +320,7 @@ void fill_host_mirror(decode_attn_plan_t* pl)
         si[b].slot_base = pl->layout.slot_base[b];
         si[b].n_splits = pl->layout.splits[b];
         si[b].seq_len = pl->seq_lens[b];
-        si[b].pad = 0;
+        si[b].tile_base = pl->layout.tile_base[b];
     }
     if (pl->max_bins > 0) {
         // one range per launched block; blocks beyond the bins in use get an empty range
@@ -382,6 +384,11 @@ KernelParams make_params(const decode_attn_plan_t* pl, const decode_attn_run_arg
     kp.grid_exit = pl->policy.capacity_batch > 0;
     kp.n_units = (int32_t)pl->layout.units.size();
     kp.wait_limit = kWaitLimitCycles;
+    kp.window = pl->policy.window_tokens;
+    kp.sinks = pl->policy.sink_tokens;
+    kp.logits = pl->policy.track_weights && a.workspace != nullptr
+                    ? reinterpret_cast<float*>(static_cast<char*>(a.workspace) + pl->off_logits)
+                    : nullptr;
     // The tensor-core kernel asks the first pages of every block into L2 ahead of its dependency
     // wait.  Seven pages, just short of two stages' worth, when a block has a single unit (the opening
     // burst is then a visible share of the step: 24.8 us without hints, 23.9 / 23.6 / 23.2 / 23.2 /
@@ -493,7 +500,8 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
     if (prefix && pl->kernel == DA_KERNEL_SIMT) return DA_ERR_UNSUPPORTED;
     // what follows a tcgen05 prefix runs on the ordinary tensor-core kernel
     int occ = query_occupancy(DA_KERNEL_MMA_TMA == pl->kernel || umma ? DA_KERNEL_MMA_TMA : pl->kernel, shape->head_dim,
-                              pl->group, &pl->block_threads, &pl->dyn_smem, prefix && !umma);
+                              pl->group, &pl->block_threads, &pl->dyn_smem, prefix && !umma,
+                              policy->window_tokens > 0 || policy->track_weights);
     if (occ <= 0) return DA_ERR_CUDA;
     pl->ctas_per_sm = policy->ctas_per_sm > 0 ? policy->ctas_per_sm : occ;
 
@@ -526,6 +534,12 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
     }
 
     pl->workspace_bytes = (size_t)pl->max_slots * shape->num_kv_heads * rec_floats(pl->group, shape->head_dim) * sizeof(float);
+    if (policy->track_weights) {
+        const int64_t tiles = policy->capacity_batch > 0 ? policy->capacity_tokens / kTileTokens + policy->capacity_batch
+                                                         : pl->layout.n_tiles;
+        pl->off_logits = align_up(pl->workspace_bytes, 256);
+        pl->workspace_bytes = pl->off_logits + (size_t)tiles * shape->num_kv_heads * pl->group * kTileTokens * sizeof(float);
+    }
 
     pl->off_units = align_up(sizeof(DevHeader), 32);
     pl->off_seq_info = pl->off_units + align_up((size_t)std::max<int64_t>(pl->max_units, 1) * sizeof(decode_attn_unit_t), 32);
@@ -778,6 +792,53 @@ int decode_attn_combine(const decode_attn_plan_t* pl, const void* workspace, voi
     return DA_OK;
 }
 
+int decode_attn_add_weights(const decode_attn_plan_t* pl, const void* workspace, const float* lse, const int32_t* seq_lens,
+                            const float* weights, float* weights_out, int64_t tokens, int64_t stride_seq,
+                            int64_t stride_head, cudaStream_t stream)
+{
+    if (!pl) return DA_ERR_INVALID_ARG;
+    if (!pl->policy.track_weights) return DA_ERR_UNSUPPORTED;
+    int32_t longest = 0;
+    for (int32_t n : pl->seq_lens) longest = std::max(longest, n);
+    if (pl->shape.batch == 0 || longest == 0) return DA_OK;
+    if (!workspace || !lse || !seq_lens || !weights || !weights_out) return DA_ERR_INVALID_ARG;
+    if (!aligned(workspace, 256) || !aligned(lse, 4) || !aligned(seq_lens, 4) || !aligned(weights, 4) || !aligned(weights_out, 4))
+        return DA_ERR_INVALID_ARG;
+    // rows of different sequences and KV heads must not overlap
+    if (tokens < longest || stride_seq < tokens || stride_head < tokens) return DA_ERR_INVALID_ARG;
+    WeightsParams wp;
+    wp.logits = reinterpret_cast<const float*>(static_cast<const char*>(workspace) + pl->off_logits);
+    wp.lse = lse;
+    wp.seq_lens = seq_lens;
+    wp.header = reinterpret_cast<const DevHeader*>(pl->dev);
+    wp.seq_info = reinterpret_cast<const SeqInfo*>(pl->dev + pl->off_seq_info);
+    wp.weights = weights;
+    wp.weights_out = weights_out;
+    wp.stride_seq = stride_seq;
+    wp.stride_head = stride_head;
+    wp.status = reinterpret_cast<int32_t*>(pl->dev + pl->off_status);
+    wp.num_kv_heads = pl->shape.num_kv_heads;
+    wp.group = pl->group;
+    wp.window = pl->policy.window_tokens;
+    wp.sinks = pl->policy.sink_tokens;
+    wp.vec = aligned(weights, 16) && aligned(weights_out, 16) && stride_seq % 4 == 0 && stride_head % 4 == 0;
+    // A capacity plan's graph is replayed for other lengths and batches: its grid covers the most any row can hold.
+    const bool capacity = pl->policy.capacity_batch > 0;
+    const int64_t most = capacity ? std::min<int64_t>((int64_t)pl->shape.max_pages_per_seq * pl->shape.page_size,
+                                                      pl->policy.capacity_tokens)
+                                  : longest;
+    if (tokens < most) return DA_ERR_INVALID_ARG;
+    wp.chunks = (int32_t)((most + kWeightsTokens - 1) / kWeightsTokens);
+    const int64_t blocks = (int64_t)wp.chunks * wp.num_kv_heads * (capacity ? pl->max_batch : pl->shape.batch);
+    if (blocks > 0x7fffffffLL) return DA_ERR_UNSUPPORTED;
+    int rc = order_behind_upload(pl, stream);
+    if (rc != DA_OK) return rc;
+    rc = weights_launch(wp, (unsigned)blocks, stream);
+    if (rc != DA_OK) return rc;
+    mark_launched(pl, stream);
+    return DA_OK;
+}
+
 int decode_attn_merge_shards(const decode_attn_shape_t* shape, int32_t n_shards, const float* out_shards,
                              const float* lse_shards, void* out, float* lse_or_null, cudaStream_t stream)
 {
@@ -857,7 +918,7 @@ int decode_attn_debug_gather(const decode_attn_plan_t* pl, int32_t seq, const vo
 {
     if (!pl || !k_cache || !v_cache || !block_table || !k_out || !v_out) return DA_ERR_INVALID_ARG;
     if (seq < 0 || seq >= pl->shape.batch) return DA_ERR_INVALID_ARG;
-    if (pl->policy.shared_prefix_tokens > 0) return DA_ERR_UNSUPPORTED;
+    if (pl->policy.shared_prefix_tokens > 0 || pl->policy.window_tokens > 0) return DA_ERR_UNSUPPORTED;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_out, 16) || !aligned(v_out, 16))
         return DA_ERR_INVALID_ARG;
     if (pl->grid == 0) return DA_OK;
@@ -876,7 +937,7 @@ int decode_attn_gather_probe(const decode_attn_plan_t* pl, const void* k_cache, 
 {
     if (!pl || !k_cache || !v_cache || !block_table || !checksum_out) return DA_ERR_INVALID_ARG;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return DA_ERR_INVALID_ARG;
-    if (pl->policy.shared_prefix_tokens > 0) return DA_ERR_UNSUPPORTED;
+    if (pl->policy.shared_prefix_tokens > 0 || pl->policy.window_tokens > 0) return DA_ERR_UNSUPPORTED;
     if (pl->grid == 0) return DA_OK;
     decode_attn_run_args_t a;
     std::memset(&a, 0, sizeof a);
@@ -1180,7 +1241,7 @@ int decode_attn_step_static(const decode_attn_shape_t* shape, const int32_t* seq
         si[b].slot_base = lay.slot_base[b];
         si[b].n_splits = lay.splits[b];
         si[b].seq_len = seq_lens_host[b];
-        si[b].pad = 0;
+        si[b].tile_base = 0;
     }
     // The array keeps the previous call's contents.  What the kernels only read is overwritten by
     // the two uploads below, records are written before they are read, and the status word is

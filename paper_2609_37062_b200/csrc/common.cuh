@@ -10,6 +10,7 @@
 #include <cstdint>
 
 #include "decode_attn.h"
+#include "window.h"
 
 namespace da {
 
@@ -25,7 +26,7 @@ struct SeqInfo {
     int32_t slot_base;  // -1: single split, written directly
     int32_t n_splits;
     int32_t seq_len;    // the length the plan was made for
-    int32_t pad;
+    int32_t tile_base;  // visible 16-token tiles of the sequences before this one (plans that track weights)
 };
 
 struct KernelParams {
@@ -82,6 +83,9 @@ struct KernelParams {
     // Test hook (decode_attn_debug_expire_wait): the producer withholds its loads, so that the
     // waits of the launch run out and its give-up path is exercised with nothing at fault.
     int32_t debug_drop_loads;
+    // Windowed plans, plans that track attention weights (the kernel's EXT variants; 0 / NULL else).
+    int32_t window, sinks;
+    float* logits;   // [visible tiles of the batch x Hkv][G][16]: every logit in the log2 domain, see logit_tile()
 #ifdef DA_TRACE
     unsigned long long* trace;  // debug builds: 32 stamps per block, or NULL
 #endif
@@ -196,6 +200,13 @@ __device__ __forceinline__ bool block_sync_or(int id, int nthreads, bool pred)
 // domain, sum of exponentials) for each of the G heads, padded to 16 bytes so
 // a record can be moved with one bulk copy.  Record r = slot * Hkv + kv_head.
 __host__ __device__ constexpr int rec_floats(int G, int D) { return (G * D + 2 * G + 3) / 4 * 4; }
+
+// The logits of one visible tile of one (sequence, KV head), [G][16 tokens] floats: the tiles of a
+// (sequence, KV head) lie one behind the other, the KV heads of a sequence behind each other.
+__host__ __device__ inline int64_t logit_tile(int tile_base, int n_tiles, int num_kv_heads, int kv_head, int tile, int G)
+{
+    return (((int64_t)tile_base * num_kv_heads + (int64_t)kv_head * n_tiles) + tile) * (16 * G);
+}
 
 // ---------------------------------------------------------------- mbarrier / bulk copy
 

@@ -184,7 +184,9 @@ struct MmaExtra {
 // MASKED: the variant launched when a RUN mask is given (ordinary attention plans): it can deal the
 // work list out again among the blocks; kept apart so that launches without a mask carry none of it.
 // WIDE: groups of 9..16 query heads: two 8-column tiles of heads per K/V tile instead of one.
-template <int D, bool DUP, int MODE, bool PREFIX, bool F16 = false, bool MASKED = false, bool WIDE = false>
+// EXT: windowed plans and plans that track weights.  Units then count visible positions (window.h), the
+// tiles at the edges of the gap are masked token by token, and the logits go to the workspace on request.
+template <int D, bool DUP, int MODE, bool PREFIX, bool F16 = false, bool MASKED = false, bool WIDE = false, bool EXT = false>
 __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const KernelParams p,
                                                                       const __grid_constant__ CUtensorMap k_map,
                                                                       const __grid_constant__ CUtensorMap v_map,
@@ -198,6 +200,12 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
     constexpr int kConsumerThreads = kMmaConsumerWarps * 32;
     constexpr int NT = WIDE ? 2 : 1;                          // 8-column tiles of query heads
     static_assert(!(WIDE && (DUP || PREFIX)), "wide groups: ordinary units, low parts of P in a second mma");
+    static_assert(!EXT || (MODE == kModeAttend && !PREFIX && !MASKED), "windows, weights: ordinary attention units");
+    // the tile of the sequence that visible tile v of a unit is
+    auto tile_of = [&](const WindowCut& w, int v) { return EXT ? window_tile(w, v) : v; };
+    auto cut_of = [&](const decode_attn_unit_t& x) { return EXT ? window_cut(x.seq_len, p.window, p.sinks) : WindowCut{0, 0, 0}; };
+    // does the unit hold its sequence's last position?
+    auto has_last = [&](const decode_attn_unit_t& x, const WindowCut& w) { return x.tok_end + 16 * w.skip_tiles == x.seq_len; };
 
     extern __shared__ uint8_t smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -285,6 +293,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
         // prefetches only (the loads below read them again, behind the wait), and an L2 prefetch
         // of the wrong line is harmless.
         const int unit_pages = (u.tok_end - u.tok_begin + 15) >> 4;
+        const WindowCut cut = cut_of(u);
         const int np = min(unit_pages, p.hint_first_pages);
         const bool masked = p.run_mask != nullptr && (u.kv_head >> 16) == 0 && __ldcg(p.run_mask + u.seq) == 0;
         // The same goes for what the first unit's critical path reads right behind the wait - the
@@ -294,8 +303,8 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
         // a line brought in early is never stale there.
         if (!masked) {
             const int32_t* const row = p.block_table + (int64_t)u.seq * p.max_pages_per_seq;
-            const int first = (u.tok_begin >> 4) >> p.tile_shift;
-            const int last = ((u.tok_begin >> 4) + min(unit_pages, 64) - 1) >> p.tile_shift;      // entries first .. last
+            const int first = tile_of(cut, u.tok_begin >> 4) >> p.tile_shift;
+            const int last = tile_of(cut, (u.tok_begin >> 4) + min(unit_pages, 64) - 1) >> p.tile_shift;      // entries first .. last
             if (unit_pages > 0 && lane * 32 <= last - first) prefetch_l2(row + first + lane * 32);
             if (MODE == kModeAttend) {
                 const char* const qrows = reinterpret_cast<const char*>(
@@ -305,7 +314,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
             }
         }
         if (lane < np && !masked) {
-            const int tile = (u.tok_begin >> 4) + lane;
+            const int tile = tile_of(cut, (u.tok_begin >> 4) + lane);
             const int id = __ldcg(p.block_table + (int64_t)u.seq * p.max_pages_per_seq + (tile >> p.tile_shift));
             if ((unsigned)id < (unsigned)p.num_pages) {
                 const int slot0 = (tile & ((1 << p.tile_shift) - 1)) << 4;
@@ -341,7 +350,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
         auto first_ids = [&](const decode_attn_unit_t& x, int end) {
             const int np = (end - x.tok_begin + 15) >> 4;
             const int32_t* t = p.block_table + (int64_t)x.seq * p.max_pages_per_seq;
-            return (lane < np) ? __ldg(t + (((x.tok_begin >> 4) + lane) >> ts)) : 0;
+            return (lane < np) ? __ldg(t + (tile_of(cut_of(x), (x.tok_begin >> 4) + lane) >> ts)) : 0;
         };
         // ---- launches with a RUN mask: the queue (see the top of the kernel)
         const int nb = p.n_work_blocks;
@@ -448,13 +457,14 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
             const int n_iters = (n_pages + kPagesPerStage - 1) / kPagesPerStage;
             const int32_t* bt = p.block_table + (int64_t)b * p.max_pages_per_seq;
             const int tile0 = t0 >> 4;                                    // first 16-token tile of the unit
+            const WindowCut cut = cut_of(u);
             int ids_next = ids_first;
             int ids_cur = 0;
             for (int it = 0; it < n_iters; ++it, ++git) {
                 if ((it & 7) == 0) {                                      // 32 page ids per 8 stages, one batch ahead
                     ids_cur = ids_next;
                     const int nxt = (it + 8) * kPagesPerStage + lane;
-                    ids_next = (nxt < n_pages) ? __ldg(bt + ((tile0 + nxt) >> ts)) : 0;
+                    ids_next = (nxt < n_pages) ? __ldg(bt + (tile_of(cut, tile0 + nxt) >> ts)) : 0;
                 }
                 const int s = git % NS;
                 if (git >= (uint32_t)NS) {
@@ -491,7 +501,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                     }
                     const uint32_t dst = base + s * Cfg::kStageBytes + which * Cfg::kTensorBytes +
                                          pg * Cfg::kPageBytes + hf * Cfg::kBoxBytes;
-                    const int slot0 = ((tile0 + it * kPagesPerStage + pg) & ((1 << ts) - 1)) << 4;   // of the tile within its page
+                    const int slot0 = (tile_of(cut, tile0 + it * kPagesPerStage + pg) & ((1 << ts) - 1)) << 4;   // of the tile within its page
                     tma_load_4d(dst, which ? &v_map : &k_map, full, hf * 64, slot0, g, page_id, l2_policy);
                     if (git == 0 && lane == 0) DA_TRACE_STAMP(blockIdx.x, 2);
 #ifdef DA_TRACE
@@ -543,6 +553,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
     struct Pre {
         int dev_len;
         int masked;
+        int tile_base;
         uint32_t qb[KSTEPS][NT][2];
     };
     auto prefetch = [&](const decode_attn_unit_t& x, Pre& o) {
@@ -551,6 +562,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
         if (MODE == kModeAttend) {
             o.dev_len = __ldg(p.seq_lens + x.seq);
             if (p.run_mask != nullptr) o.masked = __ldg(p.run_mask + x.seq) == 0;
+            if (EXT) o.tile_base = p.logits != nullptr ? p.seq_info[x.seq].tile_base : 0;
 #pragma unroll
             for (int nt = 0; nt < NT; ++nt) {
                 const int head = DUP ? (r & 3) : nt * 8 + r;
@@ -812,6 +824,12 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
             continue;
         }
 
+        const WindowCut cut = cut_of(u);
+        float* logits = nullptr;                              // of this (sequence, KV head), at the unit's first tile
+        if (EXT && p.logits != nullptr) {
+            const int n_tiles = ((u.seq_len + 15) >> 4) - cut.skip_tiles;
+            logits = p.logits + logit_tile(cur.tile_base, n_tiles, p.num_kv_heads, g, t0 >> 4, G);
+        }
         float oacc[D / 16][NT][4];
         float m_run[NT][2], l_run[NT][2];
 #pragma unroll
@@ -865,7 +883,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                         *reinterpret_cast<uint4*>(ex.v_out + o) = vv;
                     }
                 } else {
-                    if (p.new_k != nullptr && nseq == 0 && tok0 + n_valid == u.seq_len) {
+                    if (p.new_k != nullptr && nseq == 0 && tok0 + n_valid + 16 * cut.skip_tiles == u.seq_len) {
                         // Fused own-layer KV write (Algorithm 1 step 2: the row's K/V is written, then the row
                         // attends over it).  This page holds the sequence's last position, whose K and V rows
                         // are the new ones: they replace what TMA brought from the pool in the staged tiles -
@@ -897,6 +915,24 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                         __syncwarp();
                     }
+                    // Rows [hide0, hide1) of the tile lie between the sinks and the window: their logits count as
+                    // -inf, and their V rows are cleared like those past the end (a zero weight does not silence
+                    // what a row that is not seen may hold).  Only the tiles at the edges of the gap have any.
+                    int hide0 = 0, hide1 = 0;
+                    if (EXT) {
+                        const int at = tile_of(cut, tok0 >> 4) << 4;
+                        hide0 = min(max(p.sinks - at, 0), 16);
+                        hide1 = min(max(cut.first - at, 0), n_valid);
+                        if (hide0 < hide1) {
+                            for (int i = lane; i < (hide1 - hide0) * (D / 8); i += 32) {
+                                const int row = hide0 + i / (D / 8), ch = i % (D / 8);
+                                const uint32_t a = vpage + (ch >> 3) * Cfg::kBoxBytes + swz(row, ch & 7);
+                                asm volatile("st.shared.v4.u32 [%0], {%1,%1,%1,%1};" ::"r"(a), "r"(0u) : "memory");
+                            }
+                            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                            __syncwarp();
+                        }
+                    }
                     // ---- S^T = K . Q^T
                     float sacc[NT][4];
 #pragma unroll
@@ -911,7 +947,8 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                         for (int nt = 0; nt < NT; ++nt) In::mma(sacc[nt], a, qb[ks][nt][0], qb[ks][nt][1]);
                     }
                     // ---- online softmax on the fragment: rows r, r+8 (tokens), columns 2c, 2c+1 (heads)
-                    const bool v_lo = r < n_valid, v_hi = (r + 8) < n_valid;
+                    const bool v_lo = r < n_valid && !(EXT && r >= hide0 && r < hide1);
+                    const bool v_hi = (r + 8) < n_valid && !(EXT && r + 8 >= hide0 && r + 8 < hide1);
                     uint32_t b0[NT], b1[NT], b0l[NT], b1l[NT];
 #pragma unroll
                     for (int nt = 0; nt < NT; ++nt) {
@@ -919,6 +956,19 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                         float s01 = v_lo ? sacc[nt][1] * p.scale_log2 : -INFINITY;
                         float s10 = v_hi ? sacc[nt][2] * p.scale_log2 : -INFINITY;
                         float s11 = v_hi ? sacc[nt][3] * p.scale_log2 : -INFINITY;
+                        if (EXT && logits != nullptr) {
+                            // (columns past the group, and the duplicated ones, hold nothing of their own)
+                            float* const to = logits + (int64_t)page_idx * (16 * G) + r;
+                            const int h0 = nt * 8 + 2 * c;
+                            if (h0 < G && !lo_role) {
+                                __stcg(to + h0 * 16, s00);
+                                __stcg(to + h0 * 16 + 8, s10);
+                            }
+                            if (h0 + 1 < G && !lo_role) {
+                                __stcg(to + (h0 + 1) * 16, s01);
+                                __stcg(to + (h0 + 1) * 16 + 8, s11);
+                            }
+                        }
                         float mx0 = fmaxf(s00, s10), mx1 = fmaxf(s01, s11);
 #pragma unroll
                         for (int off = 4; off <= 16; off <<= 1) {
@@ -1015,7 +1065,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
         if (n_pages == 0) {
             // Nothing was read (a masked row, an empty split, a sequence of length 0): the empty
             // result is written straight away - no states to merge, no barrier, the scratch untouched.
-            if (MODE == kModeAttend && warp == 0 && nseq == 0 && u.tok_end == u.seq_len && u.tok_end > u.tok_begin)
+            if (MODE == kModeAttend && warp == 0 && nseq == 0 && has_last(u, cut) && u.tok_end > u.tok_begin)
                 append_new_row<D>(p, b, g, u.seq_len, lane);              // a masked row still writes its K/V
             block_finish_empty<D>(p, u, G, tid, kConsumerThreads);
             if (uid == ubeg && tid == 0) DA_TRACE_STAMP(blockIdx.x, 6);
@@ -1148,6 +1198,9 @@ inline int make_pool_map(CUtensorMap* map, const void* pool, const decode_attn_s
 
 typedef void (*mma_kernel_t)(const KernelParams, const CUtensorMap, const CUtensorMap, const int, const MmaExtra);
 
+// The variants for windowed plans and plans that track weights (compiled in kernel_mma_ext.cu).
+mma_kernel_t mma_ext_kernel_for(int D, int G, bool f16);
+
 // f16: q, K and V are fp16 (attention mode); else bf16.
 template <int MODE>
 inline mma_kernel_t mma_kernel_for(int D, int G, bool prefix = false, bool f16 = false, bool masked = false)
@@ -1213,9 +1266,10 @@ inline int mma_smem_bytes(int D, int G)
 }
 
 template <int MODE>
-inline int mma_prepare(int D, int G, mma_kernel_t* fn_out, bool prefix = false, bool f16 = false, bool masked = false)
+inline int mma_prepare(int D, int G, mma_kernel_t* fn_out, bool prefix = false, bool f16 = false, bool masked = false,
+                       bool ext = false)
 {
-    mma_kernel_t fn = mma_kernel_for<MODE>(D, G, prefix, f16, masked);
+    mma_kernel_t fn = ext ? mma_ext_kernel_for(D, G, f16) : mma_kernel_for<MODE>(D, G, prefix, f16, masked);
     if (!fn) return DA_ERR_UNSUPPORTED;
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, mma_smem_bytes(D, G)) != cudaSuccess) {
         (void)cudaGetLastError();
@@ -1225,10 +1279,11 @@ inline int mma_prepare(int D, int G, mma_kernel_t* fn_out, bool prefix = false, 
     return DA_OK;
 }
 
-inline int mma_query_occupancy(int D, int G, int* block_threads, int* dyn_smem, bool prefix = false, bool f16 = false)
+inline int mma_query_occupancy(int D, int G, int* block_threads, int* dyn_smem, bool prefix = false, bool f16 = false,
+                               bool ext = false)
 {
     mma_kernel_t fn;
-    if (mma_prepare<kModeAttend>(D, G, &fn, prefix, f16) != DA_OK) return -1;
+    if (mma_prepare<kModeAttend>(D, G, &fn, prefix, f16, false, ext) != DA_OK) return -1;
     *block_threads = kMmaThreads;
     *dyn_smem = mma_smem_bytes(D, G);
     int n = 0;
@@ -1247,7 +1302,8 @@ inline int mma_launch_mode(const decode_attn_shape_t& s, int G, const KernelPara
     // (the probe and gather modes only move 16-bit words: one variant serves both input types)
     const bool masked = MODE == kModeAttend && !prefix && kp.run_mask != nullptr &&
                         (kp.grid_exit ? kp.may_rank != 0 : kp.n_ranked > 0);
-    int rc = mma_prepare<MODE>(s.head_dim, G, &fn, prefix, MODE == kModeAttend && s.kv_dtype == DA_DTYPE_FP16, masked);
+    const bool ext = MODE == kModeAttend && (kp.window > 0 || kp.logits != nullptr);
+    int rc = mma_prepare<MODE>(s.head_dim, G, &fn, prefix, MODE == kModeAttend && s.kv_dtype == DA_DTYPE_FP16, masked, ext);
     if (rc != DA_OK) return rc;
     CUtensorMap kmap, vmap;
     rc = make_pool_map(&kmap, kp.k, s, s.k_stride_page, s.k_stride_token, s.k_stride_head);

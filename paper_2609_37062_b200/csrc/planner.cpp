@@ -22,6 +22,8 @@
 //    neighbouring addresses of the same pages.
 #include "planner.h"
 
+#include "window.h"
+
 #include <algorithm>
 #include <cmath>
 #include <functional>
@@ -84,6 +86,10 @@ int validate_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
     } else if (p.kernel == DA_KERNEL_UMMA_PREFIX) {
         return DA_ERR_UNSUPPORTED;   // that kernel serves shared-prefix plans only
     }
+    if (p.window_tokens < 0 || p.sink_tokens < 0 || (p.sink_tokens > 0 && p.window_tokens == 0)) return DA_ERR_INVALID_ARG;
+    if (p.track_weights != 0 && p.track_weights != 1) return DA_ERR_INVALID_ARG;
+    if ((p.window_tokens > 0 || p.track_weights) && (p.shared_prefix_tokens > 0 || p.kernel == DA_KERNEL_SIMT))
+        return DA_ERR_UNSUPPORTED;
     for (int32_t r : p.reserved)
         if (r != 0) return DA_ERR_INVALID_ARG;
     return DA_OK;
@@ -163,12 +169,23 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
     const int64_t prefix_tokens = p.shared_prefix_tokens;
     const int64_t prefix_pages = prefix_tokens / P;
     std::vector<int64_t> pages(B);
+    // With a window the plan covers the visible positions: whole tiles that no query sees are taken
+    // out of the sequence (see window.h), and everything below works on what is left of its length.
+    std::vector<int32_t>& visible = out.visible;
+    visible.resize(B);
+    int64_t tiles = 0;
+    out.tile_base.resize(B);
     for (int b = 0; b < B; ++b) {
         if (seq_lens[b] < 0) return DA_ERR_INVALID_ARG;
         if (ceil_div(seq_lens[b], s.page_size) > s.max_pages_per_seq) return DA_ERR_INVALID_ARG;
         if (seq_lens[b] < prefix_tokens) return DA_ERR_INVALID_ARG;   // every sequence contains the prefix
-        pages[b] = ceil_div(seq_lens[b] - prefix_tokens, P);
+        visible[b] = seq_lens[b] - P * window_cut(seq_lens[b], p.window_tokens, p.sink_tokens).skip_tiles;
+        pages[b] = ceil_div(visible[b] - prefix_tokens, P);
+        out.tile_base[b] = (int32_t)tiles;
+        tiles += ceil_div(visible[b], P);
     }
+    out.n_tiles = tiles;
+    if (p.track_weights && tiles > INT32_MAX) return DA_ERR_UNSUPPORTED;
 
     std::vector<SeqCut> cuts(B);
     out.chunk_tokens = 0;
@@ -333,7 +350,7 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
             decode_attn_unit_t u;
             u.seq = b;
             u.tok_begin = (int32_t)((prefix_pages + pb) * P);
-            u.tok_end = (int32_t)std::min<int64_t>((prefix_pages + pe) * P, seq_lens[b]);
+            u.tok_end = (int32_t)std::min<int64_t>((prefix_pages + pe) * P, visible[b]);
             if (u.tok_end < u.tok_begin) u.tok_end = u.tok_begin;
             u.slot = base_slot >= 0 ? (int32_t)(base_slot + PC + i) : -1;
             u.seq_len = seq_lens[b];
