@@ -383,6 +383,62 @@ int decode_attn_add_weights(const decode_attn_plan_t *plan, const void *workspac
                             const int32_t *seq_lens, const float *weights, float *weights_out, int64_t tokens,
                             int64_t stride_seq, int64_t stride_head, cudaStream_t stream);
 
+/* Eviction from the cache by accumulated attention weight.  For every
+ * sequence that holds more than budget_tokens, and for each of its KV heads by
+ * itself, the first sink_tokens and the last recent_tokens stay, and of the
+ * tokens between them the budget_tokens - sink_tokens - recent_tokens with
+ * the largest totals (decode_attn_add_weights); among equal totals the lowest
+ * position stays, NaN counts as -inf.  What stays keeps its order: the K and
+ * V rows of a KV head's j-th kept token are copied, bit for bit, to position
+ * j of the pages that the sequence's row of dst_block_table names.  The
+ * caller then uses that row (and the new length) for the sequence and takes
+ * its old pages back; sequences within the budget keep their pages, and
+ * their rows of dst_block_table are not read.
+ *
+ * The pages named by dst_block_table must be fresh: none may be a page that
+ * any sequence of the call reads or be named twice (decode_attn_validate_evict
+ * checks this on the host); pages shared by several rows are therefore left
+ * whole.  Positions in the cache shift: it is for models whose keys carry
+ * their position before they are cached.
+ *
+ * Two launches on `stream`, nothing is allocated, capture-safe (the lengths
+ * are read on the device).  A row whose length does not fit the block table
+ * or the totals is left alone (DA_ERR_STALE_PLAN), a token whose page id lies
+ * outside the pool is not moved (DA_ERR_BAD_PAGE); either is recorded in
+ * `status` when one is given. */
+typedef struct {
+    uint32_t struct_size;       /* sizeof(decode_attn_evict_args_t) */
+    uint32_t flags;             /* must be 0 */
+    int32_t budget_tokens;      /* >= 1 */
+    int32_t sink_tokens;        /* sink_tokens + recent_tokens <= budget_tokens */
+    int32_t recent_tokens;
+    int32_t dst_max_pages;      /* row stride of dst_block_table; at least ceil(budget_tokens / page_size) */
+    const int32_t *seq_lens;            /* device, [batch] */
+    const int32_t *block_table;         /* device, [batch, shape.max_pages_per_seq] */
+    const int32_t *dst_block_table;     /* device, [batch, dst_max_pages] */
+    void *k_cache;                      /* device pools of the shape, 16-byte aligned, modified */
+    void *v_cache;
+    const float *weights;       /* device, fp32 totals; the row of (b, g) starts at b * stride_seq + g * stride_head
+                                   and holds weight_tokens values, at least the longest sequence */
+    float *weights_out;         /* device, laid out the same: the totals of what stays, then zeros up to the old
+                                   length; may be `weights`, must not overlap it otherwise */
+    int64_t weight_tokens, stride_seq, stride_head;
+    int32_t *kept;              /* device, [batch, num_kv_heads, budget_tokens]: the positions that stay, ascending,
+                                   -1 behind them */
+    int32_t *seq_lens_out;      /* device, [batch]: min(seq_len, budget_tokens); not the buffer of seq_lens */
+    int32_t *status;            /* device, one word that the call lowers to the worst condition met, or NULL */
+} decode_attn_evict_args_t;
+
+int decode_attn_evict(const decode_attn_shape_t *shape, const decode_attn_evict_args_t *args, cudaStream_t stream);
+
+/* Host-only check of an eviction: the numbers of `args` (its pointers are not
+ * looked at), the lengths and the source pages against the shape, and that
+ * the destination pages of every sequence over the budget lie in the pool,
+ * are read by no sequence and named once (DA_ERR_BAD_PAGE otherwise). */
+int decode_attn_validate_evict(const decode_attn_shape_t *shape, const decode_attn_evict_args_t *args,
+                               const int32_t *seq_lens_host, const int32_t *block_table_host,
+                               const int32_t *dst_block_table_host);
+
 /* Synchronises `stream`, returns the worst condition the kernels recorded
  * since the last call (DA_OK, DA_ERR_STALE_PLAN, DA_ERR_BAD_PAGE,
  * DA_ERR_TIMEOUT) and clears it.  For tests and debugging.  plan == NULL

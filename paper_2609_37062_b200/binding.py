@@ -56,7 +56,7 @@ EXPORTED = [
     "decode_attn_step_static", "decode_attn_append_kv", "decode_attn_breakeven_tokens",
     "decode_attn_switch_thresholds", "decode_attn_switch_next", "decode_attn_validate_shared_prefix",
     "decode_attn_merge_shards", "decode_attn_append_kv_checked", "decode_attn_debug_expire_wait",
-    "decode_attn_add_weights",
+    "decode_attn_add_weights", "decode_attn_evict", "decode_attn_validate_evict",
 ]
 
 
@@ -105,6 +105,17 @@ class RunArgs(ctypes.Structure):
                 ("new_k", ctypes.c_void_p), ("new_v", ctypes.c_void_p)]
 
 
+class EvictArgs(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+                ("budget_tokens", ctypes.c_int32), ("sink_tokens", ctypes.c_int32),
+                ("recent_tokens", ctypes.c_int32), ("dst_max_pages", ctypes.c_int32),
+                ("seq_lens", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+                ("dst_block_table", ctypes.c_void_p), ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p),
+                ("weights", ctypes.c_void_p), ("weights_out", ctypes.c_void_p),
+                ("weight_tokens", ctypes.c_int64), ("stride_seq", ctypes.c_int64), ("stride_head", ctypes.c_int64),
+                ("kept", ctypes.c_void_p), ("seq_lens_out", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
 _vp = ctypes.c_void_p
 _lib.decode_attn_plan_layout.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Policy), _vp, ctypes.c_int32,
                                          ctypes.c_int32, _vp, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64),
@@ -134,6 +145,8 @@ _lib.decode_attn_append_kv_checked.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp
 _lib.decode_attn_debug_expire_wait.argtypes = [_vp, ctypes.POINTER(RunArgs), ctypes.c_int64, _vp]
 _lib.decode_attn_merge_shards.argtypes = [ctypes.POINTER(Shape), ctypes.c_int32, _vp, _vp, _vp, _vp, _vp]
 _lib.decode_attn_add_weights.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp] + [ctypes.c_int64] * 3 + [_vp]
+_lib.decode_attn_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(EvictArgs), _vp]
+_lib.decode_attn_validate_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(EvictArgs), _vp, _vp, _vp]
 _lib.decode_attn_breakeven_tokens.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int32,
                                               ctypes.c_double, ctypes.POINTER(ctypes.c_double)]
 _lib.decode_attn_switch_thresholds.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double),
@@ -349,6 +362,44 @@ def decode_attn_add_weights(plan: Plan, workspace, lse, seq_lens, weights, weigh
     if check:
         _check(rc, "decode_attn_add_weights")
     return rc
+
+
+def _evict_args(budget_tokens, sink_tokens, recent_tokens, dst_max_pages) -> EvictArgs:
+    a = EvictArgs()
+    a.struct_size = ctypes.sizeof(EvictArgs)
+    a.budget_tokens, a.sink_tokens, a.recent_tokens = budget_tokens, sink_tokens, recent_tokens
+    a.dst_max_pages = dst_max_pages
+    return a
+
+
+def decode_attn_evict(shape: Shape, budget_tokens: int, sink_tokens: int, recent_tokens: int, seq_lens, block_table,
+                      dst_block_table, k_cache, v_cache, weights, weights_out, kept, seq_lens_out, status=None,
+                      stream=None, check: bool = True) -> int:
+    """weights, weights_out: fp32 [batch, num_kv_heads, tokens] (weights_out None: in place); kept: int32 [batch,
+    num_kv_heads, budget_tokens]; seq_lens_out: int32 [batch]; status: int32 [1] or None."""
+    if weights_out is None:
+        weights_out = weights
+    if weights.shape != weights_out.shape or weights.stride() != weights_out.stride() or weights.stride(2) != 1 or \
+            weights.shape[0] < shape.batch or weights.shape[1] != shape.num_kv_heads or \
+            kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous():
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_evict")
+    a = _evict_args(budget_tokens, sink_tokens, recent_tokens, dst_block_table.shape[1])
+    a.seq_lens, a.block_table, a.dst_block_table = _ptr(seq_lens), _ptr(block_table), _ptr(dst_block_table)
+    a.k_cache, a.v_cache = _ptr(k_cache), _ptr(v_cache)
+    a.weights, a.weights_out = _ptr(weights), _ptr(weights_out)
+    a.weight_tokens, a.stride_seq, a.stride_head = weights.shape[2], weights.stride(0), weights.stride(1)
+    a.kept, a.seq_lens_out, a.status = _ptr(kept), _ptr(seq_lens_out), _ptr(status)
+    rc = _lib.decode_attn_evict(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
+    if check:
+        _check(rc, "decode_attn_evict")
+    return rc
+
+
+def decode_attn_validate_evict(shape: Shape, budget_tokens: int, sink_tokens: int, recent_tokens: int, seq_lens_host,
+                               block_table_host, dst_block_table_host) -> int:
+    lens, bt, dst = _host_i32(seq_lens_host), _host_i32(block_table_host), _host_i32(dst_block_table_host)
+    a = _evict_args(budget_tokens, sink_tokens, recent_tokens, dst.shape[1])
+    return _lib.decode_attn_validate_evict(ctypes.byref(shape), ctypes.byref(a), _ptr(lens), _ptr(bt), _ptr(dst))
 
 
 def decode_attn_last_device_status(plan: Optional[Plan], stream=None) -> int:
