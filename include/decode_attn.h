@@ -359,6 +359,76 @@ int decode_attn_merge_shards(const decode_attn_shape_t *shape, int32_t n_shards,
 int decode_attn_combine(const decode_attn_plan_t *plan, const void *workspace, void *out,
                         float *lse_or_null, cudaStream_t stream);
 
+/* ---------------------------------------------------------------------------
+ * Prompts.  Attention of several new tokens per sequence over the same paged
+ * cache: the last new_lens[b] positions of sequence b, whose K/V has been
+ * written already, are queries; the query at position i sees the positions
+ * t <= i with i - t < window_tokens or t < sink_tokens (all of t <= i without
+ * a window).  A whole prompt is new_lens = seq_lens; a later chunk of one
+ * (chunked prefill, or a few speculated tokens) has fewer.
+ *
+ * q and out hold the new tokens of all sequences one behind the other.
+ * ------------------------------------------------------------------------- */
+typedef struct decode_attn_prompt_plan decode_attn_prompt_plan_t; /* opaque, library-owned */
+
+/* One unit of work: up to 2 * floor(128 / group) consecutive new tokens of one
+ * sequence with the query heads of one KV head, against a range of 128-token
+ * K/V tiles.  Tiles are counted in the unit's own list: the first sink_tiles
+ * tiles of the sequence, then those from window_tile on. */
+typedef struct {
+    int32_t seq;          /* b                                                                       */
+    int32_t kv_head;      /* g                                                                       */
+    int32_t row;          /* first token's row of q and out                                          */
+    int32_t n_tok;        /* tokens                                                                  */
+    int32_t pos;          /* first token's position in the sequence                                  */
+    int32_t seq_len;      /* the length the plan was made for (checked against device seq_lens)      */
+    int32_t sink_tiles;
+    int32_t window_tile;
+    int32_t tile_begin;
+    int32_t tile_end;
+    int32_t slot;         /* index of the partial record in the workspace, -1: writes `out` directly  */
+    int32_t n_pieces;     /* units that share these tokens and this KV head                          */
+} decode_attn_prompt_unit_t;
+
+/* The pure host function behind decode_attn_prompt_plan: the work list, and
+ * for every thread block the first of its units.  units_out and
+ * block_begin_out may be NULL to query the sizes. */
+int decode_attn_prompt_plan_layout(const decode_attn_shape_t *shape, const decode_attn_policy_t *policy,
+                                   const int32_t *new_lens_host, const int32_t *seq_lens_host, int32_t sm_count,
+                                   decode_attn_prompt_unit_t *units_out, int64_t max_units, int64_t *n_units_out,
+                                   int32_t *block_begin_out, int64_t max_blocks, int64_t *n_blocks_out);
+
+/* Builds a plan: new_lens_host and seq_lens_host [batch] on the host, seq_lens
+ * counting the new tokens.  The policy's window_tokens, sink_tokens, sm_count,
+ * split_mode (AUTO: work dealt evenly to the SMs, cutting units where shares
+ * meet; DETERMINISTIC: units cut at multiples of chunk_tokens - of 128, 0:
+ * 4,096 - of their own tile lists, so that a sequence's bits do not depend on
+ * the batch) and chunk_tokens apply; everything else must be 0
+ * (DA_ERR_UNSUPPORTED).  Buffers, upload and lifetime are those of
+ * decode_attn_plan. */
+int decode_attn_prompt_plan(const decode_attn_shape_t *shape, const decode_attn_policy_t *policy,
+                            const int32_t *new_lens_host, const int32_t *seq_lens_host,
+                            decode_attn_prompt_plan_t **plan_out, size_t *workspace_bytes_out);
+
+int decode_attn_prompt_plan_destroy(decode_attn_prompt_plan_t *plan);
+
+/* One launch on `stream`, or two where units were cut.  Nothing is allocated,
+ * capture-safe.
+ *   q            device, shape.q_dtype [new tokens, num_q_heads, head_dim], contiguous, 16-byte aligned
+ *   k_cache, v_cache, block_table, seq_lens  as for decode_attn_run; block-table
+ *                entries of pages no query sees are never read
+ *   out          device, [new tokens, num_q_heads, head_dim] in shape.out_dtype, 16-byte aligned
+ *   lse_or_null  device, fp32 [new tokens, num_q_heads] or NULL
+ *   workspace    device, >= workspace_bytes from the plan, 256-byte aligned (may be NULL if 0)
+ * Weights are rounded once to the 16-bit input type ahead of the product with V;
+ * sums, maxima and accumulators are fp32. */
+int decode_attn_prompt_run(const decode_attn_prompt_plan_t *plan, const void *q, const void *k_cache, const void *v_cache,
+                           const int32_t *block_table, const int32_t *seq_lens, void *out, float *lse_or_null,
+                           void *workspace, size_t workspace_bytes, cudaStream_t stream);
+
+/* decode_attn_last_device_status of a prompt plan. */
+int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan, cudaStream_t stream);
+
 /* Running totals of attention weights, what an eviction by attention weight
  * ranks a cache by (decode_attn_evict).  For plans made with
  * policy.track_weights (DA_ERR_UNSUPPORTED otherwise), behind

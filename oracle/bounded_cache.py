@@ -36,10 +36,11 @@ def rows_of(inp: PagedInputs, b: int, positions, which: str) -> np.ndarray:
     return decode_bits(bits, bool(s.in_fp16)).reshape(bits.shape)
 
 
-def attention(inp: PagedInputs, new_lens, window: int = 0, sinks: int = 0, scale=None, run_mask=None):
+def attention(inp: PagedInputs, new_lens, window: int = 0, sinks: int = 0, scale=None, run_mask=None, absolute=False):
     """inp.q holds the rows of all sequences' last new_lens[b] positions, one sequence behind the other.
     Returns out [rows, Hq, D], lse [rows, Hq] and, per sequence, the attention weight of every position summed
-    over its queries and over the query heads of a KV head: [Hkv, seq_len]."""
+    over its queries and over the query heads of a KV head: [Hkv, seq_len].  absolute: out from |V| (what relative
+    errors of the weights are multiplied with)."""
     G = inp.Hq // inp.Hkv
     scale = default_scale(inp.D) if scale is None else scale
     q = decode_bits(inp.q, bool(inp.shape.in_fp16)).reshape(inp.q.shape)
@@ -60,6 +61,7 @@ def attention(inp: PagedInputs, new_lens, window: int = 0, sinks: int = 0, scale
         used = m.any(0)
         t, m = t[used], m[:, used]
         k, v = rows_of(inp, b, t, "k"), rows_of(inp, b, t, "v")
+        v = np.abs(v) if absolute else v
         for g in range(inp.Hkv):
             for h in range(g * G, (g + 1) * G):
                 with np.errstate(invalid="ignore"):

@@ -57,6 +57,8 @@ EXPORTED = [
     "decode_attn_switch_thresholds", "decode_attn_switch_next", "decode_attn_validate_shared_prefix",
     "decode_attn_merge_shards", "decode_attn_append_kv_checked", "decode_attn_debug_expire_wait",
     "decode_attn_add_weights", "decode_attn_evict", "decode_attn_validate_evict",
+    "decode_attn_prompt_plan_layout", "decode_attn_prompt_plan", "decode_attn_prompt_plan_destroy",
+    "decode_attn_prompt_run", "decode_attn_prompt_last_device_status",
 ]
 
 
@@ -105,6 +107,12 @@ class RunArgs(ctypes.Structure):
                 ("new_k", ctypes.c_void_p), ("new_v", ctypes.c_void_p)]
 
 
+class PromptUnit(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in
+                ("seq", "kv_head", "row", "n_tok", "pos", "seq_len", "sink_tiles", "window_tile", "tile_begin", "tile_end",
+                 "slot", "n_pieces")]
+
+
 class EvictArgs(ctypes.Structure):
     _fields_ = [("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
                 ("budget_tokens", ctypes.c_int32), ("sink_tokens", ctypes.c_int32),
@@ -145,6 +153,14 @@ _lib.decode_attn_append_kv_checked.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp
 _lib.decode_attn_debug_expire_wait.argtypes = [_vp, ctypes.POINTER(RunArgs), ctypes.c_int64, _vp]
 _lib.decode_attn_merge_shards.argtypes = [ctypes.POINTER(Shape), ctypes.c_int32, _vp, _vp, _vp, _vp, _vp]
 _lib.decode_attn_add_weights.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp] + [ctypes.c_int64] * 3 + [_vp]
+_lib.decode_attn_prompt_plan_layout.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Policy), _vp, _vp, ctypes.c_int32,
+                                                _vp, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64), _vp, ctypes.c_int64,
+                                                ctypes.POINTER(ctypes.c_int64)]
+_lib.decode_attn_prompt_plan.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Policy), _vp, _vp, ctypes.POINTER(_vp),
+                                         ctypes.POINTER(ctypes.c_size_t)]
+_lib.decode_attn_prompt_plan_destroy.argtypes = [_vp]
+_lib.decode_attn_prompt_run.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, ctypes.c_size_t, _vp]
+_lib.decode_attn_prompt_last_device_status.argtypes = [_vp, _vp]
 _lib.decode_attn_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(EvictArgs), _vp]
 _lib.decode_attn_validate_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(EvictArgs), _vp, _vp, _vp]
 _lib.decode_attn_breakeven_tokens.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int32,
@@ -362,6 +378,70 @@ def decode_attn_add_weights(plan: Plan, workspace, lse, seq_lens, weights, weigh
     if check:
         _check(rc, "decode_attn_add_weights")
     return rc
+
+
+def decode_attn_prompt_plan_layout(shape: Shape, policy: Policy, new_lens, seq_lens, sm_count: int):
+    """Host-only planner of prompts: (units, block_begin)."""
+    new, lens = _host_i32(new_lens), _host_i32(seq_lens)
+    n_units, n_blocks = ctypes.c_int64(), ctypes.c_int64()
+    args = (ctypes.byref(shape), ctypes.byref(policy), _ptr(new), _ptr(lens), sm_count)
+    _check(_lib.decode_attn_prompt_plan_layout(*args, None, 0, ctypes.byref(n_units), None, 0, ctypes.byref(n_blocks)),
+           "decode_attn_prompt_plan_layout")
+    units = (PromptUnit * max(1, n_units.value))()
+    begin = np.zeros(n_blocks.value + 1, dtype=np.int32)
+    _check(_lib.decode_attn_prompt_plan_layout(*args, ctypes.addressof(units), n_units.value, ctypes.byref(n_units),
+                                               _ptr(begin), n_blocks.value, ctypes.byref(n_blocks)),
+           "decode_attn_prompt_plan_layout")
+    return [units[i] for i in range(n_units.value)], begin
+
+
+class PromptPlan:
+    """Owner of one decode_attn_prompt_plan_t."""
+
+    def __init__(self, handle: int, workspace_bytes: int, shape: Shape, policy: Policy):
+        self.handle = handle
+        self.workspace_bytes = workspace_bytes
+        self.shape = shape
+        self.policy = policy
+
+    def destroy(self) -> None:
+        if self.handle:
+            _lib.decode_attn_prompt_plan_destroy(self.handle)
+            self.handle = None
+
+    def __del__(self):
+        try:
+            self.destroy()
+        except Exception:
+            pass
+
+
+def decode_attn_prompt_plan(shape: Shape, policy: Policy, new_lens_host, seq_lens_host) -> PromptPlan:
+    new, lens = _host_i32(new_lens_host), _host_i32(seq_lens_host)
+    handle = _vp()
+    ws = ctypes.c_size_t()
+    _check(_lib.decode_attn_prompt_plan(ctypes.byref(shape), ctypes.byref(policy), _ptr(new), _ptr(lens),
+                                        ctypes.byref(handle), ctypes.byref(ws)), "decode_attn_prompt_plan")
+    return PromptPlan(handle.value, ws.value, shape, policy)
+
+
+def decode_attn_prompt_plan_destroy(plan: PromptPlan) -> None:
+    plan.destroy()
+
+
+def decode_attn_prompt_run(plan: PromptPlan, q, k_cache, v_cache, block_table, seq_lens, out, lse=None, workspace=None,
+                           workspace_bytes: Optional[int] = None, stream=None, check: bool = True) -> int:
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    rc = _lib.decode_attn_prompt_run(plan.handle, _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(seq_lens),
+                                     _ptr(out), _ptr(lse), _ptr(workspace), workspace_bytes, _stream(stream))
+    if check:
+        _check(rc, "decode_attn_prompt_run")
+    return rc
+
+
+def decode_attn_prompt_last_device_status(plan: PromptPlan, stream=None) -> int:
+    return _lib.decode_attn_prompt_last_device_status(plan.handle, _stream(stream))
 
 
 def _evict_args(budget_tokens, sink_tokens, recent_tokens, dst_max_pages) -> EvictArgs:

@@ -19,6 +19,7 @@
 #include "kernel_umma.cuh"
 #include "kernel_simt.cuh"
 #include "planner.h"
+#include "prompt_launch.h"
 #include "weights.cuh"
 
 using namespace da;
@@ -63,6 +64,20 @@ struct decode_attn_plan {
     cudaEvent_t upload_done = nullptr;  // last refresh of the device work list
     cudaEvent_t launch_done = nullptr;  // behind the plan's last launch on a caller's stream (not while capturing)
     mutable bool upload_pending = false;   // the first upload may still be in flight on the plan's own stream
+    void* buffers = nullptr;            // PlanBuffers*, returned to the cache on destroy
+};
+
+struct decode_attn_prompt_plan {
+    decode_attn_shape_t shape;
+    decode_attn_policy_t policy;
+    PromptLayout layout;
+    int device = -1;
+    float scale = 0.f;
+    size_t workspace_bytes = 0;
+    char* dev = nullptr;
+    size_t off_block_begin = 0, off_merges = 0, off_status = 0;
+    cudaEvent_t upload_done = nullptr, launch_done = nullptr;
+    mutable bool upload_pending = false;
     void* buffers = nullptr;            // PlanBuffers*, returned to the cache on destroy
 };
 
@@ -421,7 +436,8 @@ bool stream_is_capturing(cudaStream_t stream)
 // that reads the device buffer is ordered behind that upload: a device-side wait on the caller's
 // stream while the copy may still be in flight (a host-side one while that stream is being
 // captured, so that no outside event enters the graph), nothing once it is known to be complete.
-int order_behind_upload(const decode_attn_plan_t* pl, cudaStream_t stream)
+template <class Plan>
+int order_behind_upload(const Plan* pl, cudaStream_t stream)
 {
     if (!pl->upload_pending) return DA_OK;
     const cudaError_t q = cudaEventQuery(pl->upload_done);
@@ -444,7 +460,8 @@ int order_behind_upload(const decode_attn_plan_t* pl, cudaStream_t stream)
 // not handed to another plan's upload while they run (see release_buffers).  Launches that are
 // being captured into a graph run later, at replay: a plan must outlive the replays of a graph
 // that holds its launches, as the header says.
-void mark_launched(const decode_attn_plan_t* pl, cudaStream_t stream)
+template <class Plan>
+void mark_launched(const Plan* pl, cudaStream_t stream)
 {
     if (pl->launch_done == nullptr || stream_is_capturing(stream)) return;
     if (cudaEventRecord(pl->launch_done, stream) != cudaSuccess) (void)cudaGetLastError();
@@ -837,6 +854,127 @@ int decode_attn_add_weights(const decode_attn_plan_t* pl, const void* workspace,
     if (rc != DA_OK) return rc;
     mark_launched(pl, stream);
     return DA_OK;
+}
+
+int decode_attn_prompt_plan(const decode_attn_shape_t* shape, const decode_attn_policy_t* policy, const int32_t* new_lens_host,
+                            const int32_t* seq_lens_host, decode_attn_prompt_plan_t** plan_out, size_t* workspace_bytes_out)
+{
+    if (!shape || !policy || !plan_out) return DA_ERR_INVALID_ARG;
+    int rc = validate_shape(*shape);
+    if (rc != DA_OK) return rc;
+    rc = validate_prompt_policy(*shape, *policy);
+    if (rc != DA_OK) return rc;
+    decode_attn_prompt_plan_t* pl = new (std::nothrow) decode_attn_prompt_plan_t();
+    if (!pl) return DA_ERR_INVALID_ARG;
+    struct Guard {
+        decode_attn_prompt_plan_t* p;
+        ~Guard() { if (p) decode_attn_prompt_plan_destroy(p); }
+    } guard{pl};
+    pl->shape = *shape;
+    pl->policy = *policy;
+    pl->scale = shape->sm_scale > 0.f ? shape->sm_scale : 1.0f / sqrtf((float)shape->head_dim);
+    DA_CUDA_TRY(cudaGetDevice(&pl->device));
+    int sm_count = policy->sm_count;
+    if (sm_count == 0) {
+        rc = device_sm_count(pl->device, &sm_count);
+        if (rc != DA_OK) return rc;
+    }
+    PromptLayout& lay = pl->layout;
+    rc = make_prompt_layout(*shape, *policy, new_lens_host, seq_lens_host, sm_count, lay);
+    if (rc != DA_OK) return rc;
+    if ((int64_t)lay.merges.size() > 0x7fffffffLL / 64) return DA_ERR_UNSUPPORTED;
+    pl->workspace_bytes = (size_t)lay.n_slots * (size_t)prompt_record_floats(shape->head_dim) * sizeof(float);
+    pl->off_block_begin = align_up(lay.units.size() * sizeof(PromptUnit), 32);
+    pl->off_merges = pl->off_block_begin + align_up(lay.block_begin.size() * sizeof(int32_t), 32);
+    pl->off_status = pl->off_merges + align_up(lay.merges.size() * sizeof(int32_t), 32);
+    const size_t total = pl->off_status + 32;
+    PlanBuffers* pb = new (std::nothrow) PlanBuffers();
+    if (!pb) return DA_ERR_INVALID_ARG;
+    pl->buffers = pb;
+    rc = acquire_buffers(pl->device, total, total, pb);
+    if (rc != DA_OK) return rc;
+    pl->dev = pb->dev;
+    pl->upload_done = pb->event;
+    pl->launch_done = pb->launched;
+    // (buffers of a destroyed plan: see decode_attn_plan)
+    DA_CUDA_TRY(cudaEventSynchronize(pl->upload_done));
+    DA_CUDA_TRY(cudaStreamWaitEvent(pb->stream, pl->launch_done, 0));
+    std::memset(pb->pinned, 0, total);
+    if (!lay.units.empty()) std::memcpy(pb->pinned, lay.units.data(), lay.units.size() * sizeof(PromptUnit));
+    std::memcpy(pb->pinned + pl->off_block_begin, lay.block_begin.data(), lay.block_begin.size() * sizeof(int32_t));
+    if (!lay.merges.empty()) std::memcpy(pb->pinned + pl->off_merges, lay.merges.data(), lay.merges.size() * sizeof(int32_t));
+    DA_CUDA_TRY(cudaMemcpyAsync(pl->dev, pb->pinned, total, cudaMemcpyHostToDevice, pb->stream));
+    DA_CUDA_TRY(cudaEventRecord(pl->upload_done, pb->stream));
+    pl->upload_pending = true;
+    if (workspace_bytes_out) *workspace_bytes_out = pl->workspace_bytes;
+    *plan_out = pl;
+    guard.p = nullptr;
+    return DA_OK;
+}
+
+int decode_attn_prompt_plan_destroy(decode_attn_prompt_plan_t* pl)
+{
+    if (!pl) return DA_OK;
+    if (pl->buffers) {
+        PlanBuffers* pb = static_cast<PlanBuffers*>(pl->buffers);
+        release_buffers(*pb);
+        delete pb;
+    }
+    delete pl;
+    return DA_OK;
+}
+
+int decode_attn_prompt_run(const decode_attn_prompt_plan_t* pl, const void* q, const void* k_cache, const void* v_cache,
+                           const int32_t* block_table, const int32_t* seq_lens, void* out, float* lse_or_null,
+                           void* workspace, size_t workspace_bytes, cudaStream_t stream)
+{
+    if (!pl) return DA_ERR_INVALID_ARG;
+    if (pl->layout.units.empty()) return DA_OK;
+    if (!q || !k_cache || !v_cache || !block_table || !seq_lens || !out) return DA_ERR_INVALID_ARG;
+    if (!aligned(q, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(out, 16) || !aligned(block_table, 4) ||
+        !aligned(seq_lens, 4) || !aligned(lse_or_null, 4))
+        return DA_ERR_INVALID_ARG;
+    if (pl->workspace_bytes > 0) {
+        if (!workspace || !aligned(workspace, 256)) return DA_ERR_INVALID_ARG;
+        if (workspace_bytes < pl->workspace_bytes) return DA_ERR_WORKSPACE_TOO_SMALL;
+    }
+    int rc = order_behind_upload(pl, stream);
+    if (rc != DA_OK) return rc;
+    PromptCall c;
+    c.q = q;
+    c.k_cache = k_cache;
+    c.v_cache = v_cache;
+    c.block_table = block_table;
+    c.seq_lens = seq_lens;
+    c.out = out;
+    c.lse = lse_or_null;
+    c.ws = static_cast<float*>(workspace);
+    c.units = reinterpret_cast<const PromptUnit*>(pl->dev);
+    c.block_begin = reinterpret_cast<const int32_t*>(pl->dev + pl->off_block_begin);
+    c.merges = reinterpret_cast<const int32_t*>(pl->dev + pl->off_merges);
+    c.status = reinterpret_cast<int32_t*>(pl->dev + pl->off_status);
+    c.n_blocks = (unsigned)(pl->layout.block_begin.size() - 1);
+    c.n_merges = (unsigned)pl->layout.merges.size();
+    // a window no sequence outgrows hides nothing
+    c.window = pl->policy.window_tokens < pl->layout.longest ? pl->policy.window_tokens : 0;
+    c.sinks = c.window > 0 ? pl->policy.sink_tokens : 0;
+    c.scale = pl->scale;
+    rc = prompt_launch(pl->shape, c, stream);
+    if (rc != DA_OK) return rc;
+    mark_launched(pl, stream);
+    return DA_OK;
+}
+
+int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t* pl, cudaStream_t stream)
+{
+    if (!pl) return DA_ERR_INVALID_ARG;
+    int32_t st = 0;
+    DA_CUDA_TRY(cudaEventSynchronize(pl->upload_done));
+    pl->upload_pending = false;
+    DA_CUDA_TRY(cudaStreamSynchronize(stream));
+    DA_CUDA_TRY(cudaMemcpy(&st, pl->dev + pl->off_status, sizeof st, cudaMemcpyDeviceToHost));
+    if (st != 0) DA_CUDA_TRY(cudaMemset(pl->dev + pl->off_status, 0, sizeof(int32_t)));
+    return st;
 }
 
 int decode_attn_merge_shards(const decode_attn_shape_t* shape, int32_t n_shards, const float* out_shards,
