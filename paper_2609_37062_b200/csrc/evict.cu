@@ -99,15 +99,17 @@ extern "C" int decode_attn_evict(const decode_attn_shape_t* shape, const decode_
     const int64_t units = rows * ((ep.budget + kMoveTokens - 1) / kMoveTokens);
     const int64_t move_blocks = (units + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
     if (rows > 0x7fffffffLL || move_blocks > 0x7fffffffLL) return DA_ERR_UNSUPPORTED;
-    const bool small = most <= 2048;
-    const void* select = small ? (const void*)decode_attn_evict_select_kernel<256> : (const void*)decode_attn_evict_select_kernel<1024>;
+    // up to 2,048 totals small blocks, several to an SM; up to 32,768 a large one whose threads still hold all keys
+    const int threads = most <= 2048 ? 256 : 1024;
+    const void* select = most <= 2048 ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8>
+                                      : (const void*)decode_attn_evict_select_kernel<1024, 2048, 32>;
     const void* move = s.head_dim == 128 ? (const void*)decode_attn_evict_move_kernel<128> : (const void*)decode_attn_evict_move_kernel<64>;
     if (smem > 32 * 1024 &&
         cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictChunk * (int)sizeof(float)) != cudaSuccess) {
         (void)cudaGetLastError();
         return DA_ERR_CUDA;
     }
-    rc = launch(select, dim3((unsigned)rows), small ? 256 : 1024, smem, ep, stream);
+    rc = launch(select, dim3((unsigned)rows), threads, smem, ep, stream);
     if (rc != DA_OK) return rc;
     return launch(move, dim3((unsigned)move_blocks), kMoveThreads, 0, ep, stream);
 }

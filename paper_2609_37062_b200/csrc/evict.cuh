@@ -6,12 +6,13 @@
 // the lowest position stays.  What stays keeps its order and moves to fresh
 // pages.  Two launches:
 //
-//   select  one block per (sequence, KV head).  The totals become 32-bit keys whose unsigned order is the
-//           order of the floats, and the key of rank k is found by three counting passes over 11, 11 and 10 bits
-//           (the later ones only over what shares the leading bits).  Then one ordered pass: every warp takes
-//           a run of neighbouring positions, counts what it keeps, and with the sums of the warps before it
-//           writes positions and totals to their places.  The totals sit in shared memory meanwhile (longer
-//           rows are walked in chunks), so they can be compacted in place.
+//   select  one block per (sequence, KV head).  The totals become 32-bit keys whose unsigned order is the order
+//           of the floats, and the key of rank k is found by counting them into bins between the least and the
+//           greatest, then looking into the bin that holds rank k the same way.  Then one ordered pass: every warp
+//           takes a run of neighbouring positions, counts what it keeps, and with the sums of the warps before it
+//           writes positions and totals to their places.  The totals sit in shared memory meanwhile (the longest
+//           rows are walked in runs), so they can be compacted in place.  (A cluster of eight blocks per row
+//           loses: the exchange of a counting step through distributed shared memory takes 1,300 cycles.)
 //   move    K and V rows of the kept positions, 16 bytes a lane, 32 tokens of one KV head per warp.
 //
 // Select reads 4 bytes per token and KV head, move reads and writes 4 D of them for every kept one: the
@@ -22,7 +23,6 @@
 
 namespace da {
 
-constexpr int kEvictDigits = 2048;                 // bins of a counting pass
 constexpr int kEvictChunk = 48 * 1024;             // totals a block holds in shared memory
 constexpr int kMoveThreads = 256;
 constexpr int kMoveTokens = 32;                    // of one (sequence, KV head) per warp
@@ -48,12 +48,15 @@ struct EvictParams {
     int32_t chunk;              // totals the launch's shared memory holds
 };
 
+// What stays whatever its total, and what is not there: above and below the key of every float.
+constexpr uint32_t kKeyStays = 0xffffffffu, kKeyNone = 0u;
+
 // Unsigned integers in the order of the floats; -0 equals +0, NaN counts as -inf.
 __device__ __forceinline__ uint32_t weight_key(float f)
 {
     if (f != f) f = -INFINITY;
     const uint32_t u = __float_as_uint(f + 0.f);
-    return (u >> 31) ? ~u : (u | 0x80000000u);
+    return u ^ ((uint32_t)((int32_t)u >> 31) | 0x80000000u);
 }
 
 // A row's length as both launches read it: -1 if it does not fit the tables or the totals (nothing is touched).
@@ -64,45 +67,22 @@ __device__ __forceinline__ int evict_length(const EvictParams& p, int b)
     return L;
 }
 
-// Sum over the threads before this one, and over all of them.
-template <int NT>
-__device__ __forceinline__ int block_scan(int x, int* sm /* [NT / 32] */, int& total)
-{
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    int inc = x;
-#pragma unroll
-    for (int off = 1; off < 32; off <<= 1) {
-        const int y = __shfl_up_sync(0xffffffffu, inc, off);
-        if (lane >= off) inc += y;
-    }
-    if (lane == 31) sm[warp] = inc;
-    __syncthreads();
-    int before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < NT / 32; ++w) {
-        const int s = sm[w];
-        if (w < warp) before += s;
-        total += s;
-    }
-    __syncthreads();
-    return before + inc - x;
-}
-
-template <int NT>
+// One block of NT threads per (sequence, KV head).  BINS: of a counting pass.  HELD: totals a thread keeps the
+// keys of in registers, where the row has no more.
+template <int NT, int BINS, int HELD>
 __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const EvictParams p)
 {
+    constexpr int WARPS = NT / 32, PER = BINS / NT;
     extern __shared__ float sm_w[];                           // [chunk] totals
-    __shared__ int sm_hist[kEvictDigits];
-    __shared__ int sm_scan[NT / 32], sm_gt[NT / 32], sm_eq[NT / 32];
-    __shared__ int sm_found[2];
-    constexpr int WARPS = NT / 32;
+    __shared__ int sm_hist[BINS];
+    __shared__ int2 sm_warp[WARPS];
+    __shared__ int sm_found[3];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int b = blockIdx.x / p.num_kv_heads, g = blockIdx.x % p.num_kv_heads;
     pdl_launch_dependents();
     pdl_wait_primary();
     const int L = evict_length(p, b);
-    int32_t* const kept = p.kept + ((int64_t)b * p.num_kv_heads + g) * p.budget;
+    int32_t* const kept = p.kept + (int64_t)blockIdx.x * p.budget;
     const int n = min(max(L, 0), p.budget);
     if (g == 0 && tid == 0) p.seq_lens_out[b] = L < 0 ? __ldg(p.seq_lens + b) : n;
     for (int i = n + tid; i < p.budget; i += NT) kept[i] = -1;
@@ -121,128 +101,199 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
         return;
     }
     const int last = L - p.recent;                            // [sinks, last) compete
+    // The row is walked in runs of up to p.chunk totals; a row of a single run (all but the longest) stays in shared
+    // memory from the first look to the last.  A warp looks after `seg` neighbouring totals of a run, a lane after
+    // every 32nd of them.
     const bool whole = L <= p.chunk;
-    if (whole) {
-#pragma unroll 8
-        for (int t = tid; t < L; t += NT) sm_w[t] = w[t];
+    const int run = min(L, p.chunk);
+    const int seg = (run + 32 * WARPS - 1) / (32 * WARPS) * 32;
+    const bool held = whole && seg <= 32 * HELD;
+    // the key of total f at position t, 0 <= t < L
+    auto key_of = [&](int t, float f) { return t < p.sinks || t >= last ? kKeyStays : weight_key(f); };
+    auto load = [&](int r0) {                                 // the totals of the run at r0
+        const int m = min(run, L - r0);
+        for (int i0 = tid; i0 < m; i0 += 16 * NT) {
+            float x[16];                                      // (in flight together: a store would hold up the load behind it)
+#pragma unroll
+            for (int u = 0; u < 16; ++u) x[u] = i0 + u * NT < m ? __ldcg(w + r0 + i0 + u * NT) : 0.f;
+#pragma unroll
+            for (int u = 0; u < 16; ++u)
+                if (i0 + u * NT < m) sm_w[i0 + u * NT] = x[u];
+        }
+    };
+    uint32_t keys[HELD];
+    if (held) {
+        const int i0 = warp * seg + lane;
+        float x[HELD];
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) x[u] = 32 * u < seg && i0 + 32 * u < L ? __ldcg(w + i0 + 32 * u) : 0.f;
+#pragma unroll
+        for (int u = 0; u < HELD; ++u) {
+            const bool in = 32 * u < seg && i0 + 32 * u < L;
+            if (in) sm_w[i0 + 32 * u] = x[u];                 // (read again by this thread alone)
+            keys[u] = in ? key_of(i0 + 32 * u, x[u]) : kKeyNone;
+        }
+    } else if (whole) {
+        load(0);
+        __syncthreads();
     }
-    __syncthreads();
-    auto total_of = [&](int t) { return whole ? sm_w[t] : w[t]; };
+    auto each_key = [&](auto&& f) {                           // whole warps call f
+        if (held) {
+#pragma unroll
+            for (int u = 0; u < HELD; ++u)
+                if (32 * u < seg) f(keys[u]);
+        } else {
+            for (int r0 = 0; r0 < L; r0 += run)
+#pragma unroll 4
+                for (int i0 = 32 * warp; i0 < run; i0 += NT) {
+                    const int i = i0 + lane, t = r0 + i;
+                    f(i < run && t < L ? key_of(t, whole ? sm_w[i] : __ldcg(w + t)) : kKeyNone);
+                }
+        }
+    };
 
-    // ---- the key of rank k among the competitors, and how many of its equals stay
+    // ---- the key of rank k among the competitors, and how many of its equals stay.  The keys between the least
+    // and the greatest are counted in BINS bins of equal width; the bin with rank k is looked into the same way until it is
+    // one key wide or all of it stays.  (Keys are the floats' bits, so totals that spread over powers of two spread
+    // over the bins; three passes at most, as a rule.)
     int k = p.budget - p.sinks - p.recent;
-    uint32_t key = 0xffffffffu;                               // k = 0: above every key
+    uint32_t key = kKeyStays - 1;                             // k = 0: above every float's
     int ties = 0;
     if (k > 0) {
-        key = 0;
-#pragma unroll 1
-        for (int pass = 0; pass < 3; ++pass) {
-            const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-            const uint32_t digits = pass == 2 ? 1023u : 2047u;
-            const uint32_t above = pass == 0 ? 0u : (pass == 1 ? ~((1u << 21) - 1) : ~((1u << 10) - 1));
-            for (int i = tid; i < kEvictDigits; i += NT) sm_hist[i] = 0;
-            __syncthreads();
-            for (int t0 = p.sinks + warp * 32; t0 < last; t0 += NT) {
-                const int t = t0 + lane;
-                bool in = t < last;
-                uint32_t x = 0;
-                if (in) x = weight_key(total_of(t));
-                in = in && (x & above) == key;
-                const uint32_t d = (x >> shift) & digits;
-                const uint32_t m = __ballot_sync(0xffffffffu, in);
-                if (m == 0) continue;
-                // Totals of one warp often share their leading bits (all of them zero, at worst): the first
-                // lane's digit is counted once for all lanes that have it, the rest one by one.
-                const uint32_t d0 = __shfl_sync(0xffffffffu, d, __ffs(m) - 1);
-                const uint32_t same = __ballot_sync(0xffffffffu, in && d == d0);
-                if (in && d != d0) atomicAdd(sm_hist + d, 1);
-                if (lane == 0) atomicAdd(sm_hist + d0, __popc(same));
+        uint32_t least = 0xffffffffu, most = 0u;
+        each_key([&](uint32_t x) {
+            if (x != kKeyNone) least = min(least, x);
+            if (x != kKeyStays) most = max(most, x);
+        });
+        least = __reduce_min_sync(0xffffffffu, least);
+        most = __reduce_max_sync(0xffffffffu, most);
+        if (lane == 0) sm_warp[warp] = make_int2((int)least, (int)most);
+        __syncthreads();
+        if (lane < WARPS) {
+            least = (uint32_t)sm_warp[lane].x;
+            most = (uint32_t)sm_warp[lane].y;
+        }
+        uint32_t lo = __reduce_min_sync(0xffffffffu, least), hi = __reduce_max_sync(0xffffffffu, most) + 1;
+        while (true) {
+            if (hi - lo == 1) {
+                key = lo;
+                ties = k;
+                break;
             }
+            const int bits = 32 - __clz((int)(hi - lo - 1));
+            constexpr int LOG_BINS = BINS == 2048 ? 11 : 10;
+            static_assert(1 << LOG_BINS == BINS, "bins");
+            const int shift = max(0, bits - LOG_BINS);
+            for (int i = tid; i < BINS; i += NT) sm_hist[i] = 0;
             __syncthreads();
-            // bins from the top: the one in which the count reaches k
-            constexpr int PER = kEvictDigits / NT;
-            int c[PER], sum = 0;
+            each_key([&](uint32_t x) {
+                // Where totals are equal (all of them zero, at worst) the lanes meet in one bin: the first lane's is
+                // counted once for all that share it, the rest one by one.
+                const bool in = x - lo < hi - lo;
+                const uint32_t d = in ? (x - lo) >> shift : (uint32_t)BINS;
+                const uint32_t d0 = __shfl_sync(0xffffffffu, d, 0);
+                const uint32_t same = __ballot_sync(0xffffffffu, d == d0);
+                if (in && d != d0) atomicAdd(sm_hist + d, 1);
+                if (in && lane == 0) atomicAdd(sm_hist + d, __popc(same));
+            });
+            __syncthreads();
+            int c[PER], sum = 0;                              // bins from the top
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                c[i] = sm_hist[kEvictDigits - 1 - (tid * PER + i)];
+                c[i] = sm_hist[BINS - 1 - (tid * PER + i)];
                 sum += c[i];
             }
-            int all;
-            int before = block_scan<NT>(sum, sm_scan, all);
+            int inc = sum;
+#pragma unroll
+            for (int off = 1; off < 32; off <<= 1) {
+                const int y = __shfl_up_sync(0xffffffffu, inc, off);
+                if (lane >= off) inc += y;
+            }
+            if (lane == 31) sm_warp[warp].x = inc;
+            __syncthreads();
+            int before = __reduce_add_sync(0xffffffffu, lane < warp ? sm_warp[lane].x : 0) + inc - sum;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                if (before < k && before + c[i] >= k) {
-                    sm_found[0] = kEvictDigits - 1 - (tid * PER + i);
+                if (before < k && before + c[i] >= k) {       // one thread, one bin
+                    sm_found[0] = BINS - 1 - (tid * PER + i);
                     sm_found[1] = before;
+                    sm_found[2] = c[i];
                 }
                 before += c[i];
             }
             __syncthreads();
-            key |= (uint32_t)sm_found[0] << shift;
+            lo += (uint32_t)sm_found[0] << shift;
             k -= sm_found[1];
-            __syncthreads();
+            if (k == sm_found[2]) {                           // all of the bin stays
+                key = lo - 1;
+                break;
+            }
+            hi = min(hi, lo + (1u << shift));
         }
-        ties = k;
     }
 
     // ---- positions and totals of what stays, in order
-    int at = 0, equal = 0;                                    // kept, equals met: in the chunks before
-    for (int c0 = 0; c0 < L; c0 += p.chunk) {
-        const int cn = min(p.chunk, L - c0);
+    int at = 0, equal = 0;                                    // kept, equals met: in the runs before
+    for (int r0 = 0; r0 < L; r0 += run) {
+        __syncthreads();                                      // sm_warp, sm_w are free
         if (!whole) {
-            __syncthreads();
-            for (int t = tid; t < cn; t += NT) sm_w[t] = w[c0 + t];
+            load(r0);
             __syncthreads();
         }
-        const int seg = (cn + 32 * WARPS - 1) / (32 * WARPS) * 32;
-        const int s0 = warp * seg, s1 = min(s0 + seg, cn);
-        auto look = [&](int i, bool& gt, bool& eq) {
-            const int t = c0 + i;
-            const uint32_t x = i < s1 ? weight_key(sm_w[i]) : 0u;
-            const bool sure = t < p.sinks || t >= last;
-            gt = i < s1 && (sure || x > key);
-            eq = i < s1 && !sure && x == key;
-        };
+        const int m = min(run, L - r0);
+        const int s0 = warp * seg, s1 = min(s0 + seg, m);
+        auto run_key = [&](int i) { return i < s1 ? key_of(r0 + i, sm_w[i]) : kKeyNone; };
         int n_gt = 0, n_eq = 0;
-        for (int i0 = s0; i0 < s1; i0 += 32) {
-            bool gt, eq;
-            look(i0 + lane, gt, eq);
-            n_gt += __popc(__ballot_sync(0xffffffffu, gt));
-            n_eq += __popc(__ballot_sync(0xffffffffu, eq));
-        }
-        if (lane == 0) {
-            sm_gt[warp] = n_gt;
-            sm_eq[warp] = n_eq;
-        }
-        __syncthreads();
-        int my_at = at, my_eq = equal;
+        if (held) {
 #pragma unroll
-        for (int x = 0; x < WARPS; ++x) {
-            const int e = sm_eq[x];
-            const int add = sm_gt[x] + min(max(ties - equal, 0), e);
-            if (x < warp) {
-                my_at += add;
-                my_eq += e;
+            for (int u = 0; u < HELD; ++u)
+                if (32 * u < seg) {
+                    n_gt += keys[u] > key;
+                    n_eq += keys[u] == key;
+                }
+        } else {
+#pragma unroll 4
+            for (int i0 = s0; i0 < s0 + seg; i0 += 32) {
+                const uint32_t x = run_key(i0 + lane);
+                n_gt += x > key;
+                n_eq += x == key;
             }
-            at += add;
-            equal += e;
         }
+        n_gt = __reduce_add_sync(0xffffffffu, n_gt);
+        n_eq = __reduce_add_sync(0xffffffffu, n_eq);
+        if (lane == 0) sm_warp[warp] = make_int2(n_gt, n_eq);
+        __syncthreads();                                      // (in place: the whole run has been read)
+        const int2 said = lane < WARPS ? sm_warp[lane] : make_int2(0, 0);
+        const int run_gt = __reduce_add_sync(0xffffffffu, said.x), run_eq = __reduce_add_sync(0xffffffffu, said.y);
+        int my_eq = equal + __reduce_add_sync(0xffffffffu, lane < warp ? said.y : 0);
+        // kept so far: all above the key, and the first `ties` equals
+        int to0 = at + __reduce_add_sync(0xffffffffu, lane < warp ? said.x : 0) + min(my_eq, ties) - min(equal, ties);
         const uint32_t lower = (1u << lane) - 1;
-        for (int i0 = s0; i0 < s1; i0 += 32) {
-            bool gt, eq;
-            look(i0 + lane, gt, eq);
-            const uint32_t me = __ballot_sync(0xffffffffu, eq);
-            const bool stay = gt || (eq && my_eq + __popc(me & lower) < ties);
-            const uint32_t ms = __ballot_sync(0xffffffffu, stay);
-            if (stay) {
-                const int to = my_at + __popc(ms & lower);
-                kept[to] = c0 + i0 + lane;
-                o[to] = sm_w[i0 + lane];
+        auto place = [&](int i, uint32_t x) {
+            bool stay = x > key;
+            if (ties > 0) {
+                const bool eq = x == key;
+                const uint32_t mask_eq = __ballot_sync(0xffffffffu, eq);
+                stay = stay || (eq && my_eq + __popc(mask_eq & lower) < ties);
+                my_eq += __popc(mask_eq);
             }
-            my_at += __popc(ms);
-            my_eq += __popc(me);
+            const uint32_t mask = __ballot_sync(0xffffffffu, stay);
+            if (stay) {
+                const int to = to0 + __popc(mask & lower);
+                kept[to] = r0 + i;
+                o[to] = sm_w[i];
+            }
+            to0 += __popc(mask);
+        };
+        if (held) {
+#pragma unroll
+            for (int u = 0; u < HELD; ++u)
+                if (32 * u < seg) place(s0 + 32 * u + lane, keys[u]);
+        } else {
+            for (int i0 = s0; i0 < s0 + seg; i0 += 32) place(i0 + lane, run_key(i0 + lane));
         }
-        __syncthreads();                                      // the chunk, and the warps' counts, may be replaced
+        at += run_gt + min(equal + run_eq, ties) - min(equal, ties);
+        equal += run_eq;
     }
     for (int t = p.budget + tid; t < L; t += NT) o[t] = 0.f;      // tokens to come start from nothing
 }

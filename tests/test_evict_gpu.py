@@ -108,8 +108,10 @@ def test_pages_heads_and_layouts(layout, page_size, hq, hkv, d, dtype):
 
 
 def test_rows_longer_than_a_block_holds():
-    """Above 49,152 totals a row is walked in chunks; compaction in place is the delicate case."""
-    for lens, budget in (([49152], 5000), ([49153, 120_000], 100_001), ([100_000], 60_000)):
+    """Longer rows are shared by a cluster of blocks, the longest walked in runs; compaction in place is the
+    delicate case."""
+    for lens, budget in (([9000, 4097, 300], 4000), ([49152], 5000), ([49153, 120_000], 100_001), ([100_000], 60_000),
+                         ([400_001, 9], 300_000)):
         w = workload(lens, budget, 2, 1, 64, seed=52, page_size=256)
         for kind in ("random", "steps", "equal"):
             t = totals(kind, (len(lens), 1, max(lens)), 9)
