@@ -955,6 +955,7 @@ int decode_attn_prompt_run(const decode_attn_prompt_plan_t* pl, const void* q, c
     c.status = reinterpret_cast<int32_t*>(pl->dev + pl->off_status);
     c.n_blocks = (unsigned)(pl->layout.block_begin.size() - 1);
     c.n_merges = (unsigned)pl->layout.merges.size();
+    c.q_rows = pl->layout.q_rows;
     // a window no sequence outgrows hides nothing
     c.window = pl->policy.window_tokens < pl->layout.longest ? pl->policy.window_tokens : 0;
     c.sinks = c.window > 0 ? pl->policy.sink_tokens : 0;

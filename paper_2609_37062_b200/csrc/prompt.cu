@@ -25,12 +25,26 @@ int launch(const void* fn, unsigned grid, int threads, size_t smem, void** args,
     return DA_OK;
 }
 
+// 3-D map of q: [head_dim, query head, token]; a box is 64 dims of one group's heads of an MMA tile's tokens.
+int make_q_map(CUtensorMap* map, const void* q, const decode_attn_shape_t& s, int64_t rows, int group, int tokens)
+{
+    const CUtensorMapDataType dt = s.q_dtype == DA_DTYPE_FP16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+    encode_tiled_fn enc = get_encode_tiled();
+    if (!enc) return DA_ERR_CUDA;
+    const cuuint64_t dims[3] = {(cuuint64_t)s.head_dim, (cuuint64_t)s.num_q_heads, (cuuint64_t)rows};
+    const cuuint64_t strides[2] = {(cuuint64_t)s.head_dim * 2, (cuuint64_t)s.num_q_heads * s.head_dim * 2};
+    const cuuint32_t box[3] = {64, (cuuint32_t)group, (cuuint32_t)tokens};
+    const cuuint32_t estr[3] = {1, 1, 1};
+    const CUresult r = enc(map, dt, 3, const_cast<void*>(q), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                           CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    return r == CUDA_SUCCESS ? DA_OK : DA_ERR_CUDA;
+}
+
 }  // namespace
 
 int prompt_launch(const decode_attn_shape_t& s, const PromptCall& c, cudaStream_t stream)
 {
     PromptParams p;
-    p.q = static_cast<const __nv_bfloat16*>(c.q);
     p.v = static_cast<const __nv_bfloat16*>(c.v_cache);
     p.block_table = c.block_table;
     p.seq_lens = c.seq_lens;
@@ -54,8 +68,10 @@ int prompt_launch(const decode_attn_shape_t& s, const PromptCall& c, cudaStream_
     while ((16 << p.tile_shift) < s.page_size) ++p.tile_shift;
     p.out_kind = s.out_dtype == DA_DTYPE_BF16 ? 1 : s.out_dtype == DA_DTYPE_FP16 ? 2 : 0;
     p.scale_log2 = c.scale * kLog2e;
-    CUtensorMap kmap, vmap;
-    int rc = make_pool_map(&kmap, c.k_cache, s, s.k_stride_page, s.k_stride_token, s.k_stride_head);
+    CUtensorMap qmap, kmap, vmap;
+    int rc = make_q_map(&qmap, c.q, s, c.q_rows, p.group, p.tokens_per_tile);
+    if (rc != DA_OK) return rc;
+    rc = make_pool_map(&kmap, c.k_cache, s, s.k_stride_page, s.k_stride_token, s.k_stride_head);
     if (rc != DA_OK) return rc;
     rc = make_pool_map(&vmap, c.v_cache, s, s.v_stride_page, s.v_stride_token, s.v_stride_head);
     if (rc != DA_OK) return rc;
@@ -67,7 +83,7 @@ int prompt_launch(const decode_attn_shape_t& s, const PromptCall& c, cudaStream_
         (void)cudaGetLastError();
         return DA_ERR_CUDA;
     }
-    void* args[] = {&p, &kmap, &vmap};
+    void* args[] = {&p, &qmap, &kmap, &vmap};
     rc = launch(fn, c.n_blocks, kPromptThreads, (size_t)smem, args, stream);
     if (rc != DA_OK || c.n_merges == 0) return rc;
     const void* merge = s.head_dim == 128 ? (const void*)decode_attn_prompt_merge_kernel<128> : (const void*)decode_attn_prompt_merge_kernel<64>;

@@ -38,7 +38,6 @@
 namespace da {
 
 struct PromptParams {
-    const __nv_bfloat16* q;          // [rows][Hq][D]
     const __nv_bfloat16* v;
     const int32_t* block_table;
     const int32_t* seq_lens;
@@ -61,7 +60,12 @@ struct PromptParams {
 
 constexpr int kPromptSoftmaxWarps = 8;
 constexpr int kPromptMmaWarp = 8, kPromptLoadWarp = 9;
-constexpr int kPromptThreads = 320;
+constexpr int kPromptThreads = 384;       // three warpgroups: two of softmax, the third with the MMA and the load warp
+// Registers: 384 x 168 at launch; the softmax warpgroups take what the third gives back, 256 x 224 + 128 x 56 in all.
+constexpr int kPromptSoftmaxRegs = 224, kPromptOtherRegs = 56;
+static_assert(256 * kPromptSoftmaxRegs + 128 * kPromptOtherRegs <= 384 * 168, "more registers than the block was launched with");
+
+constexpr int kPromptStageBytes = kPromptSoftmaxWarps * 32 * 128;   // outputs on their way out: 128 bytes of a row per thread
 
 template <int D>
 struct PromptCfg {
@@ -69,11 +73,58 @@ struct PromptCfg {
     static constexpr int kHalfBytes = 128 * 128;                 // 128 rows x 64 dims
     static constexpr int kTileBytes = kHalves * kHalfBytes;      // Q tile, K tile, V tile
     static constexpr int kStages = D == 128 ? 2 : 4;             // of K, and of V
-    static constexpr int kBarriers = 10 + 4 * kStages + 1;
-    static constexpr int kSmemBytes = (2 + 2 * kStages) * kTileBytes + 512 + 1024 /* alignment */;
+    static constexpr int kBarriers = 14 + 4 * kStages + 1;
+    static constexpr int kSmemBytes = (2 + 2 * kStages) * kTileBytes + kPromptStageBytes + 512 + 1024 /* alignment */;
     static_assert(kSmemBytes > 114 * 1024 && kSmemBytes <= 227 * 1024, "one block per SM: each takes all of tensor memory");
 };
 constexpr float kPromptRescale = 8.f;                            // log2: how far a row's maximum may run ahead of its scale
+
+// One lane of a converged warp, always the same one.  The MMAs are issued under this predicate, at the place: the
+// compiler knows it for what it is and keeps descriptors in uniform registers.  (Under lane == 0 every operand of every MMA
+// is moved there first, which paced the issue: 85 to 95 cycles an MMA instead of 64.)
+__device__ __forceinline__ bool elect_one()
+{
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
+}
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int c0, int c1, int c2)
+{
+    asm volatile("cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+                 : "memory");
+}
+
+// Bits 0 .. n - 1, for any n.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : n >= 32 ? 0xffffffffu : (1u << n) - 1u; }
+
+// Two fp32 values in a register pair: one instruction works on both.
+__device__ __forceinline__ uint64_t pack2(float lo, float hi)
+{
+    uint64_t v;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(v) : "f"(lo), "f"(hi));
+    return v;
+}
+__device__ __forceinline__ void unpack2(uint64_t v, float& lo, float& hi) { asm("mov.b64 {%0, %1}, %2;" : "=f"(lo), "=f"(hi) : "l"(v)); }
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
+{
+    uint64_t v;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(v) : "l"(a), "l"(b), "l"(c));
+    return v;
+}
+__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
+{
+    uint64_t v;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(v) : "l"(a), "l"(b));
+    return v;
+}
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float v;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(v) : "f"(a), "f"(b), "f"(c));
+    return v;
+}
 
 // Whole warp.
 __device__ __forceinline__ bool prompt_wait(uint32_t bar, uint32_t parity, volatile int* abort_flag)
@@ -83,7 +134,8 @@ __device__ __forceinline__ bool prompt_wait(uint32_t bar, uint32_t parity, volat
 
 template <int D, bool F16>
 __global__ void __launch_bounds__(kPromptThreads, 1)
-decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map)
+decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
+                          const __grid_constant__ CUtensorMap v_map)
 {
     using Cfg = PromptCfg<D>;
     constexpr int NS = Cfg::kStages;
@@ -92,15 +144,17 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
     const uint32_t base = (raw + 1023u) & ~1023u;
     uint8_t* const gbase = smem_raw + (base - raw);
     const uint32_t q_base = base, k_base = base + 2 * Cfg::kTileBytes, v_base = k_base + NS * Cfg::kTileBytes;
-    const uint32_t bar_base = v_base + NS * Cfg::kTileBytes;
-    // per MMA tile x: q (its rows are in shared memory), s (logits complete), p (weights written), o (P V complete),
-    // of (output read); per stage: K and V landed (kf, vf), K and V no longer read (ke, ve); drain
+    const uint32_t stage_base = v_base + NS * Cfg::kTileBytes;
+    const uint32_t bar_base = stage_base + kPromptStageBytes;
+    // per MMA tile x: q (its rows have landed), qe (no longer read), s (logits complete), p (a half of the weights written: of the
+    // first, of the last 64 tokens), o (P V complete), of (output read); per stage: K and V landed (kf, vf), K and V no longer read (ke, ve); drain
     auto bar_q = [&](int x) { return bar_base + 8 * x; };
     auto bar_s = [&](int x) { return bar_base + 16 + 8 * x; };
-    auto bar_p = [&](int x) { return bar_base + 32 + 8 * x; };
-    auto bar_o = [&](int x) { return bar_base + 48 + 8 * x; };
-    auto bar_of = [&](int x) { return bar_base + 64 + 8 * x; };
-    const uint32_t bar_kf = bar_base + 80, bar_ke = bar_kf + 8 * NS, bar_vf = bar_ke + 8 * NS, bar_ve = bar_vf + 8 * NS;
+    auto bar_p = [&](int x, int half) { return bar_base + 32 + 16 * x + 8 * half; };
+    auto bar_o = [&](int x) { return bar_base + 64 + 8 * x; };
+    auto bar_of = [&](int x) { return bar_base + 80 + 8 * x; };
+    auto bar_qe = [&](int x) { return bar_base + 96 + 8 * x; };
+    const uint32_t bar_kf = bar_base + 112, bar_ke = bar_kf + 8 * NS, bar_vf = bar_ke + 8 * NS, bar_ve = bar_vf + 8 * NS;
     const uint32_t bar_drain = bar_ve + 8 * NS;
     uint8_t* const misc = gbase + (bar_base - base);
     static_assert(8 * Cfg::kBarriers <= 256, "barriers");
@@ -114,12 +168,15 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
         return;
     }
     if (tid == 0) {
+        tma_prefetch_descriptor(&q_map);
         tma_prefetch_descriptor(&k_map);
         tma_prefetch_descriptor(&v_map);
         for (int x = 0; x < 2; ++x) {
-            mbar_init(bar_q(x), 4);
+            mbar_init(bar_q(x), 1);
+            mbar_init(bar_qe(x), 1);
             mbar_init(bar_s(x), 1);
-            mbar_init(bar_p(x), 4);
+            mbar_init(bar_p(x, 0), 4);
+            mbar_init(bar_p(x, 1), 4);
             mbar_init(bar_o(x), 1);
             mbar_init(bar_of(x), 4);
         }
@@ -135,19 +192,24 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
     const uint32_t tmem = *sm_tmem;
     pdl_wait_primary();
 
+    // (by role, inside the role's own code: the compiler allocates by what it sees there)
+    auto give_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPromptOtherRegs)); };
     const int G = p.group, TQ = p.tokens_per_tile;
     auto tile_at = [](const PromptUnit& u, int i) { return i < u.sink_tiles ? i : i - u.sink_tiles + u.window_tile; };
 
     if (warp == kPromptLoadWarp) {
         // ------------------------------------------------------------ TMA
+        give_registers();
         const uint64_t keep = l2_policy_evict_normal();
         const int ts = p.tile_shift;
         const int sub = (lane / Cfg::kHalves) & 7, hf = lane % Cfg::kHalves;    // lane's box: 16 tokens, half of the head dimension
         constexpr int BOXES = 8 * Cfg::kHalves;
         int n = 0;                                                              // K/V tiles so far
+        int cu[2] = {0, 0};                                                     // units so far, per MMA tile
         bool ok = true;
         for (int ui = ubeg; ui < uend && ok; ++ui) {
             const PromptUnit u = p.units[ui];
+            const int X = u.n_tok > TQ ? 2 : 1;
             const int lo = p.window > 0 ? max(0, u.pos - p.window + 1) : 0;     // what the first query sees through its window
             const int end = min(u.pos + u.n_tok, u.seq_len);
             const int32_t* const bt = p.block_table + (int64_t)u.seq * p.max_pages_per_seq;
@@ -177,6 +239,23 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 if (lane < BOXES)
                     tma_load_4d(k_base + st * Cfg::kTileBytes + hf * Cfg::kHalfBytes + sub * 2048, &k_map, bar_kf + 8 * st,
                                 hf * 64, slot0, u.kv_head, page, keep);
+                if (i == u.tile_begin) {
+                    // The unit's query rows: TQ tokens x the group's heads, rows of the MMA tile in that order.  (Tokens of
+                    // a ragged end are other rows of q, or zeros behind the last: what comes of them is not stored.)
+                    for (int x = 0; x < X && ok; ++x) {
+                        if (cu[x] > 0) ok = prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
+                        if (!ok) break;
+                        ++cu[x];
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(bar_q(x), Cfg::kHalves * G * TQ * 128);
+                            for (int h = 0; h < Cfg::kHalves; ++h)
+                                tma_load_3d(q_base + x * Cfg::kTileBytes + h * Cfg::kHalfBytes, &q_map, bar_q(x), h * 64, u.kv_head * G,
+                                            u.row + x * TQ);
+                        }
+                        __syncwarp();
+                    }
+                    if (!ok) break;
+                }
                 if (n >= NS) ok = prompt_wait(bar_ve + 8 * st, parity, sm_abort);
                 if (!ok) break;
                 const uint32_t parts = __ballot_sync(0xffffffffu, part && hf == 0 && lane < BOXES);
@@ -213,10 +292,13 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 mbar_wait(bar_vf + 8 * (i % NS), (uint32_t)(i / NS) & 1u);
             }
             if (!ok) mbar_wait(bar_kf + 8 * (n % NS), (uint32_t)(n / NS) & 1u, 1000000LL);   // the tile whose V was not issued
+            for (int x = 0; x < 2; ++x)
+                if (cu[x] > 0) mbar_wait(bar_q(x), (uint32_t)(cu[x] - 1) & 1u);
         }
     } else if (warp == kPromptMmaWarp) {
-        // ------------------------------------------------------------ MMAs (one lane)
-        if (lane == 0) {
+        // ------------------------------------------------------------ MMAs (the warp together, one lane issues)
+        give_registers();
+        {
             constexpr uint32_t idesc_qk = umma::instr_desc_16(128, 128, false, F16);
             constexpr uint32_t idesc_pv = umma::instr_desc_16(128, D, true, F16);
             constexpr uint32_t kTileUnits = Cfg::kTileBytes >> 4, kHalfUnits = Cfg::kHalfBytes >> 4;
@@ -234,36 +316,49 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                     const int st = (n + j) % NS;
                     umma::fence_after_thread_sync();
                     const uint64_t qd = q_desc + (uint64_t)(x * kTileUnits), kd = k_desc + (uint64_t)(st * kTileUnits);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int ks = 0; ks < D / 16; ++ks) {
-                        const uint32_t off = (ks >> 2) * kHalfUnits + (ks & 3) * 2;
-                        umma::mma_ss(tmem + x * 128, qd + off, kd + off, idesc_qk, ks > 0);
+                        for (int ks = 0; ks < D / 16; ++ks) {
+                            const uint32_t off = (ks >> 2) * kHalfUnits + (ks & 3) * 2;
+                            umma::mma_ss(tmem + x * 128, qd + off, kd + off, idesc_qk, ks > 0);
+                        }
+                        umma::commit(bar_s(x));
+                        if (x == X - 1) umma::commit(bar_ke + 8 * st);
+                        if (j == T - 1) umma::commit(bar_qe(x));
                     }
-                    umma::commit(bar_s(x));
-                    if (x == X - 1) umma::commit(bar_ke + 8 * st);
+                    __syncwarp();
                 };
-                auto pv = [&](int x, int j) {
+                auto pv = [&](int x, int j, int half) {
                     const int st = (n + j) % NS;
                     umma::fence_after_thread_sync();
-                    const uint64_t vd = v_desc + (uint64_t)(st * kTileUnits);
+                    const uint64_t vd = v_desc + (uint64_t)(st * kTileUnits + half * 512);
+                    const uint32_t pd = tmem + x * 128 + half * 32, od = tmem + 256 + x * 128;
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        umma::mma_ts(tmem + 256 + x * 128, tmem + x * 128 + k * 8, vd + k * 128, idesc_pv, j > 0 || k > 0);
-                    umma::commit(bar_o(x));
-                    if (x == X - 1) umma::commit(bar_ve + 8 * st);
+                        for (int k = 0; k < 4; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, j > 0 || half > 0 || k > 0);
+                        if (half == 1) {
+                            umma::commit(bar_o(x));
+                            if (x == X - 1) umma::commit(bar_ve + 8 * st);
+                        }
+                    }
+                    __syncwarp();
                 };
-                auto k_landed = [&](int j) { return umma_wait(bar_kf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort); };
+                auto k_landed = [&](int j) { return prompt_wait(bar_kf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort); };
                 for (int x = 0; x < X && ok; ++x) {
-                    ok = umma_wait(bar_q(x), (uint32_t)cu[x] & 1u, sm_abort) && k_landed(0);
+                    ok = prompt_wait(bar_q(x), (uint32_t)cu[x] & 1u, sm_abort) && k_landed(0);
                     if (ok) qk(x, 0);
                 }
                 for (int j = 0; j < T && ok; ++j) {
                     for (int x = 0; x < X && ok; ++x) {
-                        ok = umma_wait(bar_p(x), (uint32_t)cs[x] & 1u, sm_abort) &&
-                             umma_wait(bar_vf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort) &&
-                             (j > 0 || cu[x] == 0 || umma_wait(bar_of(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort));
+                        // (the weights last: every wait behind theirs would be time the tensor core stands still)
+                        ok = prompt_wait(bar_vf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort) &&
+                             (j > 0 || cu[x] == 0 || prompt_wait(bar_of(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort)) &&
+                             prompt_wait(bar_p(x, 0), (uint32_t)cs[x] & 1u, sm_abort);
                         if (!ok) break;
-                        pv(x, j);
+                        pv(x, j, 0);
+                        ok = prompt_wait(bar_p(x, 1), (uint32_t)cs[x] & 1u, sm_abort);
+                        if (!ok) break;
+                        pv(x, j, 1);
                         ++cs[x];
                         if (j + 1 < T) {
                             ok = k_landed(j + 1);
@@ -277,17 +372,20 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
             // nothing may arrive on a barrier, or be written, after the block has left
             if (ok)
                 for (int i = max(0, n - NS); i < n; ++i) {
-                    ok = ok && umma_wait(bar_ke + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
-                    ok = ok && umma_wait(bar_ve + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
+                    ok = ok && prompt_wait(bar_ke + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
+                    ok = ok && prompt_wait(bar_ve + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
                 }
+            for (int x = 0; x < 2; ++x)
+                if (cu[x] > 0) ok = ok && prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
             if (!ok) {
-                umma::commit(bar_drain);
+                if (elect_one()) umma::commit(bar_drain);
                 mbar_wait(bar_drain, 0);
             }
         }
         __syncwarp();
-    } else {
+    } else if (warp < kPromptSoftmaxWarps) {
         // ------------------------------------------------------------ softmax, output: one thread per row
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPromptSoftmaxRegs));
         const int x = warp >> 2, r = (warp & 3) * 32 + lane;
         const int tok = r / G, h = r - tok * G;
         const uint32_t lane_base = tmem + ((uint32_t)((warp & 3) * 32) << 16);
@@ -296,20 +394,6 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
         bool ok = true;
         auto in_unit = [&](const PromptUnit& u) { return x == 0 || u.n_tok > TQ; };
         auto row_valid = [&](const PromptUnit& u) { return tok < TQ && x * TQ + tok < u.n_tok; };
-        // this row of Q into the swizzled K-major tile
-        auto load_q = [&](const PromptUnit& u) {
-            const bool valid = row_valid(u);
-            const uint4* src = reinterpret_cast<const uint4*>(
-                p.q + ((int64_t)(u.row + (valid ? x * TQ + tok : 0)) * p.num_q_heads + u.kv_head * G + (valid ? h : 0)) * D);
-#pragma unroll
-            for (int c = 0; c < D / 8; ++c) {
-                const uint4 v = valid ? __ldg(src + c) : make_uint4(0u, 0u, 0u, 0u);
-                *reinterpret_cast<uint4*>(gbase + x * Cfg::kTileBytes + (c >> 3) * Cfg::kHalfBytes + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v;
-            }
-            asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar_q(x));
-        };
         int ui = ubeg;
         PromptUnit u = p.units[ui];
         if (!in_unit(u)) {
@@ -318,7 +402,6 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 if (in_unit(u)) break;
             }
         }
-        if (ui < uend) load_q(u);
         while (ui < uend && ok) {
             const bool valid = row_valid(u);
             const int q_lo = u.pos + x * TQ, q_hi = min(u.pos + u.n_tok, q_lo + TQ) - 1;     // this MMA tile's queries
@@ -336,14 +419,23 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 const bool masked = t0 + kPromptKvTokens - 1 > q_lo ||
                                     (p.window > 0 && t0 <= q_hi - p.window && t0 + kPromptKvTokens > p.sinks);
                 if (masked) {
-                    const int hi = qi - t0, lo = p.window > 0 ? qi - p.window + 1 - t0 : INT_MIN, sk = p.sinks - t0;
+                    // one bit per column, 32 at a time, then 32 selects on known bits (conditions column by column
+                    // become branches: 15,000 cycles a tile instead of a few hundred)
+                    const int hi = qi - t0 + 1, lo = p.window > 0 ? qi - p.window + 1 - t0 : 0, sk = p.sinks - t0;
 #pragma unroll
-                    for (int c = 0; c < 128; ++c)
-                        if (!(c <= hi && (c >= lo || c < sk))) s[c >> 6][c & 63] = 0xff800000u;      // -inf
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t vis = low_bits(hi - 32 * q) & (~low_bits(lo - 32 * q) | low_bits(sk - 32 * q));
+#pragma unroll
+                        for (int c = 0; c < 32; ++c) {
+                            uint32_t& x = s[q >> 1][(q & 1) * 32 + c];
+                            x = (vis & (1u << c)) != 0u ? x : 0xff800000u;                       // -inf
+                        }
+                    }
                 }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < 128; ++c) mx[c & 3] = fmaxf(mx[c & 3], __uint_as_float(s[c >> 6][c & 63]));
+                for (int c = 0; c < 128; c += 2)
+                    mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(s[c >> 6][c & 63]), __uint_as_float(s[c >> 6][(c & 63) + 1]));
                 const float m_new = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;   // the scale is positive
                 const bool grow = m_new > m + kPromptRescale || (m == -INFINITY && m_new > m);
                 if (__any_sync(0xffffffffu, grow)) {
@@ -367,34 +459,36 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                     if (grow) m = m_new;
                 }
                 const float ref = m == -INFINITY ? 0.f : m;                    // nothing seen yet: every p is 2^-inf = 0
-                float sum[2] = {0.f, 0.f};
+                const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), ref2 = pack2(-ref, -ref);
+                uint64_t sum[2] = {0, 0};
 #pragma unroll
                 for (int hh = 0; hh < 2; ++hh) {
                     uint32_t w[32];
 #pragma unroll
                     for (int c = 0; c < 32; ++c) {
-                        const float p0 = ex2f(fmaf(__uint_as_float(s[hh][2 * c]), p.scale_log2, -ref));
-                        const float p1 = ex2f(fmaf(__uint_as_float(s[hh][2 * c + 1]), p.scale_log2, -ref));
-                        sum[0] += p0;
-                        sum[1] += p1;
+                        float p0, p1;
+                        unpack2(fma2(pack2(__uint_as_float(s[hh][2 * c]), __uint_as_float(s[hh][2 * c + 1])), scale2, ref2), p0, p1);
+                        p0 = ex2f(p0);
+                        p1 = ex2f(p1);
+                        sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
                         w[c] = In16<F16>::pack(p0, p1);
                     }
                     umma::st32(sc + hh * 32, w);
+                    umma::wait_st();
+                    umma::fence_before_thread_sync();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_p(x, hh));                  // the first half's P V may start
                 }
-                l += sum[0] + sum[1];
-                umma::wait_st();
-                umma::fence_before_thread_sync();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar_p(x));
+                float l0, l1;
+                unpack2(add2(sum[0], sum[1]), l0, l1);
+                l += l0 + l1;
             }
             if (!ok) break;
-            // the next unit's rows of Q while the last P V runs (every Q K^T of this unit is complete)
             const PromptUnit done = u;
             for (++ui; ui < uend; ++ui) {
                 u = p.units[ui];
                 if (in_unit(u)) break;
             }
-            if (ui < uend) load_q(u);
             ok = prompt_wait(bar_o(x), (uint32_t)(cs - 1) & 1u, sm_abort);
             if (!ok) break;
             umma::fence_after_thread_sync();
@@ -404,40 +498,71 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 m = -INFINITY;
                 l = 0.f;
             }
-            const int64_t orow = (int64_t)(done.row + x * TQ + tok) * p.num_q_heads + done.kv_head * G + h;
-            float* const rec = done.slot >= 0 ? p.ws + (int64_t)done.slot * (kPromptTiles * kPromptRows * (D + 2)) : nullptr;
-            const float scale = rec != nullptr ? 1.f : 1.f / l;
+            // Out by way of shared memory, 128 bytes of every row at a time, so that the warp stores whole lines.  `to`: the
+            // thread's row, counted from the unit's first, of out (rows of D values) or of the record; -1: none.
+            const bool rec = done.slot >= 0;
+            const int to = !valid ? -1 : rec ? x * kPromptRows + r : (x * TQ + tok) * p.num_q_heads + h;
+            const float scale = rec ? 1.f : 1.f / l;
             const bool none = !(l > 0.f);                                      // (of a piece: no tile of it is seen by this row)
+            float* const recs = p.ws + (int64_t)(rec ? done.slot : 0) * (kPromptTiles * kPromptRows * (D + 2));
+            const int64_t row0 = (int64_t)done.row * p.num_q_heads + done.kv_head * G;
+            const int kind = rec ? 0 : p.out_kind;                             // 0: fp32, 32 columns are 128 bytes; else 64 columns
+            char* const dst = rec ? reinterpret_cast<char*>(recs) : static_cast<char*>(p.out) + row0 * (D * (kind == 0 ? 4 : 2));
+            uint8_t* const stage = gbase + (stage_base - base) + warp * (32 * 128);
+            const int row_bytes = D * (kind == 0 ? 4 : 2);
+            auto send = [&](int chunk) {                                       // the staged 128 bytes of every row of the warp
+                __syncwarp();
 #pragma unroll
-            for (int c = 0; c < D; c += 32) {
-                uint32_t o[32];
-                umma::ld32(oc + c, o);
+                for (int i = 0; i < 8; ++i) {
+                    const int rr = i * 4 + (lane >> 3), c = lane & 7;
+                    const int at = __shfl_sync(0xffffffffu, to, rr);
+                    const uint4 v = *reinterpret_cast<const uint4*>(stage + rr * 128 + ((c ^ (rr & 7)) << 4));
+                    if (at >= 0) __stcg(reinterpret_cast<uint4*>(dst + (int64_t)at * row_bytes + chunk * 128) + c, v);
+                }
+                __syncwarp();
+            };
+#pragma unroll
+            for (int c0 = 0; c0 < D; c0 += 64) {
+                uint32_t o[64];
+                umma::ld64(oc + c0, o);
                 umma::wait_ld();
-                if (c + 32 == D) {
+                if (c0 + 64 == D) {
                     umma::fence_before_thread_sync();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(bar_of(x));                     // the next unit may write O
                 }
-                if (valid) {
 #pragma unroll
-                    for (int k = 0; k < 32; k += 4) {
-                        float4 v = make_float4(__uint_as_float(o[k]) * scale, __uint_as_float(o[k + 1]) * scale,
-                                               __uint_as_float(o[k + 2]) * scale, __uint_as_float(o[k + 3]) * scale);
-                        if (none) v = make_float4(0.f, 0.f, 0.f, 0.f);
-                        if (rec != nullptr)
-                            __stcg(reinterpret_cast<float4*>(rec + (int64_t)(x * kPromptRows + r) * D + c + k), v);
-                        else
-                            store_out4(p.out, orow * D + c + k, v, p.out_kind);
+                for (int k = 0; k < 64; ++k) o[k] = none ? 0u : __float_as_uint(__uint_as_float(o[k]) * scale);
+                uint4* const mine = reinterpret_cast<uint4*>(stage + lane * 128);
+                if (kind == 0) {
+#pragma unroll
+                    for (int hh = 0; hh < 2; ++hh) {
+#pragma unroll
+                        for (int c = 0; c < 8; ++c)
+                            mine[c ^ (lane & 7)] = make_uint4(o[32 * hh + 4 * c], o[32 * hh + 4 * c + 1], o[32 * hh + 4 * c + 2], o[32 * hh + 4 * c + 3]);
+                        send(c0 / 32 + hh);
                     }
+                } else {
+                    uint32_t w[32];
+#pragma unroll
+                    for (int c = 0; c < 32; ++c) {
+                        const float a = __uint_as_float(o[2 * c]), b = __uint_as_float(o[2 * c + 1]);
+                        w[c] = kind == 1 ? In16<false>::pack(a, b) : In16<true>::pack(a, b);
+                    }
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) mine[c ^ (lane & 7)] = make_uint4(w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
+                    send(c0 / 64);
                 }
             }
             if (valid) {
-                if (rec != nullptr)
-                    __stcg(reinterpret_cast<float2*>(rec + kPromptTiles * kPromptRows * D) + x * kPromptRows + r, make_float2(m, l));
+                if (rec)
+                    __stcg(reinterpret_cast<float2*>(recs + kPromptTiles * kPromptRows * D) + x * kPromptRows + r, make_float2(m, l));
                 else if (p.lse != nullptr)
-                    p.lse[orow] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                    p.lse[row0 + to] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
             }
         }
+    } else {
+        give_registers();                                                      // (the third warpgroup's other two warps)
     }
     umma::fence_before_thread_sync();
     __syncthreads();

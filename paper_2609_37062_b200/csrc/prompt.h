@@ -25,6 +25,7 @@ struct PromptLayout {
     std::vector<int32_t> merges;            // index of the first unit of every group of units that shares query rows
     int64_t n_slots = 0;                    // records (one per unit of such a group)
     int32_t longest = 0;                    // of the sequences
+    int64_t q_rows = 0;                     // new tokens of all sequences
 };
 
 int validate_prompt_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p);

@@ -21,6 +21,7 @@ struct PromptCall {
     const int32_t* merges;
     int32_t* status;
     unsigned n_blocks, n_merges;
+    int64_t q_rows;
     int32_t window, sinks;
     float scale;
 };

@@ -76,6 +76,7 @@ int make_prompt_layout(const decode_attn_shape_t& s, const decode_attn_policy_t&
         row0 += new_lens[b];
         if (row0 > INT32_MAX) return DA_ERR_UNSUPPORTED;
     }
+    out.q_rows = row0;
     out.block_begin.push_back(0);
     if (whole.empty()) return DA_OK;
 
