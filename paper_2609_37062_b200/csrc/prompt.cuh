@@ -16,7 +16,7 @@
 // m only follows the row's maximum when that has grown by more than 2^8 (p stays below 2^8, well inside fp16):
 // until then O and the sum keep their scale; when it does, the row's O is fetched, scaled and put back.
 //
-// Threads: four softmax warps for A, four for B, one warp whose first lane issues the MMAs, one that issues the
+// Threads: four softmax warps for A, four for B, one warp of which one lane issues the MMAs, two that issue the
 // TMA boxes.  The MMA order is  P_A V_j, Q_A K_{j+1}, P_B V_j, Q_B K_{j+1}:  while one MMA tile's softmax runs,
 // the tensor core works for the other.  Blocks are persistent and walk their run of the work list; tensor memory
 // and shared memory stay set up, the barriers count on.
@@ -59,10 +59,10 @@ struct PromptParams {
 };
 
 constexpr int kPromptSoftmaxWarps = 8;
-constexpr int kPromptMmaWarp = 8, kPromptLoadWarp = 9;
-constexpr int kPromptThreads = 384;       // three warpgroups: two of softmax, the third with the MMA and the load warp
-// Registers: 384 x 168 at launch; the softmax warpgroups take what the third gives back, 256 x 224 + 128 x 56 in all.
-constexpr int kPromptSoftmaxRegs = 224, kPromptOtherRegs = 56;
+constexpr int kPromptMmaWarp = 8, kPromptLoadWarp = 9;   // and 10
+constexpr int kPromptThreads = 384;       // three warpgroups: two of softmax, the third with the MMA and the load warps
+// Registers: 384 x 168 at launch; the softmax warpgroups take what the third gives back, 256 x 216 + 128 x 72 in all.
+constexpr int kPromptSoftmaxRegs = 216, kPromptOtherRegs = 72;
 static_assert(256 * kPromptSoftmaxRegs + 128 * kPromptOtherRegs <= 384 * 168, "more registers than the block was launched with");
 
 constexpr int kPromptStageBytes = kPromptSoftmaxWarps * 32 * 128;   // outputs on their way out: 128 bytes of a row per thread
@@ -132,6 +132,24 @@ __device__ __forceinline__ bool prompt_wait(uint32_t bar, uint32_t parity, volat
     return __all_sync(0xffffffffu, umma_wait(bar, parity, abort_flag));
 }
 
+// The same wait without suspending the warp: for the waits that the tensor core stands still behind (a suspended
+// warp comes back some 400 cycles after the last arrival).
+__device__ __forceinline__ bool prompt_spin(uint32_t bar, uint32_t parity, volatile int* abort_flag)
+{
+    const long long t0 = clock64();
+    for (int i = 1;; ++i) {
+        if (__any_sync(0xffffffffu, mbar_test_wait(bar, parity))) return true;
+        if ((i & 63) == 0) {
+            bool stop = *abort_flag != 0;
+            if (!stop && clock64() - t0 > kWaitLimitCycles) {
+                *abort_flag = 1;
+                stop = true;
+            }
+            if (__any_sync(0xffffffffu, stop)) return false;
+        }
+    }
+}
+
 template <int D, bool F16>
 __global__ void __launch_bounds__(kPromptThreads, 1)
 decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensorMap q_map, const __grid_constant__ CUtensorMap k_map,
@@ -146,8 +164,8 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
     const uint32_t q_base = base, k_base = base + 2 * Cfg::kTileBytes, v_base = k_base + NS * Cfg::kTileBytes;
     const uint32_t stage_base = v_base + NS * Cfg::kTileBytes;
     const uint32_t bar_base = stage_base + kPromptStageBytes;
-    // per MMA tile x: q (its rows have landed), qe (no longer read), s (logits complete), p (a half of the weights written: of the
-    // first, of the last 64 tokens), o (P V complete), of (output read); per stage: K and V landed (kf, vf), K and V no longer read (ke, ve); drain
+    // per MMA tile x: q (its rows have landed), qe (no longer read), s (logits complete), p (weights written: of the first 96
+    // tokens, of the last 32), o (P V complete), of (output read); per stage: K and V landed (kf, vf), K and V no longer read (ke, ve); drain
     auto bar_q = [&](int x) { return bar_base + 8 * x; };
     auto bar_s = [&](int x) { return bar_base + 16 + 8 * x; };
     auto bar_p = [&](int x, int half) { return bar_base + 32 + 16 * x + 8 * half; };
@@ -197,19 +215,23 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
     const int G = p.group, TQ = p.tokens_per_tile;
     auto tile_at = [](const PromptUnit& u, int i) { return i < u.sink_tiles ? i : i - u.sink_tiles + u.window_tile; };
 
-    if (warp == kPromptLoadWarp) {
-        // ------------------------------------------------------------ TMA
+    if (warp == kPromptLoadWarp || warp == kPromptLoadWarp + 1) {
+        // ------------------------------------------------------------ TMA: a warp for Q and K, a warp for V
+        // (a warp takes 1,400 cycles to issue the 16 boxes of a tile, 90 each, while the softmax warps beside it are busy:
+        // one warp for both tensors was what paced the kernel, 3,400 against 2,900 cycles a tile)
         give_registers();
+        const bool is_v = warp == kPromptLoadWarp + 1;
+        const CUtensorMap* const map = is_v ? &v_map : &k_map;
+        const uint32_t ring = is_v ? v_base : k_base, bar_full = is_v ? bar_vf : bar_kf, bar_empty = is_v ? bar_ve : bar_ke;
         const uint64_t keep = l2_policy_evict_normal();
         const int ts = p.tile_shift;
         const int sub = (lane / Cfg::kHalves) & 7, hf = lane % Cfg::kHalves;    // lane's box: 16 tokens, half of the head dimension
         constexpr int BOXES = 8 * Cfg::kHalves;
-        int n = 0;                                                              // K/V tiles so far
+        int n = 0;                                                              // tiles so far
         int cu[2] = {0, 0};                                                     // units so far, per MMA tile
         bool ok = true;
         for (int ui = ubeg; ui < uend && ok; ++ui) {
             const PromptUnit u = p.units[ui];
-            const int X = u.n_tok > TQ ? 2 : 1;
             const int lo = p.window > 0 ? max(0, u.pos - p.window + 1) : 0;     // what the first query sees through its window
             const int end = min(u.pos + u.n_tok, u.seq_len);
             const int32_t* const bt = p.block_table + (int64_t)u.seq * p.max_pages_per_seq;
@@ -222,42 +244,18 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
             };
             int page = page_of(u.tile_begin);
             for (int i = u.tile_begin; i < u.tile_end && ok; ++i, ++n) {
-                const int t0 = tile_at(u, i) * kPromptKvTokens, s0 = t0 + sub * 16;
+                const int s0 = tile_at(u, i) * kPromptKvTokens + sub * 16;
                 const int next_page = page_of(i + 1);
-                const bool part = seen(s0) && !whole(s0);
                 if ((unsigned)page >= (unsigned)p.num_pages && seen(s0)) {
                     record_status(p.status, DA_ERR_BAD_PAGE);                   // such a box is read as zeros
                     page = (int)p.num_pages;
                 }
                 const int slot0 = (s0 >> 4 & ((1 << ts) - 1)) << 4;
                 const int st = n % NS;
-                const uint32_t parity = (uint32_t)(n / NS + 1) & 1u;
-                if (n >= NS) ok = prompt_wait(bar_ke + 8 * st, parity, sm_abort);
+                if (n >= NS) ok = prompt_wait(bar_empty + 8 * st, (uint32_t)(n / NS + 1) & 1u, sm_abort);
                 if (!ok) break;
-                if (lane == 0) mbar_arrive_expect_tx(bar_kf + 8 * st, Cfg::kTileBytes);
-                __syncwarp();
-                if (lane < BOXES)
-                    tma_load_4d(k_base + st * Cfg::kTileBytes + hf * Cfg::kHalfBytes + sub * 2048, &k_map, bar_kf + 8 * st,
-                                hf * 64, slot0, u.kv_head, page, keep);
-                if (i == u.tile_begin) {
-                    // The unit's query rows: TQ tokens x the group's heads, rows of the MMA tile in that order.  (Tokens of
-                    // a ragged end are other rows of q, or zeros behind the last: what comes of them is not stored.)
-                    for (int x = 0; x < X && ok; ++x) {
-                        if (cu[x] > 0) ok = prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
-                        if (!ok) break;
-                        ++cu[x];
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(bar_q(x), Cfg::kHalves * G * TQ * 128);
-                            for (int h = 0; h < Cfg::kHalves; ++h)
-                                tma_load_3d(q_base + x * Cfg::kTileBytes + h * Cfg::kHalfBytes, &q_map, bar_q(x), h * 64, u.kv_head * G,
-                                            u.row + x * TQ);
-                        }
-                        __syncwarp();
-                    }
-                    if (!ok) break;
-                }
-                if (n >= NS) ok = prompt_wait(bar_ve + 8 * st, parity, sm_abort);
-                if (!ok) break;
+                // V boxes with rows to clear are copied by hand
+                const bool part = is_v && seen(s0) && !whole(s0);
                 const uint32_t parts = __ballot_sync(0xffffffffu, part && hf == 0 && lane < BOXES);
                 for (uint32_t m = parts; m != 0; m &= m - 1) {
                     const int from = __ffs(m) - 1;                              // the lane whose box it is
@@ -277,21 +275,34 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                     asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
                     __syncwarp();
                 }
-                if (lane == 0) mbar_arrive_expect_tx(bar_vf + 8 * st, Cfg::kTileBytes - __popc(parts) * (16 * D * 2));
+                if (lane == 0) mbar_arrive_expect_tx(bar_full + 8 * st, Cfg::kTileBytes - __popc(parts) * (16 * D * 2));
                 __syncwarp();
                 if (lane < BOXES && !part)
-                    tma_load_4d(v_base + st * Cfg::kTileBytes + hf * Cfg::kHalfBytes + sub * 2048, &v_map, bar_vf + 8 * st,
-                                hf * 64, slot0, u.kv_head, page, keep);
+                    tma_load_4d(ring + st * Cfg::kTileBytes + hf * Cfg::kHalfBytes + sub * 2048, map, bar_full + 8 * st, hf * 64, slot0,
+                                u.kv_head, page, keep);
+                if (!is_v && i == u.tile_begin) {
+                    // The unit's query rows: TQ tokens x the group's heads, rows of the MMA tile in that order.  (Tokens of
+                    // a ragged end are other rows of q, or zeros behind the last: what comes of them is not stored.)
+                    for (int x = 0; x < (u.n_tok > TQ ? 2 : 1) && ok; ++x) {
+                        if (cu[x] > 0) ok = prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
+                        if (!ok) break;
+                        ++cu[x];
+                        if (lane == 0) {
+                            mbar_arrive_expect_tx(bar_q(x), Cfg::kHalves * G * TQ * 128);
+                            for (int h = 0; h < Cfg::kHalves; ++h)
+                                tma_load_3d(q_base + x * Cfg::kTileBytes + h * Cfg::kHalfBytes, &q_map, bar_q(x), h * 64, u.kv_head * G,
+                                            u.row + x * TQ);
+                        }
+                        __syncwarp();
+                    }
+                }
                 page = next_page;
             }
         }
         if (*sm_abort != 0) {
             // given up somewhere: nothing may land in shared memory after the block has left (a copy always lands)
-            for (int i = max(0, n - NS); i < n; ++i) {
-                mbar_wait(bar_kf + 8 * (i % NS), (uint32_t)(i / NS) & 1u);
-                mbar_wait(bar_vf + 8 * (i % NS), (uint32_t)(i / NS) & 1u);
-            }
-            if (!ok) mbar_wait(bar_kf + 8 * (n % NS), (uint32_t)(n / NS) & 1u, 1000000LL);   // the tile whose V was not issued
+            for (int i = max(0, n - NS); i <= n; ++i)
+                if (i < n || !ok) mbar_wait(bar_full + 8 * (i % NS), (uint32_t)(i / NS) & 1u, i < n ? kWaitLimitCycles : 1000000LL);
             for (int x = 0; x < 2; ++x)
                 if (cu[x] > 0) mbar_wait(bar_q(x), (uint32_t)(cu[x] - 1) & 1u);
         }
@@ -328,15 +339,18 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                     }
                     __syncwarp();
                 };
-                auto pv = [&](int x, int j, int half) {
+                auto pv = [&](int x, int j, int part) {                        // the first 96 tokens, the last 32
                     const int st = (n + j) % NS;
                     umma::fence_after_thread_sync();
-                    const uint64_t vd = v_desc + (uint64_t)(st * kTileUnits + half * 512);
-                    const uint32_t pd = tmem + x * 128 + half * 32, od = tmem + 256 + x * 128;
+                    const uint64_t vd = v_desc + (uint64_t)(st * kTileUnits);
+                    const uint32_t pd = tmem + x * 128, od = tmem + 256 + x * 128;
                     if (elect_one()) {
+                        if (part == 0) {
 #pragma unroll
-                        for (int k = 0; k < 4; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, j > 0 || half > 0 || k > 0);
-                        if (half == 1) {
+                            for (int k = 0; k < 6; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, j > 0 || k > 0);
+                        } else {
+#pragma unroll
+                            for (int k = 6; k < 8; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, true);
                             umma::commit(bar_o(x));
                             if (x == X - 1) umma::commit(bar_ve + 8 * st);
                         }
@@ -353,10 +367,10 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                         // (the weights last: every wait behind theirs would be time the tensor core stands still)
                         ok = prompt_wait(bar_vf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort) &&
                              (j > 0 || cu[x] == 0 || prompt_wait(bar_of(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort)) &&
-                             prompt_wait(bar_p(x, 0), (uint32_t)cs[x] & 1u, sm_abort);
+                             prompt_spin(bar_p(x, 0), (uint32_t)cs[x] & 1u, sm_abort);
                         if (!ok) break;
                         pv(x, j, 0);
-                        ok = prompt_wait(bar_p(x, 1), (uint32_t)cs[x] & 1u, sm_abort);
+                        ok = prompt_spin(bar_p(x, 1), (uint32_t)cs[x] & 1u, sm_abort);
                         if (!ok) break;
                         pv(x, j, 1);
                         ++cs[x];
@@ -414,28 +428,33 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 umma::fence_after_thread_sync();
                 uint32_t s[2][64];
                 umma::ld64(sc, s[0]);
-                umma::ld64(sc + 64, s[1]);
                 umma::wait_ld();
+                umma::ld64(sc + 64, s[1]);                                     // on its way while the first half is looked through
                 const bool masked = t0 + kPromptKvTokens - 1 > q_lo ||
                                     (p.window > 0 && t0 <= q_hi - p.window && t0 + kPromptKvTokens > p.sinks);
-                if (masked) {
-                    // one bit per column, 32 at a time, then 32 selects on known bits (conditions column by column
-                    // become branches: 15,000 cycles a tile instead of a few hundred)
-                    const int hi = qi - t0 + 1, lo = p.window > 0 ? qi - p.window + 1 - t0 : 0, sk = p.sinks - t0;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t vis = low_bits(hi - 32 * q) & (~low_bits(lo - 32 * q) | low_bits(sk - 32 * q));
-#pragma unroll
-                        for (int c = 0; c < 32; ++c) {
-                            uint32_t& x = s[q >> 1][(q & 1) * 32 + c];
-                            x = (vis & (1u << c)) != 0u ? x : 0xff800000u;                       // -inf
-                        }
-                    }
-                }
                 float mx[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-                for (int c = 0; c < 128; c += 2)
-                    mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(s[c >> 6][c & 63]), __uint_as_float(s[c >> 6][(c & 63) + 1]));
+                for (int hh = 0; hh < 2; ++hh) {
+                    if (hh == 1) umma::wait_ld();
+                    if (masked) {
+                        // one bit per column, 32 at a time, then 32 selects on known bits (conditions column by column
+                        // become branches: 15,000 cycles a tile instead of a few hundred)
+                        const int hi = qi - t0 + 1, lo = p.window > 0 ? qi - p.window + 1 - t0 : 0, sk = p.sinks - t0;
+#pragma unroll
+                        for (int q = 0; q < 2; ++q) {
+                            const int c0 = 64 * hh + 32 * q;
+                            const uint32_t vis = low_bits(hi - c0) & (~low_bits(lo - c0) | low_bits(sk - c0));
+#pragma unroll
+                            for (int c = 0; c < 32; ++c) {
+                                uint32_t& v = s[hh][32 * q + c];
+                                v = (vis & (1u << c)) != 0u ? v : 0xff800000u;                   // -inf
+                            }
+                        }
+                    }
+#pragma unroll
+                    for (int c = 0; c < 64; c += 2)
+                        mx[(c >> 1) & 3] = max3(mx[(c >> 1) & 3], __uint_as_float(s[hh][c]), __uint_as_float(s[hh][c + 1]));
+                }
                 const float m_new = fmaxf(fmaxf(mx[0], mx[1]), fmaxf(mx[2], mx[3])) * p.scale_log2;   // the scale is positive
                 const bool grow = m_new > m + kPromptRescale || (m == -INFINITY && m_new > m);
                 if (__any_sync(0xffffffffu, grow)) {
@@ -462,22 +481,26 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 const uint64_t scale2 = pack2(p.scale_log2, p.scale_log2), ref2 = pack2(-ref, -ref);
                 uint64_t sum[2] = {0, 0};
 #pragma unroll
-                for (int hh = 0; hh < 2; ++hh) {
-                    uint32_t w[32];
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t w[16];
 #pragma unroll
-                    for (int c = 0; c < 32; ++c) {
+                    for (int c = 0; c < 16; ++c) {
+                        const uint32_t* const v = &s[q >> 1][(q & 1) * 32 + 2 * c];
                         float p0, p1;
-                        unpack2(fma2(pack2(__uint_as_float(s[hh][2 * c]), __uint_as_float(s[hh][2 * c + 1])), scale2, ref2), p0, p1);
+                        unpack2(fma2(pack2(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, ref2), p0, p1);
                         p0 = ex2f(p0);
                         p1 = ex2f(p1);
                         sum[c & 1] = add2(sum[c & 1], pack2(p0, p1));
                         w[c] = In16<F16>::pack(p0, p1);
                     }
-                    umma::st32(sc + hh * 32, w);
-                    umma::wait_st();
-                    umma::fence_before_thread_sync();
-                    __syncwarp();
-                    if (lane == 0) mbar_arrive(bar_p(x, hh));                  // the first half's P V may start
+                    umma::st16(sc + q * 16, w);
+                    if (q >= 2) {
+                        // P V may start on the first 96 tokens, then on the rest: what follows the last weight is short
+                        umma::wait_st();
+                        umma::fence_before_thread_sync();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar_p(x, q - 2));
+                    }
                 }
                 float l0, l1;
                 unpack2(add2(sum[0], sum[1]), l0, l1);
@@ -562,7 +585,7 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
             }
         }
     } else {
-        give_registers();                                                      // (the third warpgroup's other two warps)
+        give_registers();                                                      // (the third warpgroup's last warp)
     }
     umma::fence_before_thread_sync();
     __syncthreads();
@@ -588,21 +611,26 @@ __global__ void __launch_bounds__(256) decode_attn_prompt_merge_kernel(const Pro
     const float* const rec = p.ws + (int64_t)u.slot * RF;
     const float2* const ml = reinterpret_cast<const float2*>(rec + kPromptTiles * kPromptRows * D) + row;
     const float4* const col = reinterpret_cast<const float4*>(rec) + row * D4 + d4;
-    float M = -INFINITY;
-    for (int k = 0; k < u.n_pieces; ++k) M = fmaxf(M, __ldcg(ml + k * (RF / 2)).x);
+    // (the first two pieces - most cut units have no more - are asked for together)
+    const float2 s0 = __ldcg(ml), s1 = __ldcg(ml + RF / 2);
+    const float4 v0 = __ldcg(col), v1 = __ldcg(col + RF / 4);
+    float M = fmaxf(s0.x, s1.x);
+    for (int k = 2; k < u.n_pieces; ++k) M = fmaxf(M, __ldcg(ml + k * (RF / 2)).x);
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float ls = 0.f;
-    if (M != -INFINITY)
-        for (int k = 0; k < u.n_pieces; ++k) {
-            const float2 s = __ldcg(ml + k * (RF / 2));
-            const float4 v = __ldcg(col + k * (RF / 4));
-            const float w = ex2f(s.x - M);
-            acc.x = fmaf(w, v.x, acc.x);
-            acc.y = fmaf(w, v.y, acc.y);
-            acc.z = fmaf(w, v.z, acc.z);
-            acc.w = fmaf(w, v.w, acc.w);
-            ls = fmaf(w, s.y, ls);
-        }
+    auto add = [&](const float2& s, const float4& v) {
+        const float w = ex2f(s.x - M);
+        acc.x = fmaf(w, v.x, acc.x);
+        acc.y = fmaf(w, v.y, acc.y);
+        acc.z = fmaf(w, v.z, acc.z);
+        acc.w = fmaf(w, v.w, acc.w);
+        ls = fmaf(w, s.y, ls);
+    };
+    if (M != -INFINITY) {
+        add(s0, v0);
+        add(s1, v1);
+        for (int k = 2; k < u.n_pieces; ++k) add(__ldcg(ml + k * (RF / 2)), __ldcg(col + k * (RF / 4)));
+    }
     const float inv = ls > 0.f ? 1.f / ls : 0.f;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
     const int64_t orow = (int64_t)(u.row + x * p.tokens_per_tile + tok) * p.num_q_heads + u.kv_head * p.group + h;
