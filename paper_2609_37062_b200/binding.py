@@ -195,17 +195,35 @@ def _check(status: int, where: str) -> None:
 def _ptr(t) -> Optional[int]:
     if t is None:
         return None
-    if isinstance(t, int):
-        return t
+    address = getattr(t, "data_ptr", None)            # a torch tensor, the usual case
+    if address is not None:
+        return address()
     if isinstance(t, np.ndarray):
         return t.ctypes.data
-    return t.data_ptr()
+    return t
+
+
+_raw_stream = None
+
+
+def _current_stream() -> int:
+    """torch.cuda.current_stream().cuda_stream, without the Stream object where torch lets us: that object costs
+    3 us a call, more than the launch itself."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        stream, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        torch.cuda.current_stream()                   # (initialises CUDA as ever)
+        if stream is not None and device is not None:
+            _raw_stream = lambda: stream(device())
+        else:
+            _raw_stream = lambda: torch.cuda.current_stream().cuda_stream
+    return _raw_stream()
 
 
 def _stream(stream) -> int:
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        return _current_stream()
     if isinstance(stream, int):
         return stream
     return stream.cuda_stream
@@ -364,17 +382,24 @@ def decode_attn_combine(plan: Plan, workspace, out, lse=None, stream=None, check
     return rc
 
 
+def _weights_layout(shape: Shape, weights, weights_out, where: str):
+    """Strides and row length of two buffers of totals that have to be laid out alike."""
+    size, strides = weights.shape, weights.stride()
+    if size != weights_out.shape or strides != weights_out.stride() or strides[2] != 1 or size[0] < shape.batch or \
+            size[1] != shape.num_kv_heads:
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
+    return strides, size[2]
+
+
 def decode_attn_add_weights(plan: Plan, workspace, lse, seq_lens, weights, weights_out=None, stream=None,
                             check: bool = True) -> int:
     """weights, weights_out: fp32 [batch, num_kv_heads, tokens], innermost axis contiguous, other strides equal;
     weights_out None: in place."""
     if weights_out is None:
         weights_out = weights
-    if weights.shape != weights_out.shape or weights.stride() != weights_out.stride() or weights.stride(2) != 1 or \
-            weights.shape[0] < plan.shape.batch or weights.shape[1] != plan.shape.num_kv_heads:
-        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_add_weights")
+    strides, tokens = _weights_layout(plan.shape, weights, weights_out, "decode_attn_add_weights")
     rc = _lib.decode_attn_add_weights(plan.handle, _ptr(workspace), _ptr(lse), _ptr(seq_lens), _ptr(weights),
-                                      _ptr(weights_out), weights.shape[2], weights.stride(0), weights.stride(1), _stream(stream))
+                                      _ptr(weights_out), tokens, strides[0], strides[1], _stream(stream))
     if check:
         _check(rc, "decode_attn_add_weights")
     return rc
@@ -459,15 +484,14 @@ def decode_attn_evict(shape: Shape, budget_tokens: int, sink_tokens: int, recent
     num_kv_heads, budget_tokens]; seq_lens_out: int32 [batch]; status: int32 [1] or None."""
     if weights_out is None:
         weights_out = weights
-    if weights.shape != weights_out.shape or weights.stride() != weights_out.stride() or weights.stride(2) != 1 or \
-            weights.shape[0] < shape.batch or weights.shape[1] != shape.num_kv_heads or \
-            kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous():
+    strides, tokens = _weights_layout(shape, weights, weights_out, "decode_attn_evict")
+    if kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous():
         raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_evict")
     a = _evict_args(budget_tokens, sink_tokens, recent_tokens, dst_block_table.shape[1])
     a.seq_lens, a.block_table, a.dst_block_table = _ptr(seq_lens), _ptr(block_table), _ptr(dst_block_table)
     a.k_cache, a.v_cache = _ptr(k_cache), _ptr(v_cache)
     a.weights, a.weights_out = _ptr(weights), _ptr(weights_out)
-    a.weight_tokens, a.stride_seq, a.stride_head = weights.shape[2], weights.stride(0), weights.stride(1)
+    a.weight_tokens, a.stride_seq, a.stride_head = tokens, strides[0], strides[1]
     a.kept, a.seq_lens_out, a.status = _ptr(kept), _ptr(seq_lens_out), _ptr(status)
     rc = _lib.decode_attn_evict(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
     if check:
