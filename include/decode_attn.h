@@ -111,8 +111,9 @@ typedef struct {
     int32_t window_tokens;  /* > 0: sliding window.  The step's query, at position seq_len - 1, attends the
                                last window_tokens positions (its own among them) and the first
                                sink_tokens ones.  Block-table entries of pages that hold neither are
-                               never read: an engine may give such pages back.  The plan's units then
-                               count visible positions: whole 16-token tiles of the gap are left out.
+                               never read: an engine may give such pages back (and
+                               decode_attn_validate_block_table then has entries to object to).  The plan's units
+                               then count visible positions: whole 16-token tiles of the gap are left out.
                                Tensor-core kernel MMA_TMA, no shared prefix.                          */
     int32_t sink_tokens;    /* with window_tokens: first positions that stay visible (0: none)         */
     int32_t track_weights;  /* 1: the launch also leaves every logit in the workspace, from which
@@ -401,10 +402,11 @@ int decode_attn_prompt_plan_layout(const decode_attn_shape_t *shape, const decod
 /* Builds a plan: new_lens_host and seq_lens_host [batch] on the host, seq_lens
  * counting the new tokens.  The policy's window_tokens, sink_tokens, sm_count,
  * split_mode (AUTO: work dealt evenly to the SMs, cutting units where shares
- * meet; DETERMINISTIC: units cut at multiples of chunk_tokens - of 128, 0:
- * 4,096 - of their own tile lists, so that a sequence's bits do not depend on
- * the batch) and chunk_tokens apply; everything else must be 0
- * (DA_ERR_UNSUPPORTED).  Buffers, upload and lifetime are those of
+ * meet; DETERMINISTIC: units cut at multiples of chunk_tokens - itself a
+ * multiple of 128, 0: 4,096 - of their own tile lists, so that a sequence's
+ * bits do not depend on the batch) and, in DETERMINISTIC, chunk_tokens apply;
+ * everything else must be 0 (DA_ERR_UNSUPPORTED, also for a work list of more
+ * than 4 million units).  Buffers, upload and lifetime are those of
  * decode_attn_plan. */
 int decode_attn_prompt_plan(const decode_attn_shape_t *shape, const decode_attn_policy_t *policy,
                             const int32_t *new_lens_host, const int32_t *seq_lens_host,

@@ -24,7 +24,7 @@ struct Layout {
     std::vector<int32_t> splits;            // [batch]
     std::vector<int32_t> slot_base;         // [batch], -1 when the sequence has one split
     std::vector<int32_t> visible;           // [batch] tokens the plan covers: the length, less the tiles a window cuts out
-    std::vector<int32_t> tile_base;         // [batch] visible 16-token tiles of the sequences before
+    std::vector<int32_t> tile_base;         // [batch] visible 16-token tiles of the sequences before (plans that track weights)
     int64_t n_tiles = 0;                    // of all sequences together
     int64_t n_slots = 0;
     int32_t chunk_tokens = 0;

@@ -12,6 +12,7 @@
 #include "prompt.h"
 
 #include <algorithm>
+#include <new>
 
 #include "planner.h"
 
@@ -22,6 +23,7 @@ namespace {
 constexpr int kUnitTiles = 1;     // a unit's set-up and epilogue, in tiles
 constexpr int kMinShare = 6;      // tiles: below this a cut costs more (the merge launch) than it spreads
 constexpr int kMinPiece = 3;
+constexpr int64_t kMaxUnits = 1 << 22;    // 200 MB of work list, far beyond what one call is worth making for
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
@@ -32,12 +34,13 @@ int validate_prompt_policy(const decode_attn_shape_t& s, const decode_attn_polic
     const int rc = validate_policy(s, p);
     if (rc != DA_OK) return rc;
     if (p.split_mode == DA_SPLIT_FIXED_COUNT || p.kernel != DA_KERNEL_AUTO || p.fuse_combine || p.capacity_batch > 0 ||
-        p.shared_prefix_tokens > 0 || p.track_weights)
+        p.shared_prefix_tokens > 0 || p.track_weights || p.max_splits > 0 || p.ctas_per_sm > 0)
         return DA_ERR_UNSUPPORTED;
+    if (p.split_mode == DA_SPLIT_DETERMINISTIC && p.chunk_tokens % kPromptKvTokens != 0) return DA_ERR_INVALID_ARG;
     return DA_OK;
 }
 
-int make_prompt_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, const int32_t* new_lens,
+static int fill_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, const int32_t* new_lens,
                        const int32_t* seq_lens, int sm_count, PromptLayout& out)
 {
     if (sm_count <= 0) return DA_ERR_INVALID_ARG;
@@ -46,10 +49,15 @@ int make_prompt_layout(const decode_attn_shape_t& s, const decode_attn_policy_t&
     const int per_unit = kPromptTiles * (kPromptRows / G);
     out = PromptLayout();
     std::vector<PromptUnit> whole;
-    int64_t row0 = 0;
+    int64_t row0 = 0, n_units = 0;
     for (int b = 0; b < s.batch; ++b) {
         if (new_lens[b] < 0 || seq_lens[b] < new_lens[b]) return DA_ERR_INVALID_ARG;
         if (ceil_div(seq_lens[b], s.page_size) > s.max_pages_per_seq) return DA_ERR_INVALID_ARG;
+        n_units += ceil_div(new_lens[b], per_unit) * s.num_kv_heads;
+        if (n_units > kMaxUnits) return DA_ERR_UNSUPPORTED;
+    }
+    whole.reserve((size_t)n_units);
+    for (int b = 0; b < s.batch; ++b) {
         const int64_t first = (int64_t)seq_lens[b] - new_lens[b];
         out.longest = std::max(out.longest, seq_lens[b]);
         for (int g = 0; g < s.num_kv_heads; ++g) {
@@ -99,6 +107,9 @@ int make_prompt_layout(const decode_attn_shape_t& s, const decode_attn_policy_t&
 
     if (p.split_mode == DA_SPLIT_DETERMINISTIC) {
         const int64_t chunk = std::max<int64_t>(1, (p.chunk_tokens > 0 ? p.chunk_tokens : kPromptDeterministicChunk) / kPromptKvTokens);
+        int64_t pieces = 0;
+        for (const PromptUnit& u : whole) pieces += ceil_div(u.tile_end, chunk);
+        if (pieces > kMaxUnits) return DA_ERR_UNSUPPORTED;
         for (const PromptUnit& u : whole) {
             cuts.clear();
             for (int64_t t = chunk; t < u.tile_end; t += chunk) cuts.push_back((int32_t)t);
@@ -167,6 +178,16 @@ int make_prompt_layout(const decode_attn_shape_t& s, const decode_attn_policy_t&
     return DA_OK;
 }
 
+int make_prompt_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, const int32_t* new_lens,
+                       const int32_t* seq_lens, int sm_count, PromptLayout& out)
+{
+    try {
+        return fill_layout(s, p, new_lens, seq_lens, sm_count, out);
+    } catch (const std::bad_alloc&) {
+        return DA_ERR_UNSUPPORTED;        // (nothing throws across the C boundary)
+    }
+}
+
 }  // namespace da
 
 extern "C" int decode_attn_prompt_plan_layout(const decode_attn_shape_t* shape, const decode_attn_policy_t* policy,
@@ -180,6 +201,7 @@ extern "C" int decode_attn_prompt_plan_layout(const decode_attn_shape_t* shape, 
     rc = da::validate_prompt_policy(*shape, *policy);
     if (rc != DA_OK) return rc;
     da::PromptLayout lay;
+    *n_units_out = *n_blocks_out = 0;
     rc = da::make_prompt_layout(*shape, *policy, new_lens_host, seq_lens_host, sm_count, lay);
     if (rc != DA_OK) return rc;
     *n_units_out = (int64_t)lay.units.size();

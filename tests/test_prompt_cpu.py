@@ -110,11 +110,21 @@ def test_deterministic_pieces_depend_on_the_sequence_alone():
     (dict(capacity_batch=4, capacity_tokens=100), da.DA_ERR_UNSUPPORTED), (dict(track_weights=1), da.DA_ERR_UNSUPPORTED),
     (dict(shared_prefix_tokens=16), da.DA_ERR_UNSUPPORTED),
     (dict(split_mode=da.DA_SPLIT_FIXED_COUNT, fixed_count=2), da.DA_ERR_UNSUPPORTED),
+    (dict(max_splits=4), da.DA_ERR_UNSUPPORTED), (dict(ctas_per_sm=1), da.DA_ERR_UNSUPPORTED),
+    (dict(split_mode=da.DA_SPLIT_DETERMINISTIC, chunk_tokens=16), da.DA_ERR_INVALID_ARG),
     (dict(sink_tokens=4), da.DA_ERR_INVALID_ARG), (dict(window_tokens=-1), da.DA_ERR_INVALID_ARG)])
 def test_policies_that_are_refused(kw, status):
     with pytest.raises(da.DecodeAttnError) as e:
         da.decode_attn_prompt_plan_layout(shape(1), da.make_policy(**kw), [10], [100], 148)
     assert e.value.status == status
+
+
+def test_work_lists_too_long_to_make_are_refused():
+    sh = da.make_shape(1, 16, 1, 64, 256, 1 << 23, 1 << 30, (256 * 64, 64, 64))
+    for pol, new in ((da.make_policy(), 1 << 30), (da.make_policy(split_mode=da.DA_SPLIT_DETERMINISTIC, chunk_tokens=128), 1 << 20)):
+        with pytest.raises(da.DecodeAttnError) as e:
+            da.decode_attn_prompt_plan_layout(sh, pol, [new], [1 << 30], 148)
+        assert e.value.status == da.DA_ERR_UNSUPPORTED
 
 
 @pytest.mark.parametrize("new,lens", [([-1], [10]), ([11], [10]), ([1], [16 * 65536 + 1])])
