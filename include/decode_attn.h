@@ -473,7 +473,7 @@ int decode_attn_add_weights(const decode_attn_plan_t *plan, const void *workspac
  * whole.  Positions in the cache shift: it is for models whose keys carry
  * their position before they are cached.
  *
- * Two launches on `stream`, nothing is allocated, capture-safe (the lengths
+ * One or two launches on `stream`, nothing is allocated, capture-safe (the lengths
  * are read on the device).  A row whose length does not fit the block table
  * or the totals is left alone (DA_ERR_STALE_PLAN), a token whose page id lies
  * outside the pool is not moved (DA_ERR_BAD_PAGE); either is recorded in

@@ -4,7 +4,7 @@
 // first `sinks` and the last `recent` tokens stay, and of the tokens between
 // them the budget - sinks - recent with the largest totals; among equal totals
 // the lowest position stays.  What stays keeps its order and moves to fresh
-// pages.  Two launches:
+// pages.  Two steps:
 //
 //   select  one block per (sequence, KV head).  The totals become 32-bit keys whose unsigned order is the order
 //           of the floats, and the key of rank k is found by counting them into bins between the least and the
@@ -14,6 +14,8 @@
 //           rows are walked in runs), so they can be compacted in place.  (A cluster of eight blocks per row
 //           loses: the exchange of a counting step through distributed shared memory takes 1,300 cycles.)
 //   move    K and V rows of the kept positions, 16 bytes a lane, 32 tokens of one KV head per warp.
+//
+// Where that is little per row the select blocks move their rows themselves, in one launch.
 //
 // Select reads 4 bytes per token and KV head, move reads and writes 4 D of them for every kept one: the
 // second is the bound, by memory.
@@ -67,9 +69,51 @@ __device__ __forceinline__ int evict_length(const EvictParams& p, int b)
     return L;
 }
 
+// K and V rows of the kept tokens j0 .. j0 + 31 of one (sequence, KV head), by one warp.
+template <int D>
+__device__ __forceinline__ void move_tokens(const EvictParams& p, int b, int g, int j0, int lane)
+{
+    constexpr int LT = D / 4;                                 // lanes of a token: 16-byte chunks of its K row, then of its V row
+    constexpr int TP = 32 / LT;                               // tokens a warp moves at a time
+    // lane i: source and destination page of token j0 + i
+    const int j = j0 + lane;
+    int src = 0, src_page = -1, dst_page = -1;
+    if (j < p.budget) {
+        src = __ldcg(p.kept + ((int64_t)b * p.num_kv_heads + g) * p.budget + j);
+        dst_page = __ldg(p.dst_block_table + (int64_t)b * p.dst_max_pages + (j >> p.page_shift));
+        src_page = __ldg(p.block_table + (int64_t)b * p.max_pages_per_seq + (src >> p.page_shift));
+        if ((unsigned)src_page >= (unsigned)p.num_pages || (unsigned)dst_page >= (unsigned)p.num_pages) {
+            if (p.status) record_status(p.status, DA_ERR_BAD_PAGE);   // the row is not moved
+            src_page = dst_page = -1;
+        }
+    }
+    const int mask = (1 << p.page_shift) - 1;
+    const int part = lane % LT, ch = part % (D / 8);          // which row (K, V), which 16 bytes of it
+    const bool is_v = part >= D / 8;
+    __nv_bfloat16* const pool = (is_v ? p.v : p.k) + (int64_t)g * (is_v ? p.v_stride_head : p.k_stride_head) + ch * 8;
+    const int64_t sp = is_v ? p.v_stride_page : p.k_stride_page, st = is_v ? p.v_stride_token : p.k_stride_token;
+#pragma unroll
+    for (int i0 = 0; i0 < kMoveTokens; i0 += TP * kMoveUnroll) {
+        uint4 x[kMoveUnroll];
+        int to_page[kMoveUnroll];
+#pragma unroll
+        for (int u = 0; u < kMoveUnroll; ++u) {
+            const int i = i0 + u * TP + lane / LT;
+            const int from = __shfl_sync(0xffffffffu, src_page, i), slot = __shfl_sync(0xffffffffu, src, i) & mask;
+            to_page[u] = __shfl_sync(0xffffffffu, dst_page, i);
+            if (from >= 0) x[u] = __ldcs(reinterpret_cast<const uint4*>(pool + from * sp + slot * st));
+        }
+#pragma unroll
+        for (int u = 0; u < kMoveUnroll; ++u) {
+            const int i = i0 + u * TP + lane / LT;
+            if (to_page[u] >= 0) *reinterpret_cast<uint4*>(pool + to_page[u] * sp + ((j0 + i) & mask) * st) = x[u];
+        }
+    }
+}
+
 // One block of NT threads per (sequence, KV head).  BINS: of a counting pass.  HELD: totals a thread keeps the
-// keys of in registers, where the row has no more.
-template <int NT, int BINS, int HELD>
+// keys of in registers, where the row has no more.  D: the block moves its rows itself (0: the other launch does).
+template <int NT, int BINS, int HELD, int D>
 __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const EvictParams p)
 {
     constexpr int WARPS = NT / 32, PER = BINS / NT;
@@ -296,16 +340,17 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
         equal += run_eq;
     }
     for (int t = p.budget + tid; t < L; t += NT) o[t] = 0.f;      // tokens to come start from nothing
+    if (D != 0) {
+        __syncthreads();                                      // the block's kept positions are written
+        for (int j0 = warp * kMoveTokens; j0 < p.budget; j0 += WARPS * kMoveTokens) move_tokens<D == 0 ? 64 : D>(p, b, g, j0, lane);
+    }
 }
 
 template <int D>
 __global__ void __launch_bounds__(kMoveThreads) decode_attn_evict_move_kernel(const EvictParams p)
 {
-    constexpr int LT = D / 4;                                 // lanes of a token: 16-byte chunks of its K row, then of its V row
-    constexpr int TP = 32 / LT;                               // tokens a warp moves at a time
     pdl_launch_dependents();
     pdl_wait_primary();
-    const int lane = threadIdx.x & 31;
     // KV heads of one token range next to each other: their rows share the fresh pages
     const int per_row = (p.budget + kMoveTokens - 1) / kMoveTokens;
     const int64_t unit = (int64_t)blockIdx.x * (kMoveThreads / 32) + (threadIdx.x >> 5);
@@ -313,40 +358,7 @@ __global__ void __launch_bounds__(kMoveThreads) decode_attn_evict_move_kernel(co
     const int64_t rest = unit / p.num_kv_heads;
     const int b = (int)(rest / per_row), j0 = (int)(rest % per_row) * kMoveTokens;
     if (b >= p.batch || evict_length(p, b) <= p.budget) return;
-    // lane i: source and destination page of token j0 + i
-    const int j = j0 + lane;
-    int src = 0, src_page = -1, dst_page = -1;
-    if (j < p.budget) {
-        src = __ldcg(p.kept + ((int64_t)b * p.num_kv_heads + g) * p.budget + j);
-        dst_page = __ldg(p.dst_block_table + (int64_t)b * p.dst_max_pages + (j >> p.page_shift));
-        src_page = __ldg(p.block_table + (int64_t)b * p.max_pages_per_seq + (src >> p.page_shift));
-        if ((unsigned)src_page >= (unsigned)p.num_pages || (unsigned)dst_page >= (unsigned)p.num_pages) {
-            if (p.status) record_status(p.status, DA_ERR_BAD_PAGE);   // the row is not moved
-            src_page = dst_page = -1;
-        }
-    }
-    const int mask = (1 << p.page_shift) - 1;
-    const int part = lane % LT, ch = part % (D / 8);          // which row (K, V), which 16 bytes of it
-    const bool is_v = part >= D / 8;
-    __nv_bfloat16* const pool = (is_v ? p.v : p.k) + (int64_t)g * (is_v ? p.v_stride_head : p.k_stride_head) + ch * 8;
-    const int64_t sp = is_v ? p.v_stride_page : p.k_stride_page, st = is_v ? p.v_stride_token : p.k_stride_token;
-#pragma unroll
-    for (int i0 = 0; i0 < kMoveTokens; i0 += TP * kMoveUnroll) {
-        uint4 x[kMoveUnroll];
-        int to_page[kMoveUnroll];
-#pragma unroll
-        for (int u = 0; u < kMoveUnroll; ++u) {
-            const int i = i0 + u * TP + lane / LT;
-            const int from = __shfl_sync(0xffffffffu, src_page, i), slot = __shfl_sync(0xffffffffu, src, i) & mask;
-            to_page[u] = __shfl_sync(0xffffffffu, dst_page, i);
-            if (from >= 0) x[u] = __ldcs(reinterpret_cast<const uint4*>(pool + from * sp + slot * st));
-        }
-#pragma unroll
-        for (int u = 0; u < kMoveUnroll; ++u) {
-            const int i = i0 + u * TP + lane / LT;
-            if (to_page[u] >= 0) *reinterpret_cast<uint4*>(pool + to_page[u] * sp + ((j0 + i) & mask) * st) = x[u];
-        }
-    }
+    move_tokens<D>(p, b, g, j0, threadIdx.x & 31);
 }
 
 }  // namespace da

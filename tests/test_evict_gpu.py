@@ -91,11 +91,12 @@ def check(w, dst, budget, sinks, recent, t, in_place):
 @pytest.mark.parametrize("budget,sinks,recent", [(128, 4, 32), (1, 0, 0), (1, 1, 0), (1, 0, 1), (129, 0, 0), (128, 64, 64),
                                                  (300, 37, 0), (999, 4, 500)])
 def test_what_stays(kind, budget, sinks, recent):
-    w = workload(LENS, budget, 8, 2, 64)
-    t = totals(kind, (len(LENS), 2, max(LENS) + 5), seed=budget)
-    dst = fresh_pages(w, budget)
-    for in_place in (False, True):
-        check(w, dst, budget, sinks, recent, t, in_place)
+    for lens in (LENS, LENS[:-1]):                            # large blocks and a launch of its own for the moves; small ones that move
+        w = workload(lens, budget, 8, 2, 64)
+        t = totals(kind, (len(lens), 2, max(lens) + 5), seed=budget)
+        dst = fresh_pages(w, budget)
+        for in_place in (False, True):
+            check(w, dst, budget, sinks, recent, t, in_place)
 
 
 @pytest.mark.parametrize("layout", ["token_major", "head_major"])
