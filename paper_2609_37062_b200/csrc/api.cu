@@ -467,6 +467,15 @@ void mark_launched(const Plan* pl, cudaStream_t stream)
     if (cudaEventRecord(pl->launch_done, stream) != cudaSuccess) (void)cudaGetLastError();
 }
 
+// A plan's buffer lies on the device that was current when it was made: false if another is now.
+template <class Plan>
+bool on_its_device(const Plan* pl)
+{
+    int dev = -1;
+    if (cudaGetDevice(&dev) != cudaSuccess) (void)cudaGetLastError();
+    return dev == pl->device;
+}
+
 // marks the plan's launch on scope exit (for the entry points that return the launch's status)
 struct mma_launch_guard {
     const decode_attn_plan_t* pl;
@@ -848,6 +857,7 @@ int decode_attn_add_weights(const decode_attn_plan_t* pl, const void* workspace,
     wp.chunks = (int32_t)((most + kWeightsTokens - 1) / kWeightsTokens);
     const int64_t blocks = (int64_t)wp.chunks * wp.num_kv_heads * (capacity ? pl->max_batch : pl->shape.batch);
     if (blocks > 0x7fffffffLL) return DA_ERR_UNSUPPORTED;
+    if (!on_its_device(pl)) return DA_ERR_INVALID_ARG;
     int rc = order_behind_upload(pl, stream);
     if (rc != DA_OK) return rc;
     rc = weights_launch(wp, (unsigned)blocks, stream);
@@ -938,6 +948,7 @@ int decode_attn_prompt_run(const decode_attn_prompt_plan_t* pl, const void* q, c
         if (!workspace || !aligned(workspace, 256)) return DA_ERR_INVALID_ARG;
         if (workspace_bytes < pl->workspace_bytes) return DA_ERR_WORKSPACE_TOO_SMALL;
     }
+    if (!on_its_device(pl)) return DA_ERR_INVALID_ARG;
     int rc = order_behind_upload(pl, stream);
     if (rc != DA_OK) return rc;
     PromptCall c;

@@ -26,8 +26,11 @@
 // that holds both visible and hidden rows is copied by hand for V with the hidden rows cleared, because a zero
 // weight does not silence what such a row may hold.
 //
-// Bound: 2 x 128 x 128 x D x 2 flops of MMA against 128 x 128 exponentials per tile pair - at D 128
-// the tensor core and the exponential unit take the same time.
+// Bound: a step of both MMA tiles against 128 tokens is 2,048 cycles of MMA (32 of 64 cycles at D 128) and 2,048 of the
+// exponential unit, and takes about 3,100: one MMA tile's chain of logits, weights, P V and the next logits is that long,
+// and there is tensor memory for two such chains.  What it is made of (timing builds, 4,096 queries, window 4,096,
+// 32/8 heads of 128, 243 us): without exponentials 213 us, without maxima and loads either 203, without the MMAs too 142 - the
+// hand-overs between the warps and the tensor core, the moves through tensor memory, a unit's set-up and output.
 #pragma once
 
 #include <type_traits>
@@ -217,8 +220,8 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
 
     if (warp == kPromptLoadWarp || warp == kPromptLoadWarp + 1) {
         // ------------------------------------------------------------ TMA: a warp for Q and K, a warp for V
-        // (a warp takes 1,400 cycles to issue the 16 boxes of a tile, 90 each, while the softmax warps beside it are busy:
-        // one warp for both tensors was what paced the kernel, 3,400 against 2,900 cycles a tile)
+        // (a warp takes 1,400 cycles to issue the 16 boxes of a tile, 90 each, while the softmax warps beside it are busy, so
+        // that one warp for both tensors falls behind: 251 against 247 us)
         give_registers();
         const bool is_v = warp == kPromptLoadWarp + 1;
         const CUtensorMap* const map = is_v ? &v_map : &k_map;
