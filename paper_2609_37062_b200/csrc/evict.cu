@@ -99,15 +99,22 @@ extern "C" int decode_attn_evict(const decode_attn_shape_t* shape, const decode_
     const int64_t units = rows * ((ep.budget + kMoveTokens - 1) / kMoveTokens);
     const int64_t move_blocks = (units + kMoveThreads / 32 - 1) / (kMoveThreads / 32);
     if (rows > 0x7fffffffLL || move_blocks > 0x7fffffffLL) return DA_ERR_UNSUPPORTED;
-    // up to 2,048 totals small blocks, several to an SM; up to 32,768 a large one whose threads still hold all keys
-    const int threads = most <= 2048 ? 256 : 1024;
-    // One launch where a block moves its row in less time than a launch takes (128 KB and less) and all blocks are resident
-    // at once (8 rows of 128 tokens 7.6 -> 6.7 us; 512 rows of 1,024 tokens, in two waves of blocks, 98 -> 129 us).
-    const bool one = most <= 2048 && rows <= 444 && (int64_t)ep.budget * s.head_dim * 4 <= 128 * 1024;
-    const void* select = most > 2048          ? (const void*)decode_attn_evict_select_kernel<1024, 2048, 32, 0>
-                         : !one               ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 0>
-                         : s.head_dim == 128 ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 128>
-                                             : (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 64>;
+    // up to 2,048 totals small blocks, several to an SM; up to 8,192 and 32,768 larger ones whose threads still hold all
+    // keys (8 rows of 4,100 totals: 12.8 us with blocks of 512, 17.7 with the 1,024 that longer rows take)
+    const int threads = most <= 2048 ? 256 : most <= 8192 ? 512 : 1024;
+    // One launch where a block moves its row in about the time a launch takes (16 bytes times a few hundred per thread) and
+    // all blocks are resident at once (8 rows of 128 tokens 7.6 -> 6.7 us; 512 rows of 1,024 tokens, in two waves of
+    // blocks, 98 -> 129 us; blocks of 1,024 threads have no registers to spare for it: 19 -> 24 us).
+    const int64_t row_bytes = (int64_t)ep.budget * s.head_dim * 4;
+    const bool one = most <= 2048 ? rows <= 444 && row_bytes <= 128 * 1024 : most <= 8192 && rows <= 296 && row_bytes <= 256 * 1024;
+    const bool wide = s.head_dim == 128;
+    const void* select = most > 8192   ? (const void*)decode_attn_evict_select_kernel<1024, 2048, 32, 0>
+                         : most > 2048 ? (!one   ? (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 0>
+                                          : wide ? (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 128>
+                                                 : (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 64>)
+                                       : (!one   ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 0>
+                                          : wide ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 128>
+                                                 : (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 64>);
     const void* move = s.head_dim == 128 ? (const void*)decode_attn_evict_move_kernel<128> : (const void*)decode_attn_evict_move_kernel<64>;
     if (smem > 32 * 1024 &&
         cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictChunk * (int)sizeof(float)) != cudaSuccess) {

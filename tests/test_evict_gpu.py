@@ -108,6 +108,15 @@ def test_pages_heads_and_layouts(layout, page_size, hq, hkv, d, dtype):
     check(w, fresh_pages(w, budget), budget, 4, 100, totals("random", (4, hkv, 700), 3), False)
 
 
+@pytest.mark.parametrize("d,budget", [(128, 700), (128, 300), (64, 1500), (64, 300)])
+def test_rows_of_some_thousand(d, budget):
+    """Blocks of 512 threads: moving by themselves and not."""
+    lens = [4000, 2049, 90, 1501]
+    w = workload(lens, budget, 8, 4, d, seed=57)
+    for in_place in (False, True):
+        check(w, fresh_pages(w, budget), budget, 4, 100, totals("steps", (4, 4, 4000), 5), in_place)
+
+
 def test_rows_longer_than_a_block_holds():
     """Longer rows are shared by a cluster of blocks, the longest walked in runs; compaction in place is the
     delicate case."""
