@@ -423,7 +423,11 @@ int decode_attn_prompt_plan_destroy(decode_attn_prompt_plan_t *plan);
  *   lse_or_null  device, fp32 [new tokens, num_q_heads] or NULL
  *   workspace    device, >= workspace_bytes from the plan, 256-byte aligned (may be NULL if 0)
  * Weights are rounded once to the 16-bit input type ahead of the product with V;
- * sums, maxima and accumulators are fp32. */
+ * sums, maxima and accumulators are fp32.  What no query of the call may see
+ * (slots behind the end or before every window, pages without a visible
+ * position) can hold anything; a position that one query sees is multiplied with
+ * a weight of zero for its neighbours that do not, so K and V of visible positions
+ * have to be finite. */
 int decode_attn_prompt_run(const decode_attn_prompt_plan_t *plan, const void *q, const void *k_cache, const void *v_cache,
                            const int32_t *block_table, const int32_t *seq_lens, void *out, float *lse_or_null,
                            void *workspace, size_t workspace_bytes, cudaStream_t stream);

@@ -485,9 +485,12 @@ def decode_attn_evict(shape: Shape, budget_tokens: int, sink_tokens: int, recent
     if weights_out is None:
         weights_out = weights
     strides, tokens = _weights_layout(shape, weights, weights_out, "decode_attn_evict")
-    if kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous():
+    pages, (row_stride, page_stride) = dst_block_table.shape[1], dst_block_table.stride()
+    if kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous() or \
+            seq_lens_out.numel() < shape.batch or dst_block_table.shape[0] < shape.batch or page_stride != 1 or \
+            pages * shape.page_size < budget_tokens:
         raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_evict")
-    a = _evict_args(budget_tokens, sink_tokens, recent_tokens, dst_block_table.shape[1])
+    a = _evict_args(budget_tokens, sink_tokens, recent_tokens, max(pages, row_stride))     # (columns of a wider table will do)
     a.seq_lens, a.block_table, a.dst_block_table = _ptr(seq_lens), _ptr(block_table), _ptr(dst_block_table)
     a.k_cache, a.v_cache = _ptr(k_cache), _ptr(v_cache)
     a.weights, a.weights_out = _ptr(weights), _ptr(weights_out)

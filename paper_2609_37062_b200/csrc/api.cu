@@ -826,7 +826,8 @@ int decode_attn_add_weights(const decode_attn_plan_t* pl, const void* workspace,
     if (!pl->policy.track_weights) return DA_ERR_UNSUPPORTED;
     int32_t longest = 0;
     for (int32_t n : pl->seq_lens) longest = std::max(longest, n);
-    if (pl->shape.batch == 0 || longest == 0) return DA_OK;
+    // (a capacity plan's launch may be captured now and replayed for other lengths)
+    if (longest == 0 && pl->policy.capacity_batch == 0) return DA_OK;
     if (!workspace || !lse || !seq_lens || !weights || !weights_out) return DA_ERR_INVALID_ARG;
     if (!aligned(workspace, 256) || !aligned(lse, 4) || !aligned(seq_lens, 4) || !aligned(weights, 4) || !aligned(weights_out, 4))
         return DA_ERR_INVALID_ARG;

@@ -529,7 +529,7 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
             const bool rec = done.slot >= 0;
             const int to = !valid ? -1 : rec ? x * kPromptRows + r : (x * TQ + tok) * p.num_q_heads + h;
             const float scale = rec ? 1.f : 1.f / l;
-            const bool none = !(l > 0.f);                                      // (of a piece: no tile of it is seen by this row)
+            const bool none = l == 0.f;                                      // (of a piece: no tile of it is seen by this row)
             float* const recs = p.ws + (int64_t)(rec ? done.slot : 0) * (kPromptTiles * kPromptRows * (D + 2));
             const int64_t row0 = (int64_t)done.row * p.num_q_heads + done.kv_head * G;
             const int kind = rec ? 0 : p.out_kind;                             // 0: fp32, 32 columns are 128 bytes; else 64 columns
@@ -584,7 +584,7 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                 if (rec)
                     __stcg(reinterpret_cast<float2*>(recs + kPromptTiles * kPromptRows * D) + x * kPromptRows + r, make_float2(m, l));
                 else if (p.lse != nullptr)
-                    p.lse[row0 + to] = l > 0.f ? (m + log2f(l)) * kLn2 : -INFINITY;
+                    p.lse[row0 + to] = none ? -INFINITY : (m + log2f(l)) * kLn2;
             }
         }
     } else {
@@ -622,23 +622,21 @@ __global__ void __launch_bounds__(256) decode_attn_prompt_merge_kernel(const Pro
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     float ls = 0.f;
     auto add = [&](const float2& s, const float4& v) {
-        const float w = ex2f(s.x - M);
+        const float w = M == -INFINITY ? 1.f : ex2f(s.x - M);     // nothing seen: zeros; no number in q: none in the sum
         acc.x = fmaf(w, v.x, acc.x);
         acc.y = fmaf(w, v.y, acc.y);
         acc.z = fmaf(w, v.z, acc.z);
         acc.w = fmaf(w, v.w, acc.w);
         ls = fmaf(w, s.y, ls);
     };
-    if (M != -INFINITY) {
-        add(s0, v0);
-        add(s1, v1);
-        for (int k = 2; k < u.n_pieces; ++k) add(__ldcg(ml + k * (RF / 2)), __ldcg(col + k * (RF / 4)));
-    }
-    const float inv = ls > 0.f ? 1.f / ls : 0.f;
+    add(s0, v0);
+    add(s1, v1);
+    for (int k = 2; k < u.n_pieces; ++k) add(__ldcg(ml + k * (RF / 2)), __ldcg(col + k * (RF / 4)));
+    const float inv = ls == 0.f ? 0.f : 1.f / ls;
     acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
     const int64_t orow = (int64_t)(u.row + x * p.tokens_per_tile + tok) * p.num_q_heads + u.kv_head * p.group + h;
     store_out4(p.out, orow * D + d4 * 4, acc, p.out_kind);
-    if (p.lse != nullptr && d4 == 0) p.lse[orow] = ls > 0.f ? (M + log2f(ls)) * kLn2 : -INFINITY;
+    if (p.lse != nullptr && d4 == 0) p.lse[orow] = ls == 0.f ? -INFINITY : (M + log2f(ls)) * kLn2;
 }
 
 }  // namespace da

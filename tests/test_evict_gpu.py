@@ -213,6 +213,30 @@ def test_a_bounded_generation():
             assert (out[b, g * 4].cpu().double() - o).abs().max() < 2e-3
 
 
+def test_destination_tables_that_are_columns_of_wider_ones():
+    lens, budget = [300, 400], 128
+    w = workload(lens, budget, 8, 2, 64, seed=58)
+    wd, dst = to_device(w), fresh_pages(w, budget)
+    wide = torch.full((2, 20), -1, dtype=torch.int32, device="cuda")
+    wide[:, :8] = dst.cuda()
+    t = totals("random", (2, 2, 400), 8).cuda()
+    out = []
+    for table in (dst.cuda(), wide[:, :8], wide):
+        x = to_device(w)
+        kept = torch.zeros((2, 2, budget), dtype=torch.int32, device="cuda")
+        lens_out = torch.zeros(2, dtype=torch.int32, device="cuda")
+        da.decode_attn_evict(da.shape_of_workload(x), budget, 4, 32, x.seq_lens, x.block_table, table, x.k_pool, x.v_pool, t,
+                             torch.zeros_like(t), kept, lens_out)
+        out.append((x.k_pool, x.v_pool, kept))
+    for o in out[1:]:
+        assert all(torch.equal(a, b) for a, b in zip(o, out[0]))
+    kept = torch.zeros((2, 2, budget), dtype=torch.int32, device="cuda")
+    for table in (dst[:, :7].cuda(), wide.t().contiguous().t()):               # too few pages; pages not next to each other
+        with pytest.raises(da.DecodeAttnError):
+            da.decode_attn_evict(da.shape_of_workload(wd), budget, 4, 32, wd.seq_lens, wd.block_table, table, wd.k_pool, wd.v_pool, t,
+                                 torch.zeros_like(t), kept, torch.zeros(2, dtype=torch.int32, device="cuda"))
+
+
 def test_captured_and_replayed():
     lens, budget = [300, 400, 50], 128
     w = workload(lens, budget, 8, 2, 64, seed=56)

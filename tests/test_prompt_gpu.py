@@ -176,6 +176,32 @@ def test_growing_keys_rescale_every_tile():
     compare(out, lse, w, new, 0, 0)
 
 
+def test_nan_in_a_query_stays_in_its_row():
+    """A query that is not a number makes its own row none and no other."""
+    for new, cached in (([70], [2000]), ([70], [10])):            # cut units and whole ones
+        w = prompt("pq", new, cached, 8, 2, 128, 100)
+        good = Prompt(to_device(w), new, da.make_policy())
+        good()
+        q = w.q_bits.clone()
+        q[33, 5, 7] = 0x7FC0
+        bad = Prompt(to_device(dataclasses.replace(w, q_bits=q)), new, da.make_policy())
+        bad()
+        bad.ok()
+        assert torch.isnan(bad.out[33, 5]).all() and torch.isnan(bad.lse[33, 5])
+        bad.out[33, 5], bad.lse[33, 5] = good.out[33, 5], good.lse[33, 5]
+        assert torch.equal(bad.out, good.out) and torch.equal(bad.lse, good.lse)
+
+
+def test_many_sequences_of_one_token():
+    new = [1] * 300
+    cached = [(7 * i) % 90 for i in range(300)]
+    w = prompt("pm", new, cached, 8, 2, 64, 101)
+    p = Prompt(to_device(w), new, da.make_policy(window_tokens=40, sink_tokens=3))
+    p()
+    p.ok()
+    compare(p.out, p.lse, w, new, 40, 3)
+
+
 def test_capture_and_replay():
     new, cached, window, sinks = [100, 3], [900, 50], 256, 4
     w = prompt("pr", new, cached, 32, 8, 128, 95)

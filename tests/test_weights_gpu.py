@@ -128,6 +128,25 @@ def test_capacity_plan_and_graph():
         assert torch.equal(before[n:], t[n:])
 
 
+def test_a_graph_captured_while_nothing_is_live():
+    """A capacity plan captured with no rows, then with rows of length 0, counts what it is refreshed for."""
+    w = wl.make_workload("wtz", [300, 200], 8, 2, 64, seed=47)
+    for first in ([], [0, 0]):
+        wd = to_device(w)
+        s = Step(wd, da.make_policy(track_weights=1, capacity_batch=2, capacity_tokens=600))
+        t = torch.zeros((2, 2, 320), device="cuda")
+        da.decode_attn_plan_update(s.plan, first)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            s()
+            da.decode_attn_add_weights(s.plan, s.ws, s.lse, wd.seq_lens, t)
+        da.decode_attn_plan_update(s.plan, [300, 200])
+        graph.replay()
+        s.ok()
+        check(torch.zeros_like(t), t, oracle_out(w)[2], [300, 200])
+
+
 def test_refusals():
     wd = to_device(wl.make_workload("wtr", [100, 200], 8, 2, 64, seed=46))
     s = Step(wd, da.make_policy(track_weights=1))
