@@ -9,7 +9,7 @@
 //   S_x = Q_x K_j^T       128 x 128 x D, accumulator in tensor-memory columns [128 x, 128 x + 128)
 //   softmax               one thread per row: the row's maximum, p = 2^(s * scale * log2 e - m), the row sum;
 //                         p as two 16-bit values per column back over the logits.  p is rounded once to the 16-bit
-//                         input type (the MMA takes no mixed types); its relative error, 2^-9 in bf16 and 2^-12
+//                         input type (the MMA takes no mixed types); its relative error, at most 2^-8 in bf16 and 2^-11
 //                         in fp16, averages out over the tokens, and the row sum is of the unrounded p.
 //   O_x += P_x V_j        accumulator in columns [256 + 128 x, 256 + 128 x + D), kept over all tiles
 //
