@@ -98,7 +98,8 @@ typedef struct {
     int32_t capacity_batch; /* > 0: the plan can be refreshed in place for any batch <= this value
                                (decode_attn_plan_update) and launches a fixed grid whose surplus
                                blocks exit at once (Algorithm 1 step 6, "grid exit")                  */
-    int32_t capacity_tokens;/* with capacity_batch: upper bound on sum(seq_lens) of any refresh      */
+    int32_t capacity_tokens;/* with capacity_batch: upper bound on sum(seq_lens) of any refresh (with
+                               track_weights also of the lengths the plan is made with)              */
     int32_t ctas_per_sm;    /* 0: from the occupancy of the chosen kernel                            */
     int32_t shared_prefix_tokens; /* > 0: the caller promises that the first this-many tokens of every
                                sequence live in the same physical pages (the block-table rows agree on

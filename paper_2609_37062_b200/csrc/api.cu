@@ -496,6 +496,13 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
     if (rc != DA_OK) return rc;
     rc = validate_policy(*shape, *policy);
     if (rc != DA_OK) return rc;
+    if (policy->track_weights && policy->capacity_batch > 0) {
+        // The room for logits is what capacity_tokens pays for, whatever the first lengths are.  (Without logits
+        // only units and records have to fit, which is checked below.)
+        int64_t total = 0;
+        for (int b = 0; b < shape->batch; ++b) total += seq_lens_host[b];
+        if (total > policy->capacity_tokens) return DA_ERR_INVALID_ARG;
+    }
 
     decode_attn_plan_t* pl = new (std::nothrow) decode_attn_plan_t();
     if (!pl) return DA_ERR_INVALID_ARG;
