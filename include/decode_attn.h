@@ -482,7 +482,11 @@ int decode_attn_add_weights(const decode_attn_plan_t *plan, const void *workspac
  * are read on the device).  A row whose length does not fit the block table
  * or the totals is left alone (DA_ERR_STALE_PLAN), a token whose page id lies
  * outside the pool is not moved (DA_ERR_BAD_PAGE); either is recorded in
- * `status` when one is given. */
+ * `status` when one is given.  Totals must not change while the call runs (no
+ * writer on another stream, no overlapping rows): the rows of more than 49,152
+ * totals are read several times, and where the readings do not fit together
+ * the (sequence, KV head) is given up - `kept` is -1 throughout, nothing of it
+ * is moved, its totals hold no valid values, DA_ERR_STALE_PLAN is recorded. */
 typedef struct {
     uint32_t struct_size;       /* sizeof(decode_attn_evict_args_t) */
     uint32_t flags;             /* must be 0 */

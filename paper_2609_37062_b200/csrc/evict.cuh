@@ -29,6 +29,7 @@ constexpr int kEvictChunk = 48 * 1024;             // totals a block holds in sh
 constexpr int kMoveThreads = 256;
 constexpr int kMoveTokens = 32;                    // of one (sequence, KV head) per warp
 constexpr int kMoveUnroll = 8;                     // 16-byte loads a lane keeps in flight
+constexpr int kEvictPasses = 4;                    // 32 bits of key in passes of 10 (three would do for 11)
 
 struct EvictParams {
     const int32_t* seq_lens;
@@ -80,11 +81,13 @@ __device__ __forceinline__ void move_tokens(const EvictParams& p, int b, int g, 
     int src = 0, src_page = -1, dst_page = -1;
     if (j < p.budget) {
         src = __ldcg(p.kept + ((int64_t)b * p.num_kv_heads + g) * p.budget + j);
-        dst_page = __ldg(p.dst_block_table + (int64_t)b * p.dst_max_pages + (j >> p.page_shift));
-        src_page = __ldg(p.block_table + (int64_t)b * p.max_pages_per_seq + (src >> p.page_shift));
-        if ((unsigned)src_page >= (unsigned)p.num_pages || (unsigned)dst_page >= (unsigned)p.num_pages) {
-            if (p.status) record_status(p.status, DA_ERR_BAD_PAGE);   // the row is not moved
-            src_page = dst_page = -1;
+        if (src >= 0) {                                       // (-1: select gave the row up, and has said so)
+            dst_page = __ldg(p.dst_block_table + (int64_t)b * p.dst_max_pages + (j >> p.page_shift));
+            src_page = __ldg(p.block_table + (int64_t)b * p.max_pages_per_seq + (src >> p.page_shift));
+            if ((unsigned)src_page >= (unsigned)p.num_pages || (unsigned)dst_page >= (unsigned)p.num_pages) {
+                if (p.status) record_status(p.status, DA_ERR_BAD_PAGE);   // the row is not moved
+                src_page = dst_page = -1;
+            }
         }
     }
     const int mask = (1 << p.page_shift) - 1;
@@ -201,6 +204,10 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
     // one key wide or all of it stays.  (Keys are the floats' bits, so totals that spread over powers of two spread
     // over the bins; three passes at most, as a rule.)
     int k = p.budget - p.sinks - p.recent;
+    // A row of more than one run is read anew by every pass.  Should its totals change meanwhile (they must not),
+    // the counts no longer fit together: no bin holds rank k, or the range is not down to one key after as many passes
+    // as 32 bits take.  The row is then given up, see below.
+    bool lost = false;
     uint32_t key = kKeyStays - 1;                             // k = 0: above every float's
     int ties = 0;
     if (k > 0) {
@@ -218,10 +225,14 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
             most = (uint32_t)sm_warp[lane].y;
         }
         uint32_t lo = __reduce_min_sync(0xffffffffu, least), hi = __reduce_max_sync(0xffffffffu, most) + 1;
-        while (true) {
+        for (int pass = 0;; ++pass) {
             if (hi - lo == 1) {
                 key = lo;
                 ties = k;
+                break;
+            }
+            if (pass == kEvictPasses) {
+                lost = true;
                 break;
             }
             const int bits = 32 - __clz((int)(hi - lo - 1));
@@ -230,6 +241,7 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
             const int shift = max(0, bits - LOG_BINS);
             for (int i = tid; i < BINS; i += NT) sm_hist[i] = 0;
             __syncthreads();
+            if (tid == 0) sm_found[0] = -1;
             each_key([&](uint32_t x) {
                 // Where totals are equal (all of them zero, at worst) the lanes meet in one bin: the first lane's is
                 // counted once for all that share it, the rest one by one.
@@ -266,6 +278,10 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
                 before += c[i];
             }
             __syncthreads();
+            if (sm_found[0] < 0) {
+                lost = true;
+                break;
+            }
             lo += (uint32_t)sm_found[0] << shift;
             k -= sm_found[1];
             if (k == sm_found[2]) {                           // all of the bin stays
@@ -278,7 +294,7 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
 
     // ---- positions and totals of what stays, in order
     int at = 0, equal = 0;                                    // kept, equals met: in the runs before
-    for (int r0 = 0; r0 < L; r0 += run) {
+    for (int r0 = 0; r0 < L && !lost; r0 += run) {
         __syncthreads();                                      // sm_warp, sm_w are free
         if (!whole) {
             load(r0);
@@ -322,8 +338,8 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
                 my_eq += __popc(mask_eq);
             }
             const uint32_t mask = __ballot_sync(0xffffffffu, stay);
-            if (stay) {
-                const int to = to0 + __popc(mask & lower);
+            const int to = to0 + __popc(mask & lower);
+            if (stay && to < p.budget) {                      // (always, of totals that stood still)
                 kept[to] = r0 + i;
                 o[to] = sm_w[i];
             }
@@ -338,6 +354,12 @@ __global__ void __launch_bounds__(NT) decode_attn_evict_select_kernel(const Evic
         }
         at += run_gt + min(equal + run_eq, ties) - min(equal, ties);
         equal += run_eq;
+    }
+    if (lost || at != p.budget) {                             // given up: no position stays, no row moves, reported
+        __syncthreads();
+        for (int i = tid; i < p.budget; i += NT) kept[i] = -1;
+        if (tid == 0 && p.status) record_status(p.status, DA_ERR_STALE_PLAN);
+        return;
     }
     for (int t = p.budget + tid; t < L; t += NT) o[t] = 0.f;      // tokens to come start from nothing
     if (D != 0) {
