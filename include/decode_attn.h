@@ -451,8 +451,11 @@ int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan,
  *   weights, weights_out  device, fp32; the row of (b, g) starts at
  *                b * stride_seq + g * stride_head and holds `tokens` values, at
  *                least the longest sequence (of a capacity plan: the longest it
- *                can hold); both strides are at least `tokens`.  The two may be
- *                the same buffer, and must not overlap otherwise.
+ *                can hold).  Rows must not overlap (DA_ERR_INVALID_ARG; the
+ *                batch of a capacity plan is its capacity_batch), in whichever
+ *                order they lie; the stride of a batch of one, or of a single
+ *                KV head, is not looked at.  The two may be the same buffer,
+ *                and must not overlap otherwise.
  * A log-sum-exp of magnitude x carries an fp32 rounding of about 6e-8 x, and
  * the weights that relative error.  One launch on `stream`, nothing is allocated,
  * capture-safe. */
@@ -500,7 +503,8 @@ typedef struct {
     void *k_cache;                      /* device pools of the shape, 16-byte aligned, modified */
     void *v_cache;
     const float *weights;       /* device, fp32 totals; the row of (b, g) starts at b * stride_seq + g * stride_head
-                                   and holds weight_tokens values, at least the longest sequence */
+                                   and holds weight_tokens values, at least the longest sequence; rows must not
+                                   overlap (as for decode_attn_add_weights) */
     float *weights_out;         /* device, laid out the same: the totals of what stays, then zeros up to the old
                                    length; may be `weights`, must not overlap it otherwise */
     int64_t weight_tokens, stride_seq, stride_head;

@@ -838,8 +838,8 @@ int decode_attn_add_weights(const decode_attn_plan_t* pl, const void* workspace,
     if (!workspace || !lse || !seq_lens || !weights || !weights_out) return DA_ERR_INVALID_ARG;
     if (!aligned(workspace, 256) || !aligned(lse, 4) || !aligned(seq_lens, 4) || !aligned(weights, 4) || !aligned(weights_out, 4))
         return DA_ERR_INVALID_ARG;
-    // rows of different sequences and KV heads must not overlap
-    if (tokens < longest || stride_seq < tokens || stride_head < tokens) return DA_ERR_INVALID_ARG;
+    if (tokens < longest || !totals_apart(tokens, stride_seq, stride_head, pl->max_batch, pl->shape.num_kv_heads))
+        return DA_ERR_INVALID_ARG;
     WeightsParams wp;
     wp.logits = reinterpret_cast<const float*>(static_cast<const char*>(workspace) + pl->off_logits);
     wp.lse = lse;

@@ -62,7 +62,8 @@ extern "C" int decode_attn_evict(const decode_attn_shape_t* shape, const decode_
         !aligned(a->seq_lens_out, 4) || !aligned(a->status, 4))
         return DA_ERR_INVALID_ARG;
     if (a->seq_lens_out == a->seq_lens) return DA_ERR_INVALID_ARG;   // the blocks of one row would see its new length
-    if (a->weight_tokens < 1 || a->stride_seq < a->weight_tokens || a->stride_head < a->weight_tokens) return DA_ERR_INVALID_ARG;
+    if (a->weight_tokens < 1 || !totals_apart(a->weight_tokens, a->stride_seq, a->stride_head, s.batch, s.num_kv_heads))
+        return DA_ERR_INVALID_ARG;
 
     EvictParams ep;
     ep.seq_lens = a->seq_lens;

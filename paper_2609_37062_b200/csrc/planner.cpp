@@ -60,6 +60,23 @@ int validate_shape(const decode_attn_shape_t& s)
     return DA_OK;
 }
 
+bool totals_apart(int64_t tokens, int64_t stride_seq, int64_t stride_head, int64_t batch, int64_t num_kv_heads)
+{
+    if ((batch > 1 && stride_seq < tokens) || (num_kv_heads > 1 && stride_head < tokens)) return false;
+    if (batch <= 1 || num_kv_heads <= 1) return true;
+    // Rows (b, g) and (b - db, g + dg) are dg * stride_head - db * stride_seq apart: for every dg the two db that bring
+    // them closest.  (The usual layouts, one stride beyond all rows of the other, need no search.)
+    const __int128 ss = stride_seq, sh = stride_head;
+    if (ss >= (num_kv_heads - 1) * sh + tokens || sh >= (batch - 1) * ss + tokens) return true;
+    for (int64_t dg = 1; dg < num_kv_heads; ++dg)
+        for (int next = 0; next < 2; ++next) {
+            const __int128 db = std::min<__int128>(batch - 1, std::max<__int128>(1, dg * sh / ss + next));
+            const __int128 gap = dg * sh - db * ss;
+            if (gap < tokens && -gap < tokens) return false;
+        }
+    return true;
+}
+
 int validate_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
 {
     if (p.split_mode < DA_SPLIT_AUTO || p.split_mode > DA_SPLIT_DETERMINISTIC) return DA_ERR_INVALID_ARG;

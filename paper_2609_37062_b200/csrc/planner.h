@@ -44,6 +44,9 @@ struct Layout {
 
 // Validates the fields the planner and the kernels rely on.
 int validate_shape(const decode_attn_shape_t& s);
+// Do the rows of totals of different sequences and KV heads lie apart?  Row (b, g) is the `tokens` values from
+// b * stride_seq + g * stride_head on; the stride of a single sequence, or of a single head, does not matter.
+bool totals_apart(int64_t tokens, int64_t stride_seq, int64_t stride_head, int64_t batch, int64_t num_kv_heads);
 int validate_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p);
 
 // Fills `out` for the given lengths.  sm_count and ctas_per_sm must be > 0.

@@ -66,3 +66,48 @@ def test_calls_are_refused_before_they_reach_a_device():
         setattr(a, name, bad)
         assert call() == da.DA_ERR_INVALID_ARG, name
         setattr(a, name, good)
+
+
+def layout_status(T, stride_seq, stride_head, batch=1 << 30, heads=2):
+    """What the call says to rows of totals laid out like this.  Of some 2^31 rows with budgets of 512 tokens, more than a
+    launch takes: a layout that is accepted is answered with DA_ERR_UNSUPPORTED, before any device is asked."""
+    import ctypes
+    sh = da.make_shape(batch, heads, heads, 64, 16, 8, 32, (16 * heads * 64, heads * 64, 64))
+    a = da._evict_args(512, 4, 8, 32)
+    for i, name in enumerate(("seq_lens", "block_table", "dst_block_table", "k_cache", "v_cache", "weights", "weights_out", "kept",
+                              "seq_lens_out")):
+        setattr(a, name, (i + 1) << 20)
+    a.weight_tokens, a.stride_seq, a.stride_head = T, stride_seq, stride_head
+    assert batch * heads * (512 // 32) // 8 > 2**31 - 1
+    return da._lib.decode_attn_evict(ctypes.byref(sh), ctypes.byref(a), None)
+
+
+@pytest.mark.parametrize("T", [1, 128, 1000])
+def test_overlapping_rows_of_totals_are_refused(T):
+    B = 1 << 30
+    for stride_seq, stride_head in ((2 * T, T), (3 * T, T), (2 * T + 1, T + 1), (T, B * T), (T + 3, B * (T + 3)),
+                                    (2 * T, 3 * T), (2 * T, 7 * T), (5 * T, 3 * T),
+                                    (2**60, 2**61 + 2**59), (2**62, T)):      # interleaved rows lie apart too
+        assert layout_status(T, stride_seq, stride_head) == da.DA_ERR_UNSUPPORTED, (stride_seq, stride_head)
+    for stride_seq, stride_head in ((T, T), (2 * T, 2 * T), (2 * T, 4 * T), (T, 7 * T), (2 * T - 1, T), (T, (B - 1) * T),
+                                    (2 * T + 2, T - 1), (T - 1, B * T), (0, T), (T, 0), (-2 * T, T), (2**62, 2**62)):
+        assert layout_status(T, stride_seq, stride_head) == da.DA_ERR_INVALID_ARG, (stride_seq, stride_head)
+    # one KV head, or one sequence: its stride does not matter
+    for any_stride in (0, 1, T, -5):
+        assert layout_status(T, T, any_stride, batch=2**31 - 1, heads=1) == da.DA_ERR_UNSUPPORTED
+        assert layout_status(T, any_stride, T, batch=1, heads=2**31 - 1) == da.DA_ERR_UNSUPPORTED
+    assert layout_status(T, T - 1, 0, batch=2**31 - 1, heads=1) == da.DA_ERR_INVALID_ARG
+    assert layout_status(T, 0, T - 1, batch=1, heads=2**31 - 1) == da.DA_ERR_INVALID_ARG
+
+
+def test_rows_lie_apart_exactly_when_no_two_share_a_value():
+    """All small layouts against the definition, through the host-only check that both entry points share."""
+    import itertools
+    T = 3
+    for stride_seq, stride_head, heads in itertools.product(range(1, 22), range(1, 22), (2, 3, 5)):
+        # (a batch so large that a launch refuses it has every row of a smaller one: the definition needs some 2 * heads * 21 / T)
+        rows = np.arange(200)[:, None] * stride_seq + np.arange(heads)[None, :] * stride_head
+        values = (rows.reshape(-1, 1) + np.arange(T)).ravel()
+        apart = len(np.unique(values)) == len(values)
+        got = layout_status(T, stride_seq, stride_head, batch=(1 << 31) // heads + 1, heads=heads)
+        assert got == (da.DA_ERR_UNSUPPORTED if apart else da.DA_ERR_INVALID_ARG), (stride_seq, stride_head, heads)
