@@ -213,194 +213,201 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
     const uint32_t tmem = *sm_tmem;
     pdl_wait_primary();
 
-    // (by role, inside the role's own code: the compiler allocates by what it sees there)
-    auto give_registers = [] { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPromptOtherRegs)); };
     const int G = p.group, TQ = p.tokens_per_tile;
     auto tile_at = [](const PromptUnit& u, int i) { return i < u.sink_tiles ? i : i - u.sink_tiles + u.window_tile; };
 
-    if (warp == kPromptLoadWarp || warp == kPromptLoadWarp + 1) {
-        // ------------------------------------------------------------ TMA: a warp for Q and K, a warp for V
-        // (a warp takes 1,400 cycles to issue the 16 boxes of a tile, 90 each, while the softmax warps beside it are busy, so
-        // that one warp for both tensors falls behind: 251 against 247 us)
-        give_registers();
-        const bool is_v = warp == kPromptLoadWarp + 1;
-        const CUtensorMap* const map = is_v ? &v_map : &k_map;
-        const uint32_t ring = is_v ? v_base : k_base, bar_full = is_v ? bar_vf : bar_kf, bar_empty = is_v ? bar_ve : bar_ke;
-        const uint64_t keep = l2_policy_evict_normal();
-        const int ts = p.tile_shift;
-        const int sub = (lane / Cfg::kHalves) & 7, hf = lane % Cfg::kHalves;    // lane's box: 16 tokens, half of the head dimension
-        constexpr int BOXES = 8 * Cfg::kHalves;
-        int n = 0;                                                              // tiles so far
-        int cu[2] = {0, 0};                                                     // units so far, per MMA tile
-        bool ok = true;
-        for (int ui = ubeg; ui < uend && ok; ++ui) {
-            const PromptUnit u = p.units[ui];
-            const int lo = p.window > 0 ? max(0, u.pos - p.window + 1) : 0;     // what the first query sees through its window
-            const int end = min(u.pos + u.n_tok, u.seq_len);
-            const int32_t* const bt = p.block_table + (int64_t)u.seq * p.max_pages_per_seq;
-            auto seen = [&](int s0) { return s0 < end && (s0 + 15 >= lo || s0 < p.sinks); };
-            auto whole = [&](int s0) { return s0 + 15 < u.seq_len && (s0 >= lo || s0 + 15 < p.sinks); };
-            auto page_of = [&](int i) {                                         // of this lane's 16 tokens in list tile i
-                if (i >= u.tile_end) return (int)p.num_pages;
-                const int s0 = tile_at(u, i) * kPromptKvTokens + sub * 16;
-                return seen(s0) ? __ldg(bt + (s0 >> (ts + 4))) : (int)p.num_pages;
-            };
-            int page = page_of(u.tile_begin);
-            for (int i = u.tile_begin; i < u.tile_end && ok; ++i, ++n) {
-                const int s0 = tile_at(u, i) * kPromptKvTokens + sub * 16;
-                const int next_page = page_of(i + 1);
-                if ((unsigned)page >= (unsigned)p.num_pages && seen(s0)) {
-                    record_status(p.status, DA_ERR_BAD_PAGE);                   // such a box is read as zeros
-                    page = (int)p.num_pages;
-                }
-                const int slot0 = (s0 >> 4 & ((1 << ts) - 1)) << 4;
-                const int st = n % NS;
-                if (n >= NS) ok = prompt_wait(bar_empty + 8 * st, (uint32_t)(n / NS + 1) & 1u, sm_abort);
-                if (!ok) break;
-                // V boxes with rows to clear are copied by hand
-                const bool part = is_v && seen(s0) && !whole(s0);
-                const uint32_t parts = __ballot_sync(0xffffffffu, part && hf == 0 && lane < BOXES);
-                for (uint32_t m = parts; m != 0; m &= m - 1) {
-                    const int from = __ffs(m) - 1;                              // the lane whose box it is
-                    const int pg = __shfl_sync(0xffffffffu, page, from), k0 = __shfl_sync(0xffffffffu, s0, from);
-                    const int sl = __shfl_sync(0xffffffffu, slot0, from), sb = __shfl_sync(0xffffffffu, sub, from);
-                    for (int c = lane; c < 16 * (D / 8); c += 32) {
-                        const int r = c / (D / 8), ch = c % (D / 8), k = k0 + r;
-                        uint4 x = make_uint4(0u, 0u, 0u, 0u);
-                        if (k < u.seq_len && (k >= lo || k < p.sinks) && pg < p.num_pages)
-                            x = __ldg(reinterpret_cast<const uint4*>(p.v + (int64_t)pg * p.v_stride_page + (int64_t)(sl + r) * p.v_stride_token +
-                                                                     (int64_t)u.kv_head * p.v_stride_head) + ch);
-                        *reinterpret_cast<uint4*>(gbase + (v_base - base) + st * Cfg::kTileBytes + (ch >> 3) * Cfg::kHalfBytes +
-                                                  sb * 2048 + swz(r, ch & 7)) = x;
-                    }
-                }
-                if (parts != 0) {
-                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-                    __syncwarp();
-                }
-                if (lane == 0) mbar_arrive_expect_tx(bar_full + 8 * st, Cfg::kTileBytes - __popc(parts) * (16 * D * 2));
-                __syncwarp();
-                if (lane < BOXES && !part)
-                    tma_load_4d(ring + st * Cfg::kTileBytes + hf * Cfg::kHalfBytes + sub * 2048, map, bar_full + 8 * st, hf * 64, slot0,
-                                u.kv_head, page, keep);
-                if (!is_v && i == u.tile_begin) {
-                    // The unit's query rows: TQ tokens x the group's heads, rows of the MMA tile in that order.  (Tokens of
-                    // a ragged end are other rows of q, or zeros behind the last: what comes of them is not stored.)
-                    for (int x = 0; x < (u.n_tok > TQ ? 2 : 1) && ok; ++x) {
-                        if (cu[x] > 0) ok = prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
-                        if (!ok) break;
-                        ++cu[x];
-                        if (lane == 0) {
-                            mbar_arrive_expect_tx(bar_q(x), Cfg::kHalves * G * TQ * 128);
-                            for (int h = 0; h < Cfg::kHalves; ++h)
-                                tma_load_3d(q_base + x * Cfg::kTileBytes + h * Cfg::kHalfBytes, &q_map, bar_q(x), h * 64, u.kv_head * G,
-                                            u.row + x * TQ);
-                        }
-                        __syncwarp();
-                    }
-                }
-                page = next_page;
-            }
-        }
-        if (*sm_abort != 0) {
-            // given up somewhere: nothing may land in shared memory after the block has left (a copy always lands)
-            for (int i = max(0, n - NS); i <= n; ++i)
-                if (i < n || !ok) mbar_wait(bar_full + 8 * (i % NS), (uint32_t)(i / NS) & 1u, i < n ? kWaitLimitCycles : 1000000LL);
-            for (int x = 0; x < 2; ++x)
-                if (cu[x] > 0) mbar_wait(bar_q(x), (uint32_t)(cu[x] - 1) & 1u);
-        }
-    } else if (warp == kPromptMmaWarp) {
-        // ------------------------------------------------------------ MMAs (the warp together, one lane issues)
-        give_registers();
-        {
-            constexpr uint32_t idesc_qk = umma::instr_desc_16(128, 128, false, F16);
-            constexpr uint32_t idesc_pv = umma::instr_desc_16(128, D, true, F16);
-            constexpr uint32_t kTileUnits = Cfg::kTileBytes >> 4, kHalfUnits = Cfg::kHalfBytes >> 4;
-            const uint64_t q_desc = umma::smem_desc_sw128(q_base, 16, 1024);
-            const uint64_t k_desc = umma::smem_desc_sw128(k_base, 16, 1024);
-            const uint64_t v_desc = umma::smem_desc_sw128(v_base, Cfg::kHalfBytes, 1024);
-            int n = 0;                                        // K/V tiles before the unit
-            int cs[2] = {0, 0}, cu[2] = {0, 0};               // per MMA tile: P V issued, units begun
+    // The warp's number as a value known to be the same in all its lanes: branches on it then keep what the roles
+    // share in uniform registers (without: 188 bytes spilled instead of 96, 297 us instead of 284 for 4,096 queries).
+    const int role = __shfl_sync(0xffffffffu, warp, 0);
+    if (role >= kPromptSoftmaxWarps) {
+        // (one instruction for the whole warpgroup, its idle fourth warp included, ahead of the roles; and inside the
+        // branch: the compiler allocates the code behind it by what it sees there)
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPromptOtherRegs));
+        if (role == kPromptLoadWarp || role == kPromptLoadWarp + 1) {
+            // ------------------------------------------------------------ TMA: a warp for Q and K, a warp for V
+            // (a warp takes 1,400 cycles to issue the 16 boxes of a tile, 90 each, while the softmax warps beside it are busy, so
+            // that one warp for both tensors falls behind: 251 against 247 us)
+            const bool is_v = warp == kPromptLoadWarp + 1;
+            const CUtensorMap* const map = is_v ? &v_map : &k_map;
+            const uint32_t ring = is_v ? v_base : k_base, bar_full = is_v ? bar_vf : bar_kf, bar_empty = is_v ? bar_ve : bar_ke;
+            const uint64_t keep = l2_policy_evict_normal();
+            const int ts = p.tile_shift;
+            const int sub = (lane / Cfg::kHalves) & 7, hf = lane % Cfg::kHalves;    // lane's box: 16 tokens, half of the head dimension
+            constexpr int BOXES = 8 * Cfg::kHalves;
+            int n = 0;                                                              // tiles so far
+            int cu[2] = {0, 0};                                                     // units so far, per MMA tile
             bool ok = true;
             for (int ui = ubeg; ui < uend && ok; ++ui) {
                 const PromptUnit u = p.units[ui];
-                const int T = u.tile_end - u.tile_begin;
-                const int X = u.n_tok > TQ ? 2 : 1;
-                auto qk = [&](int x, int j) {
-                    const int st = (n + j) % NS;
-                    umma::fence_after_thread_sync();
-                    const uint64_t qd = q_desc + (uint64_t)(x * kTileUnits), kd = k_desc + (uint64_t)(st * kTileUnits);
-                    if (elect_one()) {
-#pragma unroll
-                        for (int ks = 0; ks < D / 16; ++ks) {
-                            const uint32_t off = (ks >> 2) * kHalfUnits + (ks & 3) * 2;
-                            umma::mma_ss(tmem + x * 128, qd + off, kd + off, idesc_qk, ks > 0);
-                        }
-                        umma::commit(bar_s(x));
-                        if (x == X - 1) umma::commit(bar_ke + 8 * st);
-                        if (j == T - 1) umma::commit(bar_qe(x));
-                    }
-                    __syncwarp();
+                const int lo = p.window > 0 ? max(0, u.pos - p.window + 1) : 0;     // what the first query sees through its window
+                const int end = min(u.pos + u.n_tok, u.seq_len);
+                const int32_t* const bt = p.block_table + (int64_t)u.seq * p.max_pages_per_seq;
+                auto seen = [&](int s0) { return s0 < end && (s0 + 15 >= lo || s0 < p.sinks); };
+                auto whole = [&](int s0) { return s0 + 15 < u.seq_len && (s0 >= lo || s0 + 15 < p.sinks); };
+                auto page_of = [&](int i) {                                         // of this lane's 16 tokens in list tile i
+                    if (i >= u.tile_end) return (int)p.num_pages;
+                    const int s0 = tile_at(u, i) * kPromptKvTokens + sub * 16;
+                    return seen(s0) ? __ldg(bt + (s0 >> (ts + 4))) : (int)p.num_pages;
                 };
-                auto pv = [&](int x, int j, int part) {                        // the first 96 tokens, the last 32
-                    const int st = (n + j) % NS;
-                    umma::fence_after_thread_sync();
-                    const uint64_t vd = v_desc + (uint64_t)(st * kTileUnits);
-                    const uint32_t pd = tmem + x * 128, od = tmem + 256 + x * 128;
-                    if (elect_one()) {
-                        if (part == 0) {
-#pragma unroll
-                            for (int k = 0; k < 6; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, j > 0 || k > 0);
-                        } else {
-#pragma unroll
-                            for (int k = 6; k < 8; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, true);
-                            umma::commit(bar_o(x));
-                            if (x == X - 1) umma::commit(bar_ve + 8 * st);
+                int page = page_of(u.tile_begin);
+                for (int i = u.tile_begin; i < u.tile_end && ok; ++i, ++n) {
+                    const int s0 = tile_at(u, i) * kPromptKvTokens + sub * 16;
+                    const int next_page = page_of(i + 1);
+                    if ((unsigned)page >= (unsigned)p.num_pages && seen(s0)) {
+                        record_status(p.status, DA_ERR_BAD_PAGE);                   // such a box is read as zeros
+                        page = (int)p.num_pages;
+                    }
+                    const int slot0 = (s0 >> 4 & ((1 << ts) - 1)) << 4;
+                    const int st = n % NS;
+                    if (n >= NS) ok = prompt_wait(bar_empty + 8 * st, (uint32_t)(n / NS + 1) & 1u, sm_abort);
+                    if (!ok) break;
+                    // V boxes with rows to clear are copied by hand
+                    const bool part = is_v && seen(s0) && !whole(s0);
+                    const uint32_t parts = __ballot_sync(0xffffffffu, part && hf == 0 && lane < BOXES);
+                    for (uint32_t m = parts; m != 0; m &= m - 1) {
+                        const int from = __ffs(m) - 1;                              // the lane whose box it is
+                        const int pg = __shfl_sync(0xffffffffu, page, from), k0 = __shfl_sync(0xffffffffu, s0, from);
+                        const int sl = __shfl_sync(0xffffffffu, slot0, from), sb = __shfl_sync(0xffffffffu, sub, from);
+                        for (int c = lane; c < 16 * (D / 8); c += 32) {
+                            const int r = c / (D / 8), ch = c % (D / 8), k = k0 + r;
+                            uint4 x = make_uint4(0u, 0u, 0u, 0u);
+                            if (k < u.seq_len && (k >= lo || k < p.sinks) && pg < p.num_pages)
+                                x = __ldg(reinterpret_cast<const uint4*>(p.v + (int64_t)pg * p.v_stride_page +
+                                                                         (int64_t)(sl + r) * p.v_stride_token +
+                                                                         (int64_t)u.kv_head * p.v_stride_head) + ch);
+                            *reinterpret_cast<uint4*>(gbase + (v_base - base) + st * Cfg::kTileBytes + (ch >> 3) * Cfg::kHalfBytes +
+                                                      sb * 2048 + swz(r, ch & 7)) = x;
                         }
                     }
+                    if (parts != 0) {
+                        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                        __syncwarp();
+                    }
+                    if (lane == 0) mbar_arrive_expect_tx(bar_full + 8 * st, Cfg::kTileBytes - __popc(parts) * (16 * D * 2));
                     __syncwarp();
-                };
-                auto k_landed = [&](int j) { return prompt_wait(bar_kf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort); };
-                for (int x = 0; x < X && ok; ++x) {
-                    ok = prompt_wait(bar_q(x), (uint32_t)cu[x] & 1u, sm_abort) && k_landed(0);
-                    if (ok) qk(x, 0);
+                    if (lane < BOXES && !part)
+                        tma_load_4d(ring + st * Cfg::kTileBytes + hf * Cfg::kHalfBytes + sub * 2048, map, bar_full + 8 * st, hf * 64, slot0,
+                                    u.kv_head, page, keep);
+                    if (!is_v && i == u.tile_begin) {
+                        // The unit's query rows: TQ tokens x the group's heads, rows of the MMA tile in that order.  (Tokens of
+                        // a ragged end are other rows of q, or zeros behind the last: what comes of them is not stored.)
+                        for (int x = 0; x < (u.n_tok > TQ ? 2 : 1) && ok; ++x) {
+                            if (cu[x] > 0) ok = prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
+                            if (!ok) break;
+                            ++cu[x];
+                            if (lane == 0) {
+                                mbar_arrive_expect_tx(bar_q(x), Cfg::kHalves * G * TQ * 128);
+                                for (int h = 0; h < Cfg::kHalves; ++h)
+                                    tma_load_3d(q_base + x * Cfg::kTileBytes + h * Cfg::kHalfBytes, &q_map, bar_q(x), h * 64, u.kv_head * G,
+                                                u.row + x * TQ);
+                            }
+                            __syncwarp();
+                        }
+                    }
+                    page = next_page;
                 }
-                for (int j = 0; j < T && ok; ++j) {
+            }
+            if (*sm_abort != 0) {
+                // given up somewhere: nothing may land in shared memory after the block has left (a copy always lands)
+                for (int i = max(0, n - NS); i <= n; ++i)
+                    if (i < n || !ok) mbar_wait(bar_full + 8 * (i % NS), (uint32_t)(i / NS) & 1u, i < n ? kWaitLimitCycles : 1000000LL);
+                for (int x = 0; x < 2; ++x)
+                    if (cu[x] > 0) mbar_wait(bar_q(x), (uint32_t)(cu[x] - 1) & 1u);
+            }
+        } else if (role == kPromptMmaWarp) {
+            // ------------------------------------------------------------ MMAs (the warp together, one lane issues)
+            {
+                constexpr uint32_t idesc_qk = umma::instr_desc_16(128, 128, false, F16);
+                constexpr uint32_t idesc_pv = umma::instr_desc_16(128, D, true, F16);
+                constexpr uint32_t kTileUnits = Cfg::kTileBytes >> 4, kHalfUnits = Cfg::kHalfBytes >> 4;
+                const uint64_t q_desc = umma::smem_desc_sw128(q_base, 16, 1024);
+                const uint64_t k_desc = umma::smem_desc_sw128(k_base, 16, 1024);
+                const uint64_t v_desc = umma::smem_desc_sw128(v_base, Cfg::kHalfBytes, 1024);
+                int n = 0;                                        // K/V tiles before the unit
+                int cs[2] = {0, 0}, cu[2] = {0, 0};               // per MMA tile: P V issued, units begun
+                bool ok = true;
+                for (int ui = ubeg; ui < uend && ok; ++ui) {
+                    const PromptUnit u = p.units[ui];
+                    const int T = u.tile_end - u.tile_begin;
+                    const int X = u.n_tok > TQ ? 2 : 1;
+                    auto qk = [&](int x, int j) {
+                        const int st = (n + j) % NS;
+                        umma::fence_after_thread_sync();
+                        const uint64_t qd = q_desc + (uint64_t)(x * kTileUnits), kd = k_desc + (uint64_t)(st * kTileUnits);
+                        if (elect_one()) {
+#pragma unroll
+                            for (int ks = 0; ks < D / 16; ++ks) {
+                                const uint32_t off = (ks >> 2) * kHalfUnits + (ks & 3) * 2;
+                                umma::mma_ss(tmem + x * 128, qd + off, kd + off, idesc_qk, ks > 0);
+                            }
+                            umma::commit(bar_s(x));
+                            if (x == X - 1) umma::commit(bar_ke + 8 * st);
+                            if (j == T - 1) umma::commit(bar_qe(x));
+                        }
+                        __syncwarp();
+                    };
+                    auto pv = [&](int x, int j, int part) {                        // the first 96 tokens, the last 32
+                        const int st = (n + j) % NS;
+                        umma::fence_after_thread_sync();
+                        const uint64_t vd = v_desc + (uint64_t)(st * kTileUnits);
+                        const uint32_t pd = tmem + x * 128, od = tmem + 256 + x * 128;
+                        if (elect_one()) {
+                            if (part == 0) {
+#pragma unroll
+                                for (int k = 0; k < 6; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, j > 0 || k > 0);
+                            } else {
+#pragma unroll
+                                for (int k = 6; k < 8; ++k) umma::mma_ts(od, pd + k * 8, vd + k * 128, idesc_pv, true);
+                                umma::commit(bar_o(x));
+                                if (x == X - 1) umma::commit(bar_ve + 8 * st);
+                            }
+                        }
+                        __syncwarp();
+                    };
+                    auto k_landed = [&](int j) {
+                        return prompt_wait(bar_kf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort);
+                    };
                     for (int x = 0; x < X && ok; ++x) {
-                        // (the weights last: every wait behind theirs would be time the tensor core stands still)
-                        ok = prompt_wait(bar_vf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort) &&
-                             (j > 0 || cu[x] == 0 || prompt_wait(bar_of(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort)) &&
-                             prompt_spin(bar_p(x, 0), (uint32_t)cs[x] & 1u, sm_abort);
-                        if (!ok) break;
-                        pv(x, j, 0);
-                        ok = prompt_spin(bar_p(x, 1), (uint32_t)cs[x] & 1u, sm_abort);
-                        if (!ok) break;
-                        pv(x, j, 1);
-                        ++cs[x];
-                        if (j + 1 < T) {
-                            ok = k_landed(j + 1);
-                            if (ok) qk(x, j + 1);
+                        ok = prompt_wait(bar_q(x), (uint32_t)cu[x] & 1u, sm_abort) && k_landed(0);
+                        if (ok) qk(x, 0);
+                    }
+                    for (int j = 0; j < T && ok; ++j) {
+                        for (int x = 0; x < X && ok; ++x) {
+                            // (the weights last: every wait behind theirs would be time the tensor core stands still)
+                            ok = prompt_wait(bar_vf + 8 * ((n + j) % NS), (uint32_t)((n + j) / NS) & 1u, sm_abort) &&
+                                 (j > 0 || cu[x] == 0 || prompt_wait(bar_of(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort)) &&
+                                 prompt_spin(bar_p(x, 0), (uint32_t)cs[x] & 1u, sm_abort);
+                            if (!ok) break;
+                            pv(x, j, 0);
+                            ok = prompt_spin(bar_p(x, 1), (uint32_t)cs[x] & 1u, sm_abort);
+                            if (!ok) break;
+                            pv(x, j, 1);
+                            ++cs[x];
+                            if (j + 1 < T) {
+                                ok = k_landed(j + 1);
+                                if (ok) qk(x, j + 1);
+                            }
                         }
                     }
+                    for (int x = 0; x < X; ++x) ++cu[x];
+                    n += T;
                 }
-                for (int x = 0; x < X; ++x) ++cu[x];
-                n += T;
-            }
-            // nothing may arrive on a barrier, or be written, after the block has left
-            if (ok)
-                for (int i = max(0, n - NS); i < n; ++i) {
-                    ok = ok && prompt_wait(bar_ke + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
-                    ok = ok && prompt_wait(bar_ve + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
+                // nothing may arrive on a barrier, or be written, after the block has left
+                if (ok)
+                    for (int i = max(0, n - NS); i < n; ++i) {
+                        ok = ok && prompt_wait(bar_ke + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
+                        ok = ok && prompt_wait(bar_ve + 8 * (i % NS), (uint32_t)(i / NS) & 1u, sm_abort);
+                    }
+                for (int x = 0; x < 2; ++x)
+                    if (cu[x] > 0) ok = ok && prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
+                if (!ok) {
+                    if (elect_one()) umma::commit(bar_drain);
+                    mbar_wait(bar_drain, 0);
                 }
-            for (int x = 0; x < 2; ++x)
-                if (cu[x] > 0) ok = ok && prompt_wait(bar_qe(x), (uint32_t)(cu[x] - 1) & 1u, sm_abort);
-            if (!ok) {
-                if (elect_one()) umma::commit(bar_drain);
-                mbar_wait(bar_drain, 0);
             }
+            __syncwarp();
         }
-        __syncwarp();
-    } else if (warp < kPromptSoftmaxWarps) {
+    } else {
         // ------------------------------------------------------------ softmax, output: one thread per row
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kPromptSoftmaxRegs));
         const int x = warp >> 2, r = (warp & 3) * 32 + lane;
@@ -587,8 +594,6 @@ decode_attn_prompt_kernel(const PromptParams p, const __grid_constant__ CUtensor
                     p.lse[row0 + to] = none ? -INFINITY : (m + log2f(l)) * kLn2;
             }
         }
-    } else {
-        give_registers();                                                      // (the third warpgroup's last warp)
     }
     umma::fence_before_thread_sync();
     __syncthreads();
