@@ -579,8 +579,10 @@ int decode_attn_debug_expire_wait(const decode_attn_plan_t *plan, const decode_a
  * Whole step from host buffers: copies q, both pools, block table and
  * lengths to the device (into a grow-only arena the library keeps), plans,
  * runs, combines, copies `out` (and lse) back and synchronises.  pool_elems
- * is the element count of each pool.  For end-to-end measurement and simple
- * callers; serving engines keep the pools resident and use plan/run/combine.
+ * is the element count of each pool.  The block table is checked first: the
+ * entries that the step looks up (with policy.window_tokens those of pages with
+ * a visible position) must lie in the pool, else DA_ERR_BAD_PAGE.  For
+ * end-to-end measurement and simple callers; serving engines keep the pools resident and use plan/run/combine.
  * ------------------------------------------------------------------------- */
 int decode_attn_host_step(const decode_attn_shape_t *shape, const decode_attn_policy_t *policy,
                           const void *q_host, const void *k_cache_host, const void *v_cache_host,

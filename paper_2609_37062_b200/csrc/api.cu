@@ -1035,8 +1035,9 @@ int decode_attn_last_device_status(const decode_attn_plan_t* pl, cudaStream_t st
     return st;
 }
 
-int decode_attn_validate_block_table(const decode_attn_shape_t* shape, const int32_t* seq_lens_host,
-                                     const int32_t* block_table_host)
+// The entries a step looks up: with a window only those of pages that hold a visible position.
+static int validate_pages(const decode_attn_shape_t* shape, const int32_t* seq_lens_host, const int32_t* block_table_host,
+                          int32_t window, int32_t sinks)
 {
     if (!shape || (shape->batch > 0 && (!seq_lens_host || !block_table_host))) return DA_ERR_INVALID_ARG;
     int rc = validate_shape(*shape);
@@ -1045,12 +1046,20 @@ int decode_attn_validate_block_table(const decode_attn_shape_t* shape, const int
         if (seq_lens_host[b] < 0) return DA_ERR_INVALID_ARG;
         const int64_t pages = ((int64_t)seq_lens_host[b] + shape->page_size - 1) / shape->page_size;
         if (pages > shape->max_pages_per_seq) return DA_ERR_INVALID_ARG;
+        const int64_t first = window > 0 ? (int64_t)seq_lens_host[b] - window : 0;     // of the window
         for (int64_t i = 0; i < pages; ++i) {
+            if ((i + 1) * shape->page_size <= first && i * shape->page_size >= sinks) continue;
             const int32_t pg = block_table_host[(int64_t)b * shape->max_pages_per_seq + i];
             if (pg < 0 || pg >= shape->num_pages) return DA_ERR_BAD_PAGE;
         }
     }
     return DA_OK;
+}
+
+int decode_attn_validate_block_table(const decode_attn_shape_t* shape, const int32_t* seq_lens_host,
+                                     const int32_t* block_table_host)
+{
+    return validate_pages(shape, seq_lens_host, block_table_host, 0, 0);
 }
 
 int decode_attn_validate_shared_prefix(const decode_attn_shape_t* shape, int32_t shared_prefix_tokens,
@@ -1209,7 +1218,7 @@ int decode_attn_host_step(const decode_attn_shape_t* shape, const decode_attn_po
         !out_host || pool_elems <= 0)
         return DA_ERR_INVALID_ARG;
     if (policy->capacity_batch != 0) return DA_ERR_INVALID_ARG;
-    int rc = decode_attn_validate_block_table(shape, seq_lens_host, block_table_host);
+    int rc = validate_pages(shape, seq_lens_host, block_table_host, policy->window_tokens, policy->sink_tokens);
     if (rc != DA_OK) return rc;
     if (shape->batch == 0) return DA_OK;
 
