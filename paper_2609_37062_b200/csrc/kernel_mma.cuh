@@ -207,7 +207,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
     constexpr int kConsumerThreads = kMmaConsumerWarps * 32;
     constexpr int NT = WIDE ? 2 : 1;                          // 8-column tiles of query heads
     static_assert(!(WIDE && (DUP || PREFIX)), "wide groups: ordinary units, low parts of P in a second mma");
-    static_assert(!EXT || (MODE == kModeAttend && !PREFIX && !MASKED), "windows, weights: ordinary attention units");
+    static_assert(!EXT || (MODE == kModeAttend && !PREFIX), "windows, weights: ordinary attention units");
     // the tile of the sequence that visible tile v of a unit is
     auto tile_of = [&](const WindowCut& w, int v) { return EXT ? window_tile(w, v) : v; };
     auto cut_of = [&](const decode_attn_unit_t& x) { return EXT ? window_cut(x.seq_len, p.window, p.sinks) : WindowCut{0, 0, 0}; };
@@ -388,7 +388,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                 ids = first_ids(x, end);
                 return 1;
             }
-            if (x.tok_end == x.seq_len && x.tok_end > x.tok_begin && (x.kv_head >> 16) == 0)
+            if (has_last(x, cut_of(x)) && x.tok_end > x.tok_begin && (x.kv_head >> 16) == 0)
                 append_new_row<D>(p, x.seq, x.kv_head, x.seq_len, lane);     // a masked row still writes its K/V
             block_finish_empty<D>(p, x, G, lane, 32);
             return 0;
@@ -402,7 +402,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
             t1 = unit_end(u);
             int r = 1;
             if (t1 <= u.tok_begin) {
-                if (u.tok_end == u.seq_len && u.tok_end > u.tok_begin && (u.kv_head >> 16) == 0)
+                if (has_last(u, cut_of(u)) && u.tok_end > u.tok_begin && (u.kv_head >> 16) == 0)
                     append_new_row<D>(p, u.seq, u.kv_head, u.seq_len, lane);
                 block_finish_empty<D>(p, u, G, lane, 32);
                 r = 0;
@@ -451,7 +451,7 @@ __global__ void __launch_bounds__(kMmaThreads, 2) decode_attn_mma_kernel(const K
                         next_state = 1;
                         publish(nu, true);
                     } else {
-                        if (nu.tok_end == nu.seq_len && nu.tok_end > nu.tok_begin && (nu.kv_head >> 16) == 0)
+                        if (has_last(nu, cut_of(nu)) && nu.tok_end > nu.tok_begin && (nu.kv_head >> 16) == 0)
                             append_new_row<D>(p, nu.seq, nu.kv_head, nu.seq_len, lane);
                         block_finish_empty<D>(p, nu, G, lane, 32);
                         q_link = 0;
@@ -1206,7 +1206,7 @@ inline int make_pool_map(CUtensorMap* map, const void* pool, const decode_attn_s
 typedef void (*mma_kernel_t)(const KernelParams, const CUtensorMap, const CUtensorMap, const int, const MmaExtra);
 
 // The variants for windowed plans and plans that track weights (compiled in kernel_mma_ext.cu).
-mma_kernel_t mma_ext_kernel_for(int D, int G, bool f16);
+mma_kernel_t mma_ext_kernel_for(int D, int G, bool f16, bool masked);
 
 // f16: q, K and V are fp16 (attention mode); else bf16.
 template <int MODE>
@@ -1276,7 +1276,7 @@ template <int MODE>
 inline int mma_prepare(int D, int G, mma_kernel_t* fn_out, bool prefix = false, bool f16 = false, bool masked = false,
                        bool ext = false)
 {
-    mma_kernel_t fn = ext ? mma_ext_kernel_for(D, G, f16) : mma_kernel_for<MODE>(D, G, prefix, f16, masked);
+    mma_kernel_t fn = ext ? mma_ext_kernel_for(D, G, f16, masked) : mma_kernel_for<MODE>(D, G, prefix, f16, masked);
     if (!fn) return DA_ERR_UNSUPPORTED;
     if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, mma_smem_bytes(D, G)) != cudaSuccess) {
         (void)cudaGetLastError();

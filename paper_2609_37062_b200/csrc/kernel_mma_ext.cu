@@ -4,19 +4,25 @@
 
 namespace da {
 
-template <int D, bool F16>
+template <int D, bool F16, bool MASKED>
 static mma_kernel_t for_group(int G)
 {
-    if (G > 8) return decode_attn_mma_kernel<D, false, kModeAttend, false, F16, false, true, true>;
-    return G <= 4 ? decode_attn_mma_kernel<D, true, kModeAttend, false, F16, false, false, true>
-                  : decode_attn_mma_kernel<D, false, kModeAttend, false, F16, false, false, true>;
+    if (G > 8) return decode_attn_mma_kernel<D, false, kModeAttend, false, F16, MASKED, true, true>;
+    return G <= 4 ? decode_attn_mma_kernel<D, true, kModeAttend, false, F16, MASKED, false, true>
+                  : decode_attn_mma_kernel<D, false, kModeAttend, false, F16, MASKED, false, true>;
 }
 
-mma_kernel_t mma_ext_kernel_for(int D, int G, bool f16)
+template <int D>
+static mma_kernel_t for_type(int G, bool f16, bool masked)
+{
+    if (masked) return f16 ? for_group<D, true, true>(G) : for_group<D, false, true>(G);
+    return f16 ? for_group<D, true, false>(G) : for_group<D, false, false>(G);
+}
+
+mma_kernel_t mma_ext_kernel_for(int D, int G, bool f16, bool masked)
 {
     if (!mma_supports(D, G)) return nullptr;
-    if (D == 128) return f16 ? for_group<128, true>(G) : for_group<128, false>(G);
-    return f16 ? for_group<64, true>(G) : for_group<64, false>(G);
+    return D == 128 ? for_type<128>(G, f16, masked) : for_type<64>(G, f16, masked);
 }
 
 }  // namespace da
