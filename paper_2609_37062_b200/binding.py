@@ -384,9 +384,11 @@ def decode_attn_combine(plan: Plan, workspace, out, lse=None, stream=None, check
 
 def _weights_layout(shape: Shape, weights, weights_out, where: str):
     """Strides and row length of two buffers of totals that have to be laid out alike."""
+    import torch
     size, strides = weights.shape, weights.stride()
-    if size != weights_out.shape or strides != weights_out.stride() or strides[2] != 1 or size[0] < shape.batch or \
-            size[1] != shape.num_kv_heads:
+    if weights.dtype is not torch.float32 or weights_out.dtype is not torch.float32 or \
+            size != weights_out.shape or strides != weights_out.stride() or len(size) != 3 or strides[2] != 1 or \
+            size[0] < shape.batch or size[1] != shape.num_kv_heads:
         raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
     return strides, size[2]
 
@@ -485,12 +487,19 @@ def decode_attn_evict(shape: Shape, budget_tokens: int, sink_tokens: int, recent
     if weights_out is None:
         weights_out = weights
     strides, tokens = _weights_layout(shape, weights, weights_out, "decode_attn_evict")
+    import torch
+    i32 = torch.int32
     pages, (row_stride, page_stride) = dst_block_table.shape[1], dst_block_table.stride()
-    if kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous() or \
-            seq_lens_out.numel() < shape.batch or dst_block_table.shape[0] < shape.batch or page_stride != 1 or \
+    if shape.batch <= 1:
+        row_stride = pages                                    # (whatever the stride of a single row is)
+    if dst_block_table.dtype is not i32 or kept.dtype is not i32 or seq_lens_out.dtype is not i32 or \
+            (status is not None and status.dtype is not i32) or \
+            kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous() or \
+            not seq_lens_out.is_contiguous() or seq_lens_out.numel() < shape.batch or \
+            dst_block_table.shape[0] < shape.batch or page_stride != 1 or row_stride < pages or \
             pages * shape.page_size < budget_tokens:
         raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_evict")
-    a = _evict_args(budget_tokens, sink_tokens, recent_tokens, max(pages, row_stride))     # (columns of a wider table will do)
+    a = _evict_args(budget_tokens, sink_tokens, recent_tokens, row_stride)                 # (columns of a wider table will do)
     a.seq_lens, a.block_table, a.dst_block_table = _ptr(seq_lens), _ptr(block_table), _ptr(dst_block_table)
     a.k_cache, a.v_cache = _ptr(k_cache), _ptr(v_cache)
     a.weights, a.weights_out = _ptr(weights), _ptr(weights_out)
