@@ -53,6 +53,7 @@ struct decode_attn_plan {
     int64_t work_grid = 0;
     size_t workspace_bytes = 0;
     size_t off_logits = 0;   // in the workspace, behind the partial records (plans that track weights)
+    int64_t max_tiles = 0;   // that there is room for
     // device buffer (views into the cached allocation the plan holds)
     char* dev = nullptr;
     char* pinned = nullptr;
@@ -568,10 +569,10 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
 
     pl->workspace_bytes = (size_t)pl->max_slots * shape->num_kv_heads * rec_floats(pl->group, shape->head_dim) * sizeof(float);
     if (policy->track_weights) {
-        const int64_t tiles = policy->capacity_batch > 0 ? policy->capacity_tokens / kTileTokens + policy->capacity_batch
-                                                         : pl->layout.n_tiles;
+        pl->max_tiles = policy->capacity_batch > 0 ? capacity_tiles(*policy) : pl->layout.n_tiles;
+        if (pl->layout.n_tiles > pl->max_tiles) return DA_ERR_INVALID_ARG;
         pl->off_logits = align_up(pl->workspace_bytes, 256);
-        pl->workspace_bytes = pl->off_logits + (size_t)tiles * shape->num_kv_heads * pl->group * kTileTokens * sizeof(float);
+        pl->workspace_bytes = pl->off_logits + (size_t)pl->max_tiles * shape->num_kv_heads * pl->group * kTileTokens * sizeof(float);
     }
 
     pl->off_units = align_up(sizeof(DevHeader), 32);
@@ -634,6 +635,7 @@ int decode_attn_plan_update(decode_attn_plan_t* pl, int32_t batch, const int32_t
     int rc = make_layout(s, pl->policy, seq_lens_host, pl->sm_count, pl->ctas_per_sm, lay, pl->max_bins);
     if (rc != DA_OK) return rc;
     if ((int64_t)lay.units.size() > pl->max_units || lay.n_slots > pl->max_slots) return DA_ERR_INVALID_ARG;
+    if (pl->policy.track_weights && lay.n_tiles > pl->max_tiles) return DA_ERR_INVALID_ARG;
     // the previous refresh may still be reading the pinned mirror
     DA_CUDA_TRY(cudaEventSynchronize(pl->upload_done));
     pl->upload_pending = false;

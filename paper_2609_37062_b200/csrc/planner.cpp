@@ -144,6 +144,15 @@ int64_t capacity_slots(const decode_attn_shape_t& s, const decode_attn_policy_t&
     return ceil_div(p.capacity_tokens, chunk_tokens) + p.capacity_batch;
 }
 
+int64_t capacity_tiles(const decode_attn_policy_t& p)
+{
+    const int64_t all = (int64_t)p.capacity_tokens / kTileTokens + p.capacity_batch;
+    if (p.window_tokens == 0) return all;
+    // A window of W tokens reaches into at most ceil(W / 16) + 1 tiles, S sinks into ceil(S / 16).
+    const int64_t most = ceil_div(p.window_tokens, kTileTokens) + 1 + ceil_div(p.sink_tokens, kTileTokens);
+    return std::min(all, most * p.capacity_batch);
+}
+
 namespace {
 
 struct SeqCut {

@@ -61,5 +61,6 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
 // Upper bounds for a capacity plan (any batch <= capacity_batch and
 // sum(seq_lens) <= capacity_tokens).
 int64_t capacity_slots(const decode_attn_shape_t& s, const decode_attn_policy_t& p);
+int64_t capacity_tiles(const decode_attn_policy_t& p);   // visible 16-token tiles of all sequences
 
 }  // namespace da
