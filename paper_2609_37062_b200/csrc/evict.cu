@@ -1,7 +1,9 @@
 // Host side of decode_attn_evict.
 #include <algorithm>
 #include <cstring>
+#include <mutex>
 #include <new>
+#include <vector>
 
 #include "evict.cuh"
 #include "planner.h"
@@ -21,6 +23,34 @@ int check_numbers(const decode_attn_shape_t& s, const decode_attn_evict_args_t& 
         return DA_ERR_INVALID_ARG;
     if (a.dst_max_pages < 0 || (int64_t)a.dst_max_pages * s.page_size < a.budget_tokens) return DA_ERR_INVALID_ARG;
     return DA_OK;
+}
+
+// Blocks of a kernel that the current device holds at once, with the most shared memory its launches ask for (kept after the
+// first query); 0 if that cannot be told.
+int64_t resident_blocks(const void* fn, int threads, size_t smem)
+{
+    struct Entry {
+        int device;
+        const void* fn;
+        int64_t blocks;
+    };
+    static std::mutex mu;
+    static std::vector<Entry> known;
+    int dev = -1, per_sm = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    std::lock_guard<std::mutex> lock(mu);
+    for (const Entry& e : known)
+        if (e.device == dev && e.fn == fn) return e.blocks;
+    if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
+        cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, threads, smem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return 0;
+    }
+    known.push_back({dev, fn, (int64_t)sms * per_sm});
+    return (int64_t)sms * per_sm;
 }
 
 int launch(const void* fn, dim3 grid, int threads, size_t smem, EvictParams& ep, cudaStream_t stream)
@@ -103,20 +133,22 @@ extern "C" int decode_attn_evict(const decode_attn_shape_t* shape, const decode_
     // up to 2,048 totals small blocks, several to an SM; up to 8,192 and 32,768 larger ones whose threads still hold all
     // keys (8 rows of 4,100 totals: 12.8 us with blocks of 512, 17.7 with the 1,024 that longer rows take)
     const int threads = most <= 2048 ? 256 : most <= 8192 ? 512 : 1024;
-    // One launch where a block moves its row in about the time a launch takes (16 bytes times a few hundred per thread) and
-    // all blocks are resident at once (8 rows of 128 tokens 7.6 -> 6.7 us; 512 rows of 1,024 tokens, in two waves of
-    // blocks, 98 -> 129 us; blocks of 1,024 threads have no registers to spare for it: 19 -> 24 us).
-    const int64_t row_bytes = (int64_t)ep.budget * s.head_dim * 4;
-    const bool one = most <= 2048 ? rows <= 444 && row_bytes <= 128 * 1024 : most <= 8192 && rows <= 296 && row_bytes <= 256 * 1024;
+    // One launch where every warp of a block moves once (32 tokens) and all blocks are resident at once.  Rows of 1,500
+    // totals, 256 tokens of 128 dims kept: 128 rows 15.0 us against 16.9 in two launches, 440 rows 23.1 against 25.8; 384
+    // kept: 23.2 against 19.2.  Rows of 4,000, 512 kept: 128 rows 19.1 against 22.8, 256 rows (two waves) 43 against 33.
+    // (Blocks of 1,024 threads have no registers to spare for it: 19 -> 24 us.)
     const bool wide = s.head_dim == 128;
-    const void* select = most > 8192   ? (const void*)decode_attn_evict_select_kernel<1024, 2048, 32, 0>
-                         : most > 2048 ? (!one   ? (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 0>
-                                          : wide ? (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 128>
-                                                 : (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 64>)
-                                       : (!one   ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 0>
-                                          : wide ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 128>
-                                                 : (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 64>);
-    const void* move = s.head_dim == 128 ? (const void*)decode_attn_evict_move_kernel<128> : (const void*)decode_attn_evict_move_kernel<64>;
+    const void* const mover = most > 2048 ? (wide ? (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 128>
+                                                  : (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 64>)
+                                          : (wide ? (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 128>
+                                                  : (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 64>);
+    const bool one = most <= 8192 && ep.budget <= threads / 32 * kMoveTokens &&
+                     rows <= resident_blocks(mover, threads, (most <= 2048 ? 2048 : 8192) * sizeof(float));
+    const void* select = one           ? mover
+                         : most > 8192 ? (const void*)decode_attn_evict_select_kernel<1024, 2048, 32, 0>
+                         : most > 2048 ? (const void*)decode_attn_evict_select_kernel<512, 1024, 16, 0>
+                                       : (const void*)decode_attn_evict_select_kernel<256, 1024, 8, 0>;
+    const void* move = wide ? (const void*)decode_attn_evict_move_kernel<128> : (const void*)decode_attn_evict_move_kernel<64>;
     if (smem > 32 * 1024 &&
         cudaFuncSetAttribute(select, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvictChunk * (int)sizeof(float)) != cudaSuccess) {
         (void)cudaGetLastError();
