@@ -386,9 +386,9 @@ def _weights_layout(shape: Shape, weights, weights_out, where: str):
     """Strides and row length of two buffers of totals that have to be laid out alike."""
     import torch
     size, strides = weights.shape, weights.stride()
-    if weights.dtype is not torch.float32 or weights_out.dtype is not torch.float32 or \
-            size != weights_out.shape or strides != weights_out.stride() or len(size) != 3 or strides[2] != 1 or \
-            size[0] < shape.batch or size[1] != shape.num_kv_heads:
+    if weights.dtype is not torch.float32 or len(size) != 3 or strides[2] != 1 or size[0] < shape.batch or \
+            size[1] != shape.num_kv_heads or (weights_out is not weights and (
+                weights_out.dtype is not torch.float32 or weights_out.shape != size or weights_out.stride() != strides)):
         raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
     return strides, size[2]
 
@@ -471,9 +471,12 @@ def decode_attn_prompt_last_device_status(plan: PromptPlan, stream=None) -> int:
     return _lib.decode_attn_prompt_last_device_status(plan.handle, _stream(stream))
 
 
+_EVICT_ARGS_SIZE = ctypes.sizeof(EvictArgs)
+
+
 def _evict_args(budget_tokens, sink_tokens, recent_tokens, dst_max_pages) -> EvictArgs:
     a = EvictArgs()
-    a.struct_size = ctypes.sizeof(EvictArgs)
+    a.struct_size = _EVICT_ARGS_SIZE
     a.budget_tokens, a.sink_tokens, a.recent_tokens = budget_tokens, sink_tokens, recent_tokens
     a.dst_max_pages = dst_max_pages
     return a
@@ -486,25 +489,24 @@ def decode_attn_evict(shape: Shape, budget_tokens: int, sink_tokens: int, recent
     num_kv_heads, budget_tokens]; seq_lens_out: int32 [batch]; status: int32 [1] or None."""
     if weights_out is None:
         weights_out = weights
-    strides, tokens = _weights_layout(shape, weights, weights_out, "decode_attn_evict")
     import torch
-    i32 = torch.int32
-    pages, (row_stride, page_stride) = dst_block_table.shape[1], dst_block_table.stride()
-    if shape.batch <= 1:
+    strides, tokens = _weights_layout(shape, weights, weights_out, "decode_attn_evict")
+    batch, i32 = shape.batch, torch.int32
+    (tables, pages), (row_stride, page_stride) = dst_block_table.shape, dst_block_table.stride()
+    if batch <= 1:
         row_stride = pages                                    # (whatever the stride of a single row is)
     if dst_block_table.dtype is not i32 or kept.dtype is not i32 or seq_lens_out.dtype is not i32 or \
             (status is not None and status.dtype is not i32) or \
-            kept.numel() < shape.batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous() or \
-            not seq_lens_out.is_contiguous() or seq_lens_out.numel() < shape.batch or \
-            dst_block_table.shape[0] < shape.batch or page_stride != 1 or row_stride < pages or \
-            pages * shape.page_size < budget_tokens:
+            kept.numel() < batch * shape.num_kv_heads * budget_tokens or not kept.is_contiguous() or \
+            not seq_lens_out.is_contiguous() or seq_lens_out.numel() < batch or \
+            tables < batch or page_stride != 1 or row_stride < pages or pages * shape.page_size < budget_tokens:
         raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_evict")
     a = _evict_args(budget_tokens, sink_tokens, recent_tokens, row_stride)                 # (columns of a wider table will do)
-    a.seq_lens, a.block_table, a.dst_block_table = _ptr(seq_lens), _ptr(block_table), _ptr(dst_block_table)
+    a.seq_lens, a.block_table, a.dst_block_table = _ptr(seq_lens), _ptr(block_table), dst_block_table.data_ptr()
     a.k_cache, a.v_cache = _ptr(k_cache), _ptr(v_cache)
-    a.weights, a.weights_out = _ptr(weights), _ptr(weights_out)
+    a.weights, a.weights_out = weights.data_ptr(), weights_out.data_ptr()
     a.weight_tokens, a.stride_seq, a.stride_head = tokens, strides[0], strides[1]
-    a.kept, a.seq_lens_out, a.status = _ptr(kept), _ptr(seq_lens_out), _ptr(status)
+    a.kept, a.seq_lens_out, a.status = kept.data_ptr(), seq_lens_out.data_ptr(), _ptr(status)
     rc = _lib.decode_attn_evict(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
     if check:
         _check(rc, "decode_attn_evict")
