@@ -15,8 +15,8 @@
 #include "combine.cuh"
 #include "common.cuh"
 #include "decode_attn.h"
-#include "kernel_mma.cuh"
-#include "kernel_umma.cuh"
+#include "kernel_mma_launch.cuh"
+#include "kernel_umma_launch.cuh"
 #include "kernel_simt.cuh"
 #include "planner.h"
 #include "prompt_launch.h"
