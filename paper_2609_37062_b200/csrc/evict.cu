@@ -3,7 +3,6 @@
 #include <cstring>
 #include <mutex>
 #include <new>
-#include <vector>
 
 #include "evict.cuh"
 #include "planner.h"
@@ -35,21 +34,22 @@ int64_t resident_blocks(const void* fn, int threads, size_t smem)
         int64_t blocks;
     };
     static std::mutex mu;
-    static std::vector<Entry> known;
+    static Entry known[64];                                   // (four kernels; nothing here may throw)
+    static int n_known = 0;
     int dev = -1, per_sm = 0, sms = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) {
         (void)cudaGetLastError();
         return 0;
     }
     std::lock_guard<std::mutex> lock(mu);
-    for (const Entry& e : known)
-        if (e.device == dev && e.fn == fn) return e.blocks;
+    for (int i = 0; i < n_known; ++i)
+        if (known[i].device == dev && known[i].fn == fn) return known[i].blocks;
     if (cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess ||
         cudaOccupancyMaxActiveBlocksPerMultiprocessor(&per_sm, fn, threads, smem) != cudaSuccess) {
         (void)cudaGetLastError();
         return 0;
     }
-    known.push_back({dev, fn, (int64_t)sms * per_sm});
+    if (n_known < 64) known[n_known++] = {dev, fn, (int64_t)sms * per_sm};
     return (int64_t)sms * per_sm;
 }
 
