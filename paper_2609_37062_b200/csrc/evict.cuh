@@ -15,7 +15,7 @@
 //           loses: the exchange of a counting step through distributed shared memory takes 1,300 cycles.)
 //   move    K and V rows of the kept positions, 16 bytes a lane, 32 tokens of one KV head per warp.
 //
-// Where that is little per row the select blocks move their rows themselves, in one launch.
+// Where each of a block's warps would move once, the select blocks move their rows themselves, in one launch.
 //
 // Select reads 4 bytes per token and KV head, move reads and writes 4 D of them for every kept one: the
 // second is the bound, by memory.
