@@ -340,7 +340,7 @@ def _own_rows(s):
 def _own_chunk(s):
     da = s["da"]
     da.decode_attn_prepare_rows(s["shape"], None, s["k"], s["v"], s["slots"], k_cache=s["pool"], cache_bits=4)
-    da.decode_attn_kv4_expand(s["dst_shape"], s["shape"], s["pool"], s["block_table"], s["seq_lens"], s["dst_table"],
+    da.decode_attn_expand_kv(s["dst_shape"], s["shape"], s["pool"], s["block_table"], s["seq_lens"], s["dst_table"],
                               s["k_pool"], s["v_pool"])
     return {"k": s["k_pool"], "v": s["v_pool"]}
 
