@@ -57,7 +57,8 @@ typedef enum {
     DA_ERR_STALE_PLAN = -4,          /* seq_lens differ from the ones the plan was made for            */
     DA_ERR_CUDA = -5,                /* a CUDA runtime/driver call failed, or no device                */
     DA_ERR_BAD_PAGE = -6,            /* a referenced block-table entry lies outside [0, num_pages)     */
-    DA_ERR_TIMEOUT = -7              /* a bounded device-side wait gave up                             */
+    DA_ERR_TIMEOUT = -7,             /* a bounded device-side wait gave up                             */
+    DA_ERR_NO_PAGES = -8             /* the list of free pages is too short (decode_attn_step_tables)  */
 } da_status_t;
 
 enum { DA_DTYPE_BF16 = 1, DA_DTYPE_FP32 = 2, DA_DTYPE_FP16 = 3 };
@@ -75,6 +76,7 @@ typedef enum {
     DA_KERNEL_SIMT = 1,     /* CUDA-core kernel, 16-byte vectorised global loads; groups of up to 8   */
     DA_KERNEL_MMA_TMA = 2,  /* TMA-staged pages in shared memory, mma.sync (bf16 or fp16) for QK^T, PV;
                                groups of up to 16 heads (two 8-column tiles of heads above 8)         */
+    DA_KERNEL_PACKED = 4,   /* caches held in 4 bits (policy.cache_bits = 4), and only those; see below     */
     DA_KERNEL_UMMA_PREFIX = 3 /* shared-prefix plans only (head_dim 128, groups of 1 to 16 heads): the prefix
                                units run on the tcgen05 tensor cores, 128 query rows at a time with
                                accumulators in tensor memory; what follows the prefix runs as MMA_TMA */
@@ -120,7 +122,9 @@ typedef struct {
     int32_t track_weights;  /* 1: the launch also leaves every logit in the workspace, from which
                                decode_attn_add_weights adds each cached token's attention weight to a
                                running total.  Tensor-core kernel MMA_TMA, no shared prefix.           */
-    int32_t reserved[2];
+    int32_t cache_bits;     /* 0 or 16: K and V in 16 bits.  4: one pool of tiles in 4 bits, see "Caches in
+                               4 bits" below.  No shared prefix, no track_weights.                      */
+    int32_t reserved[1];
 } decode_attn_policy_t;
 
 typedef struct {
@@ -435,6 +439,170 @@ int decode_attn_prompt_run(const decode_attn_prompt_plan_t *plan, const void *q,
 
 /* decode_attn_last_device_status of a prompt plan. */
 int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Caches in 4 bits.  One pool of bytes holds K and V: a value is a code in
+ * e2m1 (a sign and a magnitude of 0, .5, 1, 1.5, 2, 3, 4 or 6; 4 bits) times
+ * the fp16 scale of the 32 dims that it lies in, 4.5 bits a value.  The scale
+ * of 32 values is the largest magnitude among them over 6, rounded to fp16
+ * (to at most 65,504), a code the nearest to value / scale, ties to the even
+ * code, 6 at most.  K and V are finite: infinities are held as 6 * 65,504
+ * over the zeros and small values beside them, NaN as anything.  Values whose
+ * block stays below 6 * 2^-14 in magnitude are held more coarsely, below
+ * 6 * 2^-25 as zeros.
+ *
+ * The tokens of one KV head of one page lie in page_size / 16 tiles, one
+ * behind the other, of 16 * D + 64 * (D / 32) bytes each (D: head_dim):
+ *   K codes   at 0:    row r (token r of the tile) has D / 2 bytes; dims d and d + 1 (d even) share the byte
+ *                      (d % 32 / 8) * (D / 8) + 4 * (d / 32) + d % 8 / 2, dim d its low half
+ *   V codes   at 8 D:  the same rows; dims d and d + 1 share byte d / 2, of which bit 5 is turned over in rows 8
+ *                      to 15 when D is 128
+ *   K scales  at 16 D: fp16 [16 rows][D / 32]
+ *   V scales  behind:  fp16 [D / 32][16]; row r is entry 4 (r / 4) + ((r % 4) xor (r / 4))
+ * (an order in which the attending warps read their operands straight from
+ * shared memory).  The tiles of head h of page p start at byte
+ * p * k_stride_page + h * k_stride_head of the pool: in a shape that is used
+ * with cache_bits 4 these two strides count bytes, are multiples of 16 and at
+ * least decode_attn_packed_head_bytes; the other four strides are not looked at.
+ *
+ * decode_attn_prepare_rows writes such a cache, decode_attn_expand_kv
+ * turns pages of it into 16-bit pages (for prompts), and decode steps read it
+ * as it is: a plan with policy.cache_bits = 4, then run and combine with the
+ * pool as k_cache and v_cache = NULL.  q and `out` are as ever.  Split modes,
+ * windows with sinks, RUN masks (by the planner's packing: masked rows are
+ * skipped, running ones not dealt out again), capacity plans and fused
+ * combine are served; new_k / new_v, shared prefixes, track_weights and the
+ * calls that move 16-bit rows (append, gather, evict) are not.  Products with
+ * K are exact up to fp32 sums; weights and values are rounded once to fp16
+ * ahead of the product with V.
+ * ------------------------------------------------------------------------- */
+
+/* Bytes of one KV head of one page of a cache in 4 bits; 0 for a head_dim or
+ * page_size that the library does not serve. */
+int64_t decode_attn_packed_head_bytes(int32_t head_dim, int32_t page_size);
+
+/* Expands the cached tokens [0, seq_len) of every sequence of a cache in 4
+ * bits into 16-bit pages (code * scale, rounded once to the shape's kv_dtype):
+ * what decode_attn_prompt_run and every other call on 16-bit pools can read.
+ *   shape          the 16-bit pools and their tables: batch, num_kv_heads, head_dim, page_size, num_pages and
+ *                  strides of k_cache and v_cache; max_pages_per_seq is dst_block_table's row stride
+ *   packed_shape   the pool in 4 bits: num_pages, k_stride_page, k_stride_head (bytes), max_pages_per_seq (of
+ *                  block_table); batch, num_kv_heads, head_dim and page_size as in shape
+ *   block_table, seq_lens, dst_block_table   device
+ *   status_or_null device, one word lowered to the worst condition met
+ * Rows behind a sequence's end are left as they were.  A length that does not
+ * fit either table leaves its sequence out (DA_ERR_STALE_PLAN), a page id
+ * outside its pool the tile (DA_ERR_BAD_PAGE).  Destination pages are named
+ * once.  One launch on `stream`, nothing is allocated, capture-safe; its grid
+ * covers the narrower of the two tables. */
+int decode_attn_expand_kv(const decode_attn_shape_t *shape, const decode_attn_shape_t *packed_shape, const void *pool,
+                          const int32_t *block_table, const int32_t *seq_lens, const int32_t *dst_block_table,
+                          void *k_cache, void *v_cache, int32_t *status_or_null, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Rows of new tokens: what lies between the projection of a step's tokens and
+ * their attention, in one pass.  For every row (token) with position >= 0:
+ *   head x of q or k:  x <- x / sqrt(mean(x^2) + eps) * weight      (with weights)
+ *                      x <- x rotated by the row of cos_sin of its position   (with cos_sin)
+ * in fp32, rounded once to the shape's kv_dtype; q goes to q_out, k to k_out
+ * and / or to its slot of the cache, v to its slot.  Rotation turns the pairs
+ * of the first rotary_dim dims: pair i is dims (i, i + rotary_dim / 2), or
+ * (2 i, 2 i + 1) with `interleaved`; (a, b) <- (a c - b s, b c + a s) with
+ * c = cos_sin[position][i], s = cos_sin[position][rotary_dim / 2 + i].
+ * A slot is page * page_size + place in the page; a negative slot: K and V of
+ * the row are not cached.  A row whose position is negative is padding (as
+ * decode_attn_step_tables marks it) and leaves everything as it was.
+ * With cache_bits 4, K (rounded as above) and V are quantised on the way: the
+ * same bytes as from rounded rows written by a second call.
+ * Slots of one call must differ.  One launch on `stream`, nothing is
+ * allocated, capture-safe.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    uint32_t struct_size;       /* sizeof(decode_attn_rows_args_t) */
+    uint32_t flags;             /* must be 0 */
+    int32_t rows;               /* tokens */
+    int32_t cache_bits;         /* 0 or 16: k_cache and v_cache are pools of the shape; 4: k_cache is a pool in 4 bits */
+    int32_t rotary_dim;         /* with cos_sin: a multiple of 8, 8 .. head_dim; 0 else */
+    int32_t interleaved;        /* 0 or 1 */
+    int32_t max_positions;      /* rows of cos_sin; a position behind leaves its row out (DA_ERR_STALE_PLAN) */
+    float eps;
+    const void *q;              /* device, 16-bit heads [rows][num_q_heads][head_dim]; a row's heads lie behind each other, */
+    const void *k;              /* rows are q_stride (k_stride, v_stride) elements apart, multiples of 8; 16-byte aligned. */
+    const void *v;              /* q may be NULL; so may v, or both of k and v, where there is no cache to write */
+    int64_t q_stride, k_stride, v_stride;
+    const void *q_weight;       /* device, 16-bit, 16-byte aligned: head_dim values for all heads, or with a stride of */
+    const void *k_weight;       /* head_dim a row of its own for each head (a stride of 0: shared).  NULL: no norm */
+    int64_t q_weight_stride, k_weight_stride;
+    const float *cos_sin;       /* device, fp32 [max_positions][rotary_dim], 16-byte aligned, or NULL: no rotation */
+    const int32_t *positions;   /* device, [rows]; may be NULL without cos_sin */
+    const int64_t *slots;       /* device, [rows]; may be NULL without a cache */
+    void *q_out;                /* device, rows q_out_stride apart, aligned like q; may be q with its stride */
+    void *k_out;                /* the same for k, or NULL */
+    int64_t q_out_stride, k_out_stride;
+    void *k_cache;              /* device pools, 16-byte aligned, or NULL */
+    void *v_cache;              /* (NULL with cache_bits 4) */
+    int32_t *status;            /* device, one word lowered to the worst condition met, or NULL; a slot outside the
+                                   pool is not written (DA_ERR_BAD_PAGE) */
+} decode_attn_rows_args_t;
+
+/* shape: num_q_heads, num_kv_heads, head_dim, page_size, num_pages, strides
+ * and kv_dtype (bf16 or fp16, of all rows, weights and 16-bit pools); its
+ * batch and max_pages_per_seq are not looked at. */
+int decode_attn_prepare_rows(const decode_attn_shape_t *shape, const decode_attn_rows_args_t *args, cudaStream_t stream);
+
+/* ---------------------------------------------------------------------------
+ * Step tables: block tables, slots and positions of a step, built on the
+ * device from how many tokens every sequence gains, so that lengths need not
+ * come back to the host.  Sequence b holds seq_lens[b] tokens on
+ * ceil(seq_lens[b] / page_size) pages; its new length is
+ * max(0, seq_lens[b] + gains[b]).
+ *  1. Sequences with a negative gain (rejected tokens, sequences that ended)
+ *     give back the pages that they no longer need: pushed onto the list of
+ *     free pages in the order of the sequences and of their positions.  Their
+ *     block-table entries keep what they held.  All their pages must be the
+ *     sequence's own: not shared with other rows, not taken back before.
+ *  2. Sequences with a positive gain take the pages that they lack off the
+ *     end of the list, in the same order: the j-th page taken is
+ *     free_pages[n - 1 - j], n being the list's length after 1.  They are
+ *     written to the block table.
+ *  3. The new tokens of all sequences are the rows of the step, one behind the
+ *     other: row i of sequence b has position seq_lens[b] + (i -
+ *     row_starts[b]) and the slot of that position.  Rows behind the last one
+ *     up to max_rows (a captured step's padding) get -1 throughout.
+ * A sequence is left as it was, without rows, where its length or new length
+ * does not fit the block table or is negative (DA_ERR_STALE_PLAN); where it grows and
+ * its rows and those of the growing sequences before it are more than
+ * max_rows (DA_ERR_WORKSPACE_TOO_SMALL); where it lacks pages and these and
+ * those that the sequences before it lack are more than the list holds
+ * (DA_ERR_NO_PAGES); where it gives back pages for which, behind those given
+ * back before, free_capacity leaves no room (DA_ERR_NO_PAGES).  A page id
+ * outside the pool gives its tokens the slot -1 (DA_ERR_BAD_PAGE).  A
+ * free_count outside [0, free_capacity] leaves all as it was (DA_ERR_STALE_PLAN,
+ * no rows).  What is met is recorded in `status` when one is given.
+ * One or two launches on `stream`, nothing is allocated, capture-safe.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+    uint32_t struct_size;       /* sizeof(decode_attn_tables_args_t) */
+    uint32_t flags;             /* must be 0 */
+    int32_t max_rows;           /* entries of slots, positions and row_seq */
+    int32_t free_capacity;      /* entries of free_pages */
+    const int32_t *seq_lens;    /* device, [batch]: tokens before the call */
+    const int32_t *gains;       /* device, [batch] */
+    int32_t *seq_lens_out;      /* device, [batch]: tokens after it; may be seq_lens */
+    int32_t *block_table;       /* device, [batch, shape.max_pages_per_seq], modified */
+    int32_t *free_pages;        /* device, [free_capacity], modified */
+    const int32_t *free_count;  /* device, one word: pages in the list */
+    int32_t *free_count_out;    /* device, one word: pages after the call; may be free_count */
+    int32_t *row_starts;        /* device, [batch + 1]: first row of every sequence, then the number of rows */
+    int32_t *page_starts;       /* device, [batch + 1]: pages taken by the sequences before, then by all */
+    int64_t *slots;             /* device, [max_rows], 8-byte aligned */
+    int32_t *positions;         /* device, [max_rows] */
+    int32_t *row_seq;           /* device, [max_rows]: the sequence of every row, or NULL */
+    int32_t *status;            /* device, one word that the call lowers to the worst condition met, or NULL */
+} decode_attn_tables_args_t;
+
+/* shape: batch, page_size, max_pages_per_seq and num_pages. */
+int decode_attn_step_tables(const decode_attn_shape_t *shape, const decode_attn_tables_args_t *args, cudaStream_t stream);
 
 /* Running totals of attention weights, what an eviction by attention weight
  * ranks a cache by (decode_attn_evict).  For plans made with

@@ -33,6 +33,7 @@ DA_ERR_STALE_PLAN = -4
 DA_ERR_CUDA = -5
 DA_ERR_BAD_PAGE = -6
 DA_ERR_TIMEOUT = -7
+DA_ERR_NO_PAGES = -8
 
 DA_DTYPE_BF16 = 1
 DA_DTYPE_FP32 = 2
@@ -46,6 +47,7 @@ DA_KERNEL_AUTO = 0
 DA_KERNEL_SIMT = 1
 DA_KERNEL_MMA_TMA = 2
 DA_KERNEL_UMMA_PREFIX = 3
+DA_KERNEL_PACKED = 4
 
 EXPORTED = [
     "decode_attn_plan_layout", "decode_attn_plan", "decode_attn_plan_update", "decode_attn_plan_get_info",
@@ -59,6 +61,7 @@ EXPORTED = [
     "decode_attn_add_weights", "decode_attn_evict", "decode_attn_validate_evict",
     "decode_attn_prompt_plan_layout", "decode_attn_prompt_plan", "decode_attn_prompt_plan_destroy",
     "decode_attn_prompt_run", "decode_attn_prompt_last_device_status",
+    "decode_attn_packed_head_bytes", "decode_attn_expand_kv", "decode_attn_prepare_rows", "decode_attn_step_tables",
 ]
 
 
@@ -69,7 +72,8 @@ class Policy(ctypes.Structure):
                 ("fuse_combine", ctypes.c_int32), ("capacity_batch", ctypes.c_int32),
                 ("capacity_tokens", ctypes.c_int32), ("ctas_per_sm", ctypes.c_int32),
                 ("shared_prefix_tokens", ctypes.c_int32), ("window_tokens", ctypes.c_int32),
-                ("sink_tokens", ctypes.c_int32), ("track_weights", ctypes.c_int32), ("reserved", ctypes.c_int32 * 2)]
+                ("sink_tokens", ctypes.c_int32), ("track_weights", ctypes.c_int32), ("cache_bits", ctypes.c_int32),
+                ("reserved", ctypes.c_int32 * 1)]
 
 
 class Shape(ctypes.Structure):
@@ -124,6 +128,30 @@ class EvictArgs(ctypes.Structure):
                 ("kept", ctypes.c_void_p), ("seq_lens_out", ctypes.c_void_p), ("status", ctypes.c_void_p)]
 
 
+class RowsArgs(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32), ("rows", ctypes.c_int32),
+                ("cache_bits", ctypes.c_int32), ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+                ("max_positions", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("q_stride", ctypes.c_int64), ("k_stride", ctypes.c_int64), ("v_stride", ctypes.c_int64),
+                ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p),
+                ("q_weight_stride", ctypes.c_int64), ("k_weight_stride", ctypes.c_int64),
+                ("cos_sin", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p),
+                ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+                ("q_out_stride", ctypes.c_int64), ("k_out_stride", ctypes.c_int64),
+                ("k_cache", ctypes.c_void_p), ("v_cache", ctypes.c_void_p), ("status", ctypes.c_void_p)]
+
+
+class TablesArgs(ctypes.Structure):
+    _fields_ = [("struct_size", ctypes.c_uint32), ("flags", ctypes.c_uint32),
+                ("max_rows", ctypes.c_int32), ("free_capacity", ctypes.c_int32),
+                ("seq_lens", ctypes.c_void_p), ("gains", ctypes.c_void_p), ("seq_lens_out", ctypes.c_void_p),
+                ("block_table", ctypes.c_void_p), ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+                ("free_count_out", ctypes.c_void_p), ("row_starts", ctypes.c_void_p), ("page_starts", ctypes.c_void_p),
+                ("slots", ctypes.c_void_p), ("positions", ctypes.c_void_p), ("row_seq", ctypes.c_void_p),
+                ("status", ctypes.c_void_p)]
+
+
 _vp = ctypes.c_void_p
 _lib.decode_attn_plan_layout.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Policy), _vp, ctypes.c_int32,
                                          ctypes.c_int32, _vp, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64),
@@ -163,6 +191,11 @@ _lib.decode_attn_prompt_run.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, 
 _lib.decode_attn_prompt_last_device_status.argtypes = [_vp, _vp]
 _lib.decode_attn_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(EvictArgs), _vp]
 _lib.decode_attn_validate_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(EvictArgs), _vp, _vp, _vp]
+_lib.decode_attn_packed_head_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
+_lib.decode_attn_packed_head_bytes.restype = ctypes.c_int64
+_lib.decode_attn_expand_kv.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Shape)] + [_vp] * 8
+_lib.decode_attn_prepare_rows.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(RowsArgs), _vp]
+_lib.decode_attn_step_tables.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(TablesArgs), _vp]
 _lib.decode_attn_breakeven_tokens.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int32,
                                               ctypes.c_double, ctypes.POINTER(ctypes.c_double)]
 _lib.decode_attn_switch_thresholds.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double),
@@ -239,13 +272,14 @@ def make_policy(split_mode: int = DA_SPLIT_AUTO, fixed_count: int = 0, chunk_tok
                 max_splits: int = 0, sm_count: int = 0, kernel: int = DA_KERNEL_AUTO, fuse_combine: int = 0,
                 capacity_batch: int = 0, capacity_tokens: int = 0, ctas_per_sm: int = 0,
                 shared_prefix_tokens: int = 0, window_tokens: int = 0, sink_tokens: int = 0,
-                track_weights: int = 0) -> Policy:
+                track_weights: int = 0, cache_bits: int = 0) -> Policy:
     p = Policy()
     p.split_mode, p.fixed_count, p.chunk_tokens, p.max_splits = split_mode, fixed_count, chunk_tokens, max_splits
     p.sm_count, p.kernel, p.fuse_combine = sm_count, kernel, fuse_combine
     p.capacity_batch, p.capacity_tokens, p.ctas_per_sm = capacity_batch, capacity_tokens, ctas_per_sm
     p.shared_prefix_tokens = shared_prefix_tokens
     p.window_tokens, p.sink_tokens, p.track_weights = window_tokens, sink_tokens, track_weights
+    p.cache_bits = cache_bits
     return p
 
 
@@ -262,6 +296,22 @@ def make_shape(batch: int, num_q_heads: int, num_kv_heads: int, head_dim: int, p
     s.out_dtype = out_dtype
     s.sm_scale = sm_scale
     return s
+
+
+def decode_attn_packed_head_bytes(head_dim: int, page_size: int) -> int:
+    """Bytes of one KV head of one page of a cache in 4 bits."""
+    return _lib.decode_attn_packed_head_bytes(head_dim, page_size)
+
+
+def make_kv4_shape(batch: int, num_q_heads: int, num_kv_heads: int, head_dim: int, page_size: int, max_pages_per_seq: int,
+                   num_pages: int, strides: Optional[Sequence[int]] = None, out_dtype: int = DA_DTYPE_FP32,
+                   sm_scale: float = 0.0, in_dtype: int = DA_DTYPE_BF16) -> Shape:
+    """The shape of a cache in 4 bits: a uint8 pool [num_pages, num_kv_heads, decode_attn_packed_head_bytes(...)], or
+    with other strides = (page, head) in bytes."""
+    head = decode_attn_packed_head_bytes(head_dim, page_size)
+    page_stride, head_stride = strides or (num_kv_heads * head, head)
+    return make_shape(batch, num_q_heads, num_kv_heads, head_dim, page_size, max_pages_per_seq, num_pages,
+                      (page_stride, 0, head_stride), (0, 0, 0), out_dtype=out_dtype, sm_scale=sm_scale, in_dtype=in_dtype)
 
 
 def shape_of_workload(w, out_dtype: int = DA_DTYPE_FP32, sm_scale: float = 0.0) -> Shape:
@@ -518,6 +568,110 @@ def decode_attn_validate_evict(shape: Shape, budget_tokens: int, sink_tokens: in
     lens, bt, dst = _host_i32(seq_lens_host), _host_i32(block_table_host), _host_i32(dst_block_table_host)
     a = _evict_args(budget_tokens, sink_tokens, recent_tokens, dst.shape[1])
     return _lib.decode_attn_validate_evict(ctypes.byref(shape), ctypes.byref(a), _ptr(lens), _ptr(bt), _ptr(dst))
+
+
+def decode_attn_expand_kv(shape: Shape, packed_shape: Shape, pool, block_table, seq_lens, dst_block_table, k_cache, v_cache,
+                          status=None, stream=None, check: bool = True) -> int:
+    """The cached tokens of a cache in 4 bits (packed_shape, pool, block_table) as 16-bit pages (shape, k_cache, v_cache,
+    dst_block_table); status: int32 [1] or None."""
+    rc = _lib.decode_attn_expand_kv(ctypes.byref(shape), ctypes.byref(packed_shape), _ptr(pool), _ptr(block_table),
+                                    _ptr(seq_lens), _ptr(dst_block_table), _ptr(k_cache), _ptr(v_cache), _ptr(status),
+                                    _stream(stream))
+    if check:
+        _check(rc, "decode_attn_expand_kv")
+    return rc
+
+
+_ROWS_ARGS_SIZE = ctypes.sizeof(RowsArgs)
+_TABLES_ARGS_SIZE = ctypes.sizeof(TablesArgs)
+
+
+def _heads(x, rows: int, heads: int, dim: int, dtype):
+    """Address and row stride of rows of heads [rows, heads, dim] that lie behind each other within a row."""
+    if x is None:
+        return None, 0
+    size, strides = x.shape, x.stride()
+    if x.dtype is not dtype or len(size) != 3 or size[0] < rows or size[1] != heads or size[2] != dim or strides[2] != 1 or \
+            (heads > 1 and strides[1] != dim):
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_prepare_rows")
+    return x.data_ptr(), strides[0] if size[0] > 1 else heads * dim
+
+
+def _head_weight(w, heads: int, dim: int, dtype):
+    if w is None:
+        return None, 0
+    if w.dtype is not dtype or not w.is_contiguous() or w.numel() not in (dim, heads * dim) or w.shape[-1] != dim:
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_prepare_rows")
+    return w.data_ptr(), dim if w.dim() > 1 and w.shape[0] == heads and heads > 1 else 0
+
+
+def decode_attn_prepare_rows(shape: Shape, q, k, v, slots=None, positions=None, cos_sin=None, q_out=None, k_out=None,
+                             k_cache=None, v_cache=None, q_weight=None, k_weight=None, eps: float = 1e-6,
+                             interleaved: bool = False, cache_bits: int = 16, rows: Optional[int] = None, status=None,
+                             stream=None, check: bool = True) -> int:
+    """q, k, v: 16-bit [rows, heads, head_dim], the heads of a row contiguous, rows any stride (slices of one projection);
+    slots: int64 [rows]; positions: int32 [rows]; cos_sin: fp32 [positions, rotary_dim]; q_out, k_out like q and k;
+    q_weight, k_weight: [head_dim] or [heads, head_dim]; cache_bits 4: k_cache is the pool in 4 bits.  rows: the first so
+    many (default: all)."""
+    import torch
+    dtype = torch.float16 if shape.kv_dtype == DA_DTYPE_FP16 else torch.bfloat16
+    hq, hkv, d = shape.num_q_heads, shape.num_kv_heads, shape.head_dim
+    if rows is None:
+        rows = (q if q is not None else k).shape[0]
+    if (slots is not None and (slots.dtype is not torch.int64 or slots.numel() < rows or not slots.is_contiguous())) or \
+            (positions is not None and (positions.dtype is not torch.int32 or positions.numel() < rows or
+                                        not positions.is_contiguous())) or \
+            (cos_sin is not None and (cos_sin.dtype is not torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous())) or \
+            (status is not None and status.dtype is not torch.int32):
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_prepare_rows")
+    a = RowsArgs()
+    a.struct_size = _ROWS_ARGS_SIZE
+    a.rows, a.cache_bits, a.interleaved, a.eps = rows, cache_bits, interleaved, eps
+    a.q, a.q_stride = _heads(q, rows, hq, d, dtype)
+    a.k, a.k_stride = _heads(k, rows, hkv, d, dtype)
+    a.v, a.v_stride = _heads(v, rows, hkv, d, dtype)
+    a.q_out, a.q_out_stride = _heads(q_out, rows, hq, d, dtype)
+    a.k_out, a.k_out_stride = _heads(k_out, rows, hkv, d, dtype)
+    a.q_weight, a.q_weight_stride = _head_weight(q_weight, hq, d, dtype)
+    a.k_weight, a.k_weight_stride = _head_weight(k_weight, hkv, d, dtype)
+    if cos_sin is not None:
+        a.cos_sin, a.max_positions, a.rotary_dim = cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
+    a.positions, a.slots = _ptr(positions), _ptr(slots)
+    a.k_cache, a.v_cache, a.status = _ptr(k_cache), _ptr(v_cache), _ptr(status)
+    rc = _lib.decode_attn_prepare_rows(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
+    if check:
+        _check(rc, "decode_attn_prepare_rows")
+    return rc
+
+
+def decode_attn_step_tables(shape: Shape, seq_lens, gains, seq_lens_out, block_table, free_pages, free_count, free_count_out,
+                            row_starts, page_starts, slots, positions, row_seq=None, status=None, stream=None,
+                            check: bool = True) -> int:
+    """All int32 but slots (int64), contiguous: seq_lens, gains, seq_lens_out [batch]; block_table [batch, pages];
+    free_pages [capacity]; free_count, free_count_out [1]; row_starts, page_starts [batch + 1]; slots, positions, row_seq
+    [max_rows]; status [1] or None.  seq_lens_out may be seq_lens, free_count_out free_count."""
+    import torch
+    i32, batch, where = torch.int32, shape.batch, "decode_attn_step_tables"
+    max_rows = slots.numel()
+    for x, need in ((seq_lens, batch), (gains, batch), (seq_lens_out, batch), (block_table, batch * shape.max_pages_per_seq),
+                    (free_pages, 0), (free_count, 1), (free_count_out, 1), (row_starts, batch + 1), (page_starts, batch + 1),
+                    (positions, max_rows), (row_seq, max_rows), (status, 1)):
+        if x is not None and (x.dtype is not i32 or x.numel() < need or not x.is_contiguous()):
+            raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
+    if slots.dtype is not torch.int64 or not slots.is_contiguous():
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
+    a = TablesArgs()
+    a.struct_size = _TABLES_ARGS_SIZE
+    a.max_rows, a.free_capacity = max_rows, free_pages.numel()
+    a.seq_lens, a.gains, a.seq_lens_out = _ptr(seq_lens), _ptr(gains), _ptr(seq_lens_out)
+    a.block_table, a.free_pages = _ptr(block_table), _ptr(free_pages)
+    a.free_count, a.free_count_out = _ptr(free_count), _ptr(free_count_out)
+    a.row_starts, a.page_starts = _ptr(row_starts), _ptr(page_starts)
+    a.slots, a.positions, a.row_seq, a.status = _ptr(slots), _ptr(positions), _ptr(row_seq), _ptr(status)
+    rc = _lib.decode_attn_step_tables(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
+    if check:
+        _check(rc, where)
+    return rc
 
 
 def decode_attn_last_device_status(plan: Optional[Plan], stream=None) -> int:

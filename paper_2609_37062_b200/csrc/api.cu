@@ -16,6 +16,7 @@
 #include "common.cuh"
 #include "decode_attn.h"
 #include "kernel_mma_launch.cuh"
+#include "kernel_packed.h"
 #include "kernel_umma_launch.cuh"
 #include "kernel_simt.cuh"
 #include "planner.h"
@@ -236,6 +237,7 @@ int pick_kernel(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
 {
     if (p.kernel != DA_KERNEL_AUTO) return p.kernel;
     const int G = s.num_q_heads / s.num_kv_heads;
+    if (p.cache_bits == 4) return DA_KERNEL_PACKED;
     if (p.shared_prefix_tokens > 0 && umma_supports(s.head_dim, G)) return DA_KERNEL_UMMA_PREFIX;
     // The TMA-fed kernel wins at every group size, group 1 included (no reuse for the tensor core
     // there, but the stream is what counts: 7.1 against 5.1 TB/s on 1 GB of MHA cache).
@@ -258,6 +260,7 @@ int query_occupancy_uncached(int kernel, int D, int G, int* block_threads, int* 
         }
         return n;
     }
+    if (kernel == DA_KERNEL_PACKED) return packed_query_occupancy(D, G, ext, block_threads, dyn_smem);
     return mma_query_occupancy(D, G, block_threads, dyn_smem, prefix, false, ext);
 }
 
@@ -493,7 +496,14 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
 {
     if (!shape || !policy || !plan_out) return DA_ERR_INVALID_ARG;
     if (shape->batch > 0 && !seq_lens_host) return DA_ERR_INVALID_ARG;
-    int rc = validate_shape(*shape);
+    int rc = DA_OK;
+    decode_attn_shape_t packed;
+    if (policy->cache_bits == 4) {
+        rc = packed_shape(*shape, &packed);
+        if (rc != DA_OK) return rc;
+        shape = &packed;
+    }
+    rc = validate_shape(*shape);
     if (rc != DA_OK) return rc;
     rc = validate_policy(*shape, *policy);
     if (rc != DA_OK) return rc;
@@ -533,7 +543,7 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
     const bool prefix = policy->shared_prefix_tokens > 0;
     if (prefix && pl->kernel == DA_KERNEL_SIMT) return DA_ERR_UNSUPPORTED;
     // what follows a tcgen05 prefix runs on the ordinary tensor-core kernel
-    int occ = query_occupancy(DA_KERNEL_MMA_TMA == pl->kernel || umma ? DA_KERNEL_MMA_TMA : pl->kernel, shape->head_dim,
+    int occ = query_occupancy(umma ? DA_KERNEL_MMA_TMA : pl->kernel, shape->head_dim,
                               pl->group, &pl->block_threads, &pl->dyn_smem, prefix && !umma,
                               policy->window_tokens > 0 || policy->track_weights);
     if (occ <= 0) return DA_ERR_CUDA;
@@ -715,7 +725,9 @@ static int run_impl(const decode_attn_plan_t* pl, const decode_attn_run_args_t* 
         if (pl->kernel != DA_KERNEL_MMA_TMA || pl->policy.shared_prefix_tokens > 0) return DA_ERR_UNSUPPORTED;
     }
     if (pl->shape.batch == 0 && pl->policy.capacity_batch == 0) return DA_OK;
-    if (!a->q || !a->k_cache || !a->v_cache || !a->block_table || !a->seq_lens || !a->out) return DA_ERR_INVALID_ARG;
+    // (a cache in 4 bits is one pool of K and V)
+    if (!a->q || !a->k_cache || (pl->kernel == DA_KERNEL_PACKED) != (a->v_cache == nullptr) || !a->block_table || !a->seq_lens || !a->out)
+        return DA_ERR_INVALID_ARG;
     if (!aligned(a->q, 16) || !aligned(a->k_cache, 16) || !aligned(a->v_cache, 16) || !aligned(a->out, 16) ||
         !aligned(a->block_table, 4) || !aligned(a->seq_lens, 4))
         return DA_ERR_INVALID_ARG;
@@ -731,7 +743,7 @@ static int run_impl(const decode_attn_plan_t* pl, const decode_attn_run_args_t* 
     }
     KernelParams kp = make_params(pl, *a);
     if (debug_limit > 0) {
-        if (pl->kernel != DA_KERNEL_MMA_TMA) return DA_ERR_UNSUPPORTED;
+        if (pl->kernel != DA_KERNEL_MMA_TMA && pl->kernel != DA_KERNEL_PACKED) return DA_ERR_UNSUPPORTED;
         kp.wait_limit = debug_limit;
         kp.debug_drop_loads = 1;
         kp.hint_first_pages = 0;
@@ -740,6 +752,9 @@ static int run_impl(const decode_attn_plan_t* pl, const decode_attn_run_args_t* 
         simt_kernel_t fn = simt_kernel_for(pl->shape.head_dim, pl->group);
         if (!fn) return DA_ERR_UNSUPPORTED;
         int rc = simt_launch(fn, kp, (unsigned)pl->grid, stream);
+        if (rc != DA_OK) return rc;
+    } else if (pl->kernel == DA_KERNEL_PACKED) {
+        int rc = packed_launch(pl->shape, pl->group, kp, (unsigned)pl->grid, stream);
         if (rc != DA_OK) return rc;
     } else {
         const unsigned n_front = (unsigned)pl->layout.n_front_units;
@@ -1087,7 +1102,7 @@ int decode_attn_debug_gather(const decode_attn_plan_t* pl, int32_t seq, const vo
 {
     if (!pl || !k_cache || !v_cache || !block_table || !k_out || !v_out) return DA_ERR_INVALID_ARG;
     if (seq < 0 || seq >= pl->shape.batch) return DA_ERR_INVALID_ARG;
-    if (pl->policy.shared_prefix_tokens > 0 || pl->policy.window_tokens > 0) return DA_ERR_UNSUPPORTED;
+    if (pl->policy.shared_prefix_tokens > 0 || pl->policy.window_tokens > 0 || pl->kernel == DA_KERNEL_PACKED) return DA_ERR_UNSUPPORTED;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(k_out, 16) || !aligned(v_out, 16))
         return DA_ERR_INVALID_ARG;
     if (pl->grid == 0) return DA_OK;
@@ -1106,7 +1121,7 @@ int decode_attn_gather_probe(const decode_attn_plan_t* pl, const void* k_cache, 
 {
     if (!pl || !k_cache || !v_cache || !block_table || !checksum_out) return DA_ERR_INVALID_ARG;
     if (!aligned(k_cache, 16) || !aligned(v_cache, 16)) return DA_ERR_INVALID_ARG;
-    if (pl->policy.shared_prefix_tokens > 0 || pl->policy.window_tokens > 0) return DA_ERR_UNSUPPORTED;
+    if (pl->policy.shared_prefix_tokens > 0 || pl->policy.window_tokens > 0 || pl->kernel == DA_KERNEL_PACKED) return DA_ERR_UNSUPPORTED;
     if (pl->grid == 0) return DA_OK;
     decode_attn_run_args_t a;
     std::memset(&a, 0, sizeof a);
@@ -1176,6 +1191,7 @@ int decode_attn_append_kv_checked(const decode_attn_plan_t* pl, const void* new_
                                   cudaStream_t stream)
 {
     if (!pl) return DA_ERR_INVALID_ARG;
+    if (pl->kernel == DA_KERNEL_PACKED) return DA_ERR_UNSUPPORTED;
     int rc = order_behind_upload(pl, stream);      // the upload also zeroes the status word this launch may write
     if (rc != DA_OK) return rc;
     rc = append_impl(&pl->shape, reinterpret_cast<int32_t*>(pl->dev + pl->off_status), new_k, new_v, block_table,
@@ -1220,6 +1236,7 @@ int decode_attn_host_step(const decode_attn_shape_t* shape, const decode_attn_po
         !out_host || pool_elems <= 0)
         return DA_ERR_INVALID_ARG;
     if (policy->capacity_batch != 0) return DA_ERR_INVALID_ARG;
+    if (policy->cache_bits == 4) return DA_ERR_UNSUPPORTED;
     int rc = validate_pages(shape, seq_lens_host, block_table_host, policy->window_tokens, policy->sink_tokens);
     if (rc != DA_OK) return rc;
     if (shape->batch == 0) return DA_OK;
@@ -1289,6 +1306,7 @@ const char* decode_attn_strerror(int status)
         case DA_ERR_CUDA: return "CUDA call failed or no CUDA device";
         case DA_ERR_BAD_PAGE: return "block table refers to a page outside the pool";
         case DA_ERR_TIMEOUT: return "a bounded device-side wait gave up";
+        case DA_ERR_NO_PAGES: return "the list of free pages is too short";
         default: return "unknown status";
     }
 }

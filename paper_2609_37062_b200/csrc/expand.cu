@@ -1,0 +1,184 @@
+// Pages of a cache in 4 bits to 16-bit pages (decode_attn_expand_kv).
+//
+// Bound by memory: 4.5 bits read and 16 written a value.  A warp takes one tile of one KV head; 16 lanes (8 at head_dim
+// 64) write a row of K or V whole, 16 bytes a lane, from one word of codes each.  All loads of the tile are asked for before
+// the first value is used.
+#include <cstring>
+
+#include "common.cuh"
+#include "packed.cuh"
+#include "planner.h"
+
+using namespace da;
+
+namespace {
+
+constexpr int kExpandThreads = 256;
+constexpr int kExpandTiles = 8;        // tiles of a sequence that a block takes, all KV heads of them
+
+struct ExpandParams {
+    const char* pool;
+    const int32_t *block_table, *seq_lens, *dst_table;
+    uint16_t *k, *v;
+    int32_t* status;
+    int64_t src_stride_page, src_stride_head, src_pages, num_pages;
+    int64_t k_stride_page, k_stride_token, k_stride_head;
+    int64_t v_stride_page, v_stride_token, v_stride_head;
+    int32_t num_kv_heads, src_width, dst_width, page_shift;
+};
+
+template <bool F16>
+__device__ __forceinline__ uint32_t round_pair(float lo, float hi)
+{
+    if (F16) {
+        const __half2 h = __floats2half2_rn(lo, hi);
+        return *reinterpret_cast<const uint32_t*>(&h);
+    }
+    const __nv_bfloat162 h = __floats2bfloat162_rn(lo, hi);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+
+template <bool F16>
+__device__ __forceinline__ uint4 expand_word(uint32_t w, __half scale)
+{
+    uint32_t c[4], r[4];
+    packed_unpack(w, c);
+    const float s = __half2float(scale);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&c[i]));
+        r[i] = round_pair<F16>(f.x * s, f.y * s);             // (the products are exact: 2 and 11 significant bits)
+    }
+    return make_uint4(r[0], r[1], r[2], r[3]);
+}
+
+template <int D, bool F16>
+__global__ void __launch_bounds__(kExpandThreads) decode_attn_expand_kernel(const ExpandParams p)
+{
+    constexpr int L = D / 8;                                  // lanes of a row
+    constexpr int STEP = 32 / L;                              // rows at a time
+    constexpr int N = 16 / STEP;
+    pdl_launch_dependents();
+    pdl_wait_primary();
+    const int b = blockIdx.y, lane = threadIdx.x & 31;
+    const int len = __ldg(p.seq_lens + b);
+    const int64_t fits = (int64_t)(p.src_width < p.dst_width ? p.src_width : p.dst_width) << p.page_shift;
+    if (len < 0 || len > fits) {
+        if (blockIdx.x == 0 && threadIdx.x == 0 && p.status != nullptr) record_status(p.status, DA_ERR_STALE_PLAN);
+        return;
+    }
+    const int n_tiles = (len + 15) >> 4;
+    const int tile0 = blockIdx.x * kExpandTiles;
+    for (int i = threadIdx.x >> 5; i < kExpandTiles * p.num_kv_heads; i += kExpandThreads / 32) {
+        const int tile = tile0 + i / p.num_kv_heads, head = i % p.num_kv_heads;
+        if (tile >= n_tiles) break;
+        const int page_at = tile >> (p.page_shift - 4), in_page = tile & ((1 << (p.page_shift - 4)) - 1);
+        const int src_page = __ldg(p.block_table + (int64_t)b * p.src_width + page_at);
+        const int dst_page = __ldg(p.dst_table + (int64_t)b * p.dst_width + page_at);
+        if ((unsigned)src_page >= (unsigned)p.src_pages || (unsigned)dst_page >= (unsigned)p.num_pages) {
+            if (lane == 0 && p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
+            continue;
+        }
+        const char* const src = p.pool + src_page * p.src_stride_page + head * p.src_stride_head + in_page * packed_tile_bytes(D);
+        const uint32_t* const kc = reinterpret_cast<const uint32_t*>(src);
+        const uint32_t* const vc = reinterpret_cast<const uint32_t*>(src + packed_v_codes(D));
+        const __half* const ks = reinterpret_cast<const __half*>(src + packed_k_scales(D));
+        const __half* const vs = reinterpret_cast<const __half*>(src + packed_v_scales(D));
+        const int l = lane % L, r0 = lane / L;
+        const int rows = min(16, len - tile * 16);
+        uint32_t kw[N], vw[N];
+        __half kf[N], vf[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int r = j * STEP + r0;
+            kw[j] = __ldg(kc + packed_k_word(D, r, l));
+            vw[j] = __ldg(vc + packed_v_word(D, r, l));
+            kf[j] = __ldg(ks + packed_k_scale(D, r, l >> 2));
+            vf[j] = __ldg(vs + packed_v_scale(r, l >> 2));
+        }
+        uint16_t* const kd = p.k + dst_page * p.k_stride_page + (in_page * 16) * p.k_stride_token + head * p.k_stride_head + 8 * l;
+        uint16_t* const vd = p.v + dst_page * p.v_stride_page + (in_page * 16) * p.v_stride_token + head * p.v_stride_head + 8 * l;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int r = j * STEP + r0;
+            if (r < rows) {
+                *reinterpret_cast<uint4*>(kd + r * p.k_stride_token) = expand_word<F16>(kw[j], kf[j]);
+                *reinterpret_cast<uint4*>(vd + r * p.v_stride_token) = expand_word<F16>(vw[j], vf[j]);
+            }
+        }
+    }
+}
+
+bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+}  // namespace
+
+extern "C" int64_t decode_attn_packed_head_bytes(int32_t head_dim, int32_t page_size)
+{
+    if (head_dim != 64 && head_dim != 128) return 0;
+    if (page_size < 16 || page_size > 256 || (page_size & (page_size - 1)) != 0) return 0;
+    return (int64_t)(page_size / 16) * packed_tile_bytes(head_dim);
+}
+
+extern "C" int decode_attn_expand_kv(const decode_attn_shape_t* shape, const decode_attn_shape_t* from, const void* pool,
+                                     const int32_t* block_table, const int32_t* seq_lens, const int32_t* dst_block_table,
+                                     void* k_cache, void* v_cache, int32_t* status_or_null, cudaStream_t stream)
+{
+    if (!shape || !from) return DA_ERR_INVALID_ARG;
+    int rc = validate_shape(*shape);
+    if (rc != DA_OK) return rc;
+    decode_attn_shape_t f;
+    rc = packed_shape(*from, &f);
+    if (rc == DA_OK) rc = validate_shape(f);
+    if (rc != DA_OK) return rc;
+    const decode_attn_shape_t& s = *shape;
+    if (f.batch != s.batch || f.num_kv_heads != s.num_kv_heads || f.head_dim != s.head_dim || f.page_size != s.page_size)
+        return DA_ERR_INVALID_ARG;
+    const int width = s.max_pages_per_seq < f.max_pages_per_seq ? s.max_pages_per_seq : f.max_pages_per_seq;
+    if (s.batch == 0 || width == 0) return DA_OK;
+    if (!pool || !block_table || !seq_lens || !dst_block_table || !k_cache || !v_cache) return DA_ERR_INVALID_ARG;
+    if (!aligned(pool, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(block_table, 4) || !aligned(seq_lens, 4) ||
+        !aligned(dst_block_table, 4) || !aligned(status_or_null, 4))
+        return DA_ERR_INVALID_ARG;
+    if (s.batch > 65535) return DA_ERR_UNSUPPORTED;
+    ExpandParams p;
+    std::memset(&p, 0, sizeof p);
+    p.pool = static_cast<const char*>(pool);
+    p.block_table = block_table;
+    p.seq_lens = seq_lens;
+    p.dst_table = dst_block_table;
+    p.k = static_cast<uint16_t*>(k_cache);
+    p.v = static_cast<uint16_t*>(v_cache);
+    p.status = status_or_null;
+    p.src_stride_page = f.k_stride_page;
+    p.src_stride_head = f.k_stride_head;
+    p.src_pages = f.num_pages;
+    p.num_pages = s.num_pages;
+    p.k_stride_page = s.k_stride_page; p.k_stride_token = s.k_stride_token; p.k_stride_head = s.k_stride_head;
+    p.v_stride_page = s.v_stride_page; p.v_stride_token = s.v_stride_token; p.v_stride_head = s.v_stride_head;
+    p.num_kv_heads = s.num_kv_heads;
+    p.src_width = f.max_pages_per_seq;
+    p.dst_width = s.max_pages_per_seq;
+    while ((1 << p.page_shift) < s.page_size) ++p.page_shift;
+    const int64_t tiles = (int64_t)width * (s.page_size / 16);
+    const int64_t blocks = (tiles + kExpandTiles - 1) / kExpandTiles;
+    if (blocks > 0x7fffffffLL || tiles * 16 > INT32_MAX) return DA_ERR_UNSUPPORTED;
+    const bool f16 = s.kv_dtype == DA_DTYPE_FP16;
+    auto fn = s.head_dim == 128 ? (f16 ? decode_attn_expand_kernel<128, true> : decode_attn_expand_kernel<128, false>)
+                                : (f16 ? decode_attn_expand_kernel<64, true> : decode_attn_expand_kernel<64, false>);
+    cudaLaunchConfig_t cfg;
+    cfg.gridDim = dim3((unsigned)blocks, (unsigned)s.batch, 1);
+    cfg.blockDim = dim3(kExpandThreads, 1, 1);
+    cfg.dynamicSmemBytes = 0;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    if (cudaLaunchKernelEx(&cfg, fn, p) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return DA_ERR_CUDA;
+    }
+    return DA_OK;
+}

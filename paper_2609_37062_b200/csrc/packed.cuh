@@ -1,0 +1,51 @@
+// Conversions of the cache in 4 bits (packed.h): codes in e2m1 to fp16 pairs and back.
+#pragma once
+
+#include <cuda_fp16.h>
+
+#include "packed.h"
+
+namespace da {
+
+// The 8 codes of a word as four fp16 pairs (exact: every magnitude has two significant bits).  The instruction runs at
+// about half the rate of an fp16 multiplication.
+__device__ __forceinline__ void packed_unpack(uint32_t w, uint32_t (&r)[4])
+{
+    asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+        "mov.b32 {b0, b1, b2, b3}, %4;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %0, b0;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %1, b1;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %2, b2;\n\t"
+        "cvt.rn.f16x2.e2m1x2 %3, b3;\n\t}"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3])
+        : "r"(w));
+}
+
+// The scale of 32 values whose largest magnitude is amax: amax / 6 in fp16, finite.
+__device__ __forceinline__ __half packed_scale(float amax) { return __float2half_rn(fminf(__fdiv_rn(amax, 6.0f), 65504.0f)); }
+
+// Two codes from a value's quotients: nearest, ties to the even code, at most 6.
+__device__ __forceinline__ uint32_t packed_pair(float lo, float hi)
+{
+    uint32_t r;
+    asm("{\n\t.reg .b8 b;\n\t"
+        "cvt.rn.satfinite.e2m1x2.f32 b, %2, %1;\n\t"
+        "cvt.u32.u8 %0, b;\n\t}"
+        : "=r"(r)
+        : "f"(lo), "f"(hi));
+    return r;
+}
+
+// Eight codes of the values x, whose block has the scale s.  The quotients are IEEE divisions: the codes are those of the
+// definition, not of an approximation.
+__device__ __forceinline__ uint32_t packed_word(const float (&x)[8], __half s)
+{
+    const float f = __half2float(s);
+    if (f == 0.f) return 0u;
+    uint32_t w = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w |= packed_pair(__fdiv_rn(x[2 * i], f), __fdiv_rn(x[2 * i + 1], f)) << (8 * i);
+    return w;
+}
+
+}  // namespace da

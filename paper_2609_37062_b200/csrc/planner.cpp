@@ -22,6 +22,7 @@
 //    neighbouring addresses of the same pages.
 #include "planner.h"
 
+#include "packed.h"
 #include "window.h"
 
 #include <algorithm>
@@ -60,6 +61,20 @@ int validate_shape(const decode_attn_shape_t& s)
     return DA_OK;
 }
 
+int packed_shape(const decode_attn_shape_t& s, decode_attn_shape_t* out)
+{
+    *out = s;
+    out->k_stride_token = out->v_stride_page = out->v_stride_token = out->v_stride_head = 256;
+    if (s.k_stride_page <= 0 || s.k_stride_head <= 0 || s.k_stride_page % 16 != 0 || s.k_stride_head % 16 != 0) return DA_ERR_INVALID_ARG;
+    if ((s.head_dim != 64 && s.head_dim != 128) || s.page_size < 16 || s.num_kv_heads < 1 || s.num_pages < 1) return DA_OK;
+    const int64_t bytes = (int64_t)(s.page_size / kTileTokens) * packed_tile_bytes(s.head_dim);
+    if (s.k_stride_page < bytes || s.k_stride_head < bytes) return DA_ERR_INVALID_ARG;
+    // heads within pages, or pages within heads: two of them never share bytes
+    const __int128 sp = s.k_stride_page, sh = s.k_stride_head;
+    if (sp < (s.num_kv_heads - 1) * sh + bytes && sh < (s.num_pages - 1) * sp + bytes) return DA_ERR_INVALID_ARG;
+    return DA_OK;
+}
+
 bool totals_apart(int64_t tokens, int64_t stride_seq, int64_t stride_head, int64_t batch, int64_t num_kv_heads)
 {
     if ((batch > 1 && stride_seq < tokens) || (num_kv_heads > 1 && stride_head < tokens)) return false;
@@ -80,7 +95,7 @@ bool totals_apart(int64_t tokens, int64_t stride_seq, int64_t stride_head, int64
 int validate_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
 {
     if (p.split_mode < DA_SPLIT_AUTO || p.split_mode > DA_SPLIT_DETERMINISTIC) return DA_ERR_INVALID_ARG;
-    if (p.kernel < DA_KERNEL_AUTO || p.kernel > DA_KERNEL_UMMA_PREFIX) return DA_ERR_INVALID_ARG;
+    if (p.kernel < DA_KERNEL_AUTO || p.kernel > DA_KERNEL_PACKED) return DA_ERR_INVALID_ARG;
     if (p.split_mode == DA_SPLIT_FIXED_COUNT && p.fixed_count < 1) return DA_ERR_INVALID_ARG;
     if (p.chunk_tokens < 0 || p.max_splits < 0 || p.sm_count < 0 || p.ctas_per_sm < 0 ||
         p.capacity_batch < 0 || p.capacity_tokens < 0)
@@ -97,6 +112,8 @@ int validate_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
         const int G = s.num_q_heads / s.num_kv_heads;
         if (p.kernel == DA_KERNEL_UMMA_PREFIX) {
             if (s.head_dim != 128) return DA_ERR_UNSUPPORTED;
+        } else if (p.kernel == DA_KERNEL_PACKED) {
+            return DA_ERR_UNSUPPORTED;
         } else if (p.kernel == DA_KERNEL_SIMT || G > 4) {
             return DA_ERR_UNSUPPORTED;
         }
@@ -107,6 +124,9 @@ int validate_policy(const decode_attn_shape_t& s, const decode_attn_policy_t& p)
     if (p.track_weights != 0 && p.track_weights != 1) return DA_ERR_INVALID_ARG;
     if ((p.window_tokens > 0 || p.track_weights) && (p.shared_prefix_tokens > 0 || p.kernel == DA_KERNEL_SIMT))
         return DA_ERR_UNSUPPORTED;
+    if (p.cache_bits != 0 && p.cache_bits != 16 && p.cache_bits != 4) return DA_ERR_INVALID_ARG;
+    if ((p.cache_bits == 4) != (p.kernel == DA_KERNEL_PACKED) && (p.kernel != DA_KERNEL_AUTO)) return DA_ERR_UNSUPPORTED;
+    if (p.cache_bits == 4 && (p.shared_prefix_tokens > 0 || p.track_weights)) return DA_ERR_UNSUPPORTED;
     for (int32_t r : p.reserved)
         if (r != 0) return DA_ERR_INVALID_ARG;
     return DA_OK;
@@ -509,7 +529,14 @@ extern "C" int decode_attn_plan_layout(const decode_attn_shape_t* shape, const d
                                        int32_t* chunk_tokens_out)
 {
     if (!shape || !policy) return DA_ERR_INVALID_ARG;
-    int rc = da::validate_shape(*shape);
+    int rc = DA_OK;
+    decode_attn_shape_t packed;
+    if (policy->cache_bits == 4) {
+        rc = da::packed_shape(*shape, &packed);
+        if (rc != DA_OK) return rc;
+        shape = &packed;
+    }
+    rc = da::validate_shape(*shape);
     if (rc != DA_OK) return rc;
     rc = da::validate_policy(*shape, *policy);
     if (rc != DA_OK) return rc;

@@ -44,6 +44,9 @@ struct Layout {
 
 // Validates the fields the planner and the kernels rely on.
 int validate_shape(const decode_attn_shape_t& s);
+// The shape of a cache in 4 bits as everything that plans sees it: checks its two strides (bytes) and fills in the four that
+// do not apply.  What it leaves to validate_shape fails there.
+int packed_shape(const decode_attn_shape_t& s, decode_attn_shape_t* out);
 // Do the rows of totals of different sequences and KV heads lie apart?  Row (b, g) is the `tokens` values from
 // b * stride_seq + g * stride_head on; the stride of a single sequence, or of a single head, does not matter.
 bool totals_apart(int64_t tokens, int64_t stride_seq, int64_t stride_head, int64_t batch, int64_t num_kv_heads);

@@ -34,7 +34,7 @@ int validate_prompt_policy(const decode_attn_shape_t& s, const decode_attn_polic
     const int rc = validate_policy(s, p);
     if (rc != DA_OK) return rc;
     if (p.split_mode == DA_SPLIT_FIXED_COUNT || p.kernel != DA_KERNEL_AUTO || p.fuse_combine || p.capacity_batch > 0 ||
-        p.shared_prefix_tokens > 0 || p.track_weights || p.max_splits > 0 || p.ctas_per_sm > 0)
+        p.shared_prefix_tokens > 0 || p.track_weights || p.cache_bits == 4 || p.max_splits > 0 || p.ctas_per_sm > 0)
         return DA_ERR_UNSUPPORTED;
     if (p.split_mode == DA_SPLIT_DETERMINISTIC && p.chunk_tokens % kPromptKvTokens != 0) return DA_ERR_INVALID_ARG;
     return DA_OK;
