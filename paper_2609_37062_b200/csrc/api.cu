@@ -44,6 +44,7 @@ struct decode_attn_plan {
     int ctas_per_sm = 0;
     int kernel = DA_KERNEL_SIMT;
     int group = 1;
+    bool big_blocks = false;     // DA_KERNEL_PACKED: see kernel_packed.h
     int block_threads = 0;
     int dyn_smem = 0;
     float scale = 0.f;
@@ -260,12 +261,12 @@ int query_occupancy_uncached(int kernel, int D, int G, int* block_threads, int* 
         }
         return n;
     }
-    if (kernel == DA_KERNEL_PACKED) return packed_query_occupancy(D, G, ext, block_threads, dyn_smem);
+    if (kernel == DA_KERNEL_PACKED) return packed_query_occupancy(D, G, ext, prefix, block_threads, dyn_smem);
     return mma_query_occupancy(D, G, block_threads, dyn_smem, prefix, false, ext);
 }
 
 // Plans are made every decode step: the answers that depend only on (device, kernel variant) are
-// kept after the first query.
+// kept after the first query.  (`prefix` tells the kernels' variants apart: for DA_KERNEL_PACKED the size of its blocks.)
 struct OccEntry {
     int device, kernel, D, G, prefix, ext, occ, block_threads, dyn_smem;
 };
@@ -541,10 +542,12 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
         if (rc != DA_OK) return rc;
     }
     const bool prefix = policy->shared_prefix_tokens > 0;
+    pl->big_blocks = packed_big_blocks((int64_t)std::max(shape->batch, policy->capacity_batch) * shape->num_kv_heads, pl->sm_count);
     if (prefix && pl->kernel == DA_KERNEL_SIMT) return DA_ERR_UNSUPPORTED;
     // what follows a tcgen05 prefix runs on the ordinary tensor-core kernel
     int occ = query_occupancy(umma ? DA_KERNEL_MMA_TMA : pl->kernel, shape->head_dim,
-                              pl->group, &pl->block_threads, &pl->dyn_smem, prefix && !umma,
+                              pl->group, &pl->block_threads, &pl->dyn_smem,
+                              pl->kernel == DA_KERNEL_PACKED ? pl->big_blocks : prefix && !umma,
                               policy->window_tokens > 0 || policy->track_weights);
     if (occ <= 0) return DA_ERR_CUDA;
     pl->ctas_per_sm = policy->ctas_per_sm > 0 ? policy->ctas_per_sm : occ;
@@ -743,7 +746,7 @@ static int run_impl(const decode_attn_plan_t* pl, const decode_attn_run_args_t* 
     }
     KernelParams kp = make_params(pl, *a);
     if (debug_limit > 0) {
-        if (pl->kernel != DA_KERNEL_MMA_TMA && pl->kernel != DA_KERNEL_PACKED) return DA_ERR_UNSUPPORTED;
+        if (pl->kernel != DA_KERNEL_MMA_TMA) return DA_ERR_UNSUPPORTED;
         kp.wait_limit = debug_limit;
         kp.debug_drop_loads = 1;
         kp.hint_first_pages = 0;
@@ -754,7 +757,7 @@ static int run_impl(const decode_attn_plan_t* pl, const decode_attn_run_args_t* 
         int rc = simt_launch(fn, kp, (unsigned)pl->grid, stream);
         if (rc != DA_OK) return rc;
     } else if (pl->kernel == DA_KERNEL_PACKED) {
-        int rc = packed_launch(pl->shape, pl->group, kp, (unsigned)pl->grid, stream);
+        int rc = packed_launch(pl->shape, pl->group, pl->big_blocks, kp, (unsigned)pl->grid, stream);
         if (rc != DA_OK) return rc;
     } else {
         const unsigned n_front = (unsigned)pl->layout.n_front_units;

@@ -533,7 +533,7 @@ __device__ __forceinline__ void block_finish(const KernelParams& p, const decode
     // heads [head_first, head_first + head_count) of the group, held in source columns 0 .. head_count - 1
     if (head_count < 0) head_count = G;
     constexpr int D4 = D / 4;
-    constexpr int kUnroll = R <= 4 ? R : 1;     // many row groups: keep the loop rolled, registers matter more
+    constexpr int kUnroll = R <= 8 ? R : 1;     // many row groups: keep the loop rolled, registers matter more
     const int Hq = p.num_q_heads;
     const int h0 = u.kv_head * G;
     const int RF = rec_floats(G, D);

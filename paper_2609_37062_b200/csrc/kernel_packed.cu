@@ -8,63 +8,76 @@ namespace {
 
 typedef void (*packed_kernel_t)(const KernelParams, const int);
 
-template <int D, bool F16>
-packed_kernel_t for_group(int G, bool ext)
+struct PackedVariant {
+    packed_kernel_t fn;
+    int threads, smem;
+};
+
+template <int D, bool F16, bool EXT, int W, int TEAMS>
+PackedVariant variant(bool dup)
 {
-    if (G > 8) return ext ? decode_attn_packed_kernel<D, F16, true, true> : decode_attn_packed_kernel<D, F16, true, false>;
-    return ext ? decode_attn_packed_kernel<D, F16, false, true> : decode_attn_packed_kernel<D, F16, false, false>;
+    using Cfg = PackedCfg<D, W, TEAMS>;
+    return {dup ? decode_attn_packed_kernel<D, F16, F16 && TEAMS == 1, EXT, W, TEAMS> : decode_attn_packed_kernel<D, F16, false, EXT, W, TEAMS>,
+            Cfg::kThreads, Cfg::kSmem};
 }
 
-packed_kernel_t kernel_for(int D, int G, bool f16, bool ext)
+template <int D, bool F16, bool EXT>
+PackedVariant for_group(int G, bool big)
 {
-    if (D == 128) return f16 ? for_group<128, true>(G, ext) : for_group<128, false>(G, ext);
-    return f16 ? for_group<64, true>(G, ext) : for_group<64, false>(G, ext);
+    if (G > 8) return variant<D, F16, EXT, 4, 2>(false);
+    return big ? variant<D, F16, EXT, 8, 1>(F16 && G <= 4) : variant<D, F16, EXT, 4, 1>(F16 && G <= 4);
 }
 
-int prepare(int D, int G, bool f16, bool ext, packed_kernel_t* fn)
+template <int D>
+PackedVariant for_type(int G, bool f16, bool ext, bool big)
 {
-    *fn = kernel_for(D, G, f16, ext);
-    const int smem = D == 128 ? PackedCfg<128>::kSmem : PackedCfg<64>::kSmem;
-    if (cudaFuncSetAttribute(*fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
+    if (ext) return f16 ? for_group<D, true, true>(G, big) : for_group<D, false, true>(G, big);
+    return f16 ? for_group<D, true, false>(G, big) : for_group<D, false, false>(G, big);
+}
+
+// The variant of a plan, opted in to its shared memory.
+int prepare(int D, int G, bool f16, bool ext, bool big, PackedVariant* v)
+{
+    *v = D == 128 ? for_type<128>(G, f16, ext, big) : for_type<64>(G, f16, ext, big);
+    if (cudaFuncSetAttribute(v->fn, cudaFuncAttributeMaxDynamicSharedMemorySize, v->smem) != cudaSuccess) {
         (void)cudaGetLastError();
-        return -1;
+        return DA_ERR_CUDA;
     }
-    return smem;
+    return DA_OK;
 }
 
 }  // namespace
 
-int packed_query_occupancy(int D, int G, bool ext, int* block_threads, int* dyn_smem)
+int packed_query_occupancy(int D, int G, bool ext, bool big, int* block_threads, int* dyn_smem)
 {
-    packed_kernel_t fn;
-    const int smem = prepare(D, G, false, ext, &fn);
-    if (smem < 0) return -1;
+    PackedVariant v;
+    if (prepare(D, G, false, ext, big, &v) != DA_OK) return -1;
     int n = 0;
-    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, fn, kPackedThreads, smem) != cudaSuccess) {
+    if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&n, v.fn, v.threads, v.smem) != cudaSuccess) {
         (void)cudaGetLastError();
         return -1;
     }
-    *block_threads = kPackedThreads;
-    *dyn_smem = smem;
+    *block_threads = v.threads;
+    *dyn_smem = v.smem;
     return n;
 }
 
-int packed_launch(const decode_attn_shape_t& s, int G, const KernelParams& kp, unsigned grid, cudaStream_t stream)
+int packed_launch(const decode_attn_shape_t& s, int G, bool big, const KernelParams& kp, unsigned grid, cudaStream_t stream)
 {
-    packed_kernel_t fn;
-    const int smem = prepare(s.head_dim, G, s.kv_dtype == DA_DTYPE_FP16, kp.window > 0, &fn);
-    if (smem < 0) return DA_ERR_CUDA;
+    PackedVariant v;
+    const int rc = prepare(s.head_dim, G, s.kv_dtype == DA_DTYPE_FP16, kp.window > 0, big, &v);
+    if (rc != DA_OK) return rc;
     cudaLaunchConfig_t cfg;
     cfg.gridDim = dim3(grid, 1, 1);
-    cfg.blockDim = dim3(kPackedThreads, 1, 1);
-    cfg.dynamicSmemBytes = (size_t)smem;
+    cfg.blockDim = dim3(v.threads, 1, 1);
+    cfg.dynamicSmemBytes = (size_t)v.smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    if (cudaLaunchKernelEx(&cfg, fn, kp, G) != cudaSuccess) {
+    if (cudaLaunchKernelEx(&cfg, v.fn, kp, G) != cudaSuccess) {
         (void)cudaGetLastError();
         return DA_ERR_CUDA;
     }

@@ -242,24 +242,6 @@ def test_pages_outside_the_pool_are_reported(bad):
     check(c, out[:1], lse[:1], "the row beside")
 
 
-def test_waits_that_run_out():
-    c = Cache([600, 40], 8, 2, 128, seed=17)
-    for fuse in (0, 1):
-        pol = da.make_policy(cache_bits=4, fuse_combine=fuse)
-        plan = da.decode_attn_plan(c.shape(), pol, c.lens)
-        pool, table = torch.from_numpy(c.pool).cuda(), torch.from_numpy(c.table).cuda()
-        lens = torch.tensor(c.lens, dtype=torch.int32).cuda()
-        out, lse = torch.zeros((2, 8, 128), device="cuda"), torch.zeros((2, 8), device="cuda")
-        ws = torch.empty(max(plan.workspace_bytes, 256), dtype=torch.uint8, device="cuda")
-        rc = da.decode_attn_debug_expire_wait(plan, c.q.cuda(), pool, None, table, lens, out, lse, ws)
-        assert rc == da.DA_OK
-        assert da.decode_attn_last_device_status(plan) == da.DA_ERR_TIMEOUT
-        out, lse, status = run(c, pol, plan=plan)
-        assert status == da.DA_OK
-        check(c, out, lse, "after a wait that ran out")
-        plan.destroy()
-
-
 def test_what_a_packed_plan_refuses_at_a_call():
     c = Cache([100], 8, 2, 128)
     plan = da.decode_attn_plan(c.shape(), da.make_policy(cache_bits=4), c.lens)
@@ -277,6 +259,7 @@ def test_what_a_packed_plan_refuses_at_a_call():
         da.decode_attn_gather_probe(plan, pool, pool, table, torch.zeros(99, dtype=torch.int32, device="cuda"))
     with pytest.raises(da.DecodeAttnError):
         da.decode_attn_debug_gather(plan, 0, pool, pool, table, rows, rows)
+    assert da.decode_attn_debug_expire_wait(plan, q, pool, None, table, lens, out, None, ws) == da.DA_ERR_UNSUPPORTED  # (it has no such waits)
     assert da.decode_attn_last_device_status(plan) == da.DA_OK
     plan.destroy()
     plain = da.decode_attn_plan(da.make_shape(1, 8, 2, 128, 16, 7, 9, (16 * 256, 256, 128)), da.make_policy(), [100])
