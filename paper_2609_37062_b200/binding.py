@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -194,8 +195,8 @@ _lib.decode_attn_validate_evict.argtypes = [ctypes.POINTER(Shape), ctypes.POINTE
 _lib.decode_attn_packed_head_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
 _lib.decode_attn_packed_head_bytes.restype = ctypes.c_int64
 _lib.decode_attn_expand_kv.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(Shape)] + [_vp] * 8
-_lib.decode_attn_prepare_rows.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(RowsArgs), _vp]
-_lib.decode_attn_step_tables.argtypes = [ctypes.POINTER(Shape), ctypes.POINTER(TablesArgs), _vp]
+_lib.decode_attn_prepare_rows.argtypes = [ctypes.POINTER(Shape), _vp, _vp]
+_lib.decode_attn_step_tables.argtypes = [ctypes.POINTER(Shape), _vp, _vp]
 _lib.decode_attn_breakeven_tokens.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.c_double, ctypes.c_int32,
                                               ctypes.c_double, ctypes.POINTER(ctypes.c_double)]
 _lib.decode_attn_switch_thresholds.argtypes = [ctypes.c_double, ctypes.c_double, ctypes.POINTER(ctypes.c_double),
@@ -582,27 +583,52 @@ def decode_attn_expand_kv(shape: Shape, packed_shape: Shape, pool, block_table, 
     return rc
 
 
-_ROWS_ARGS_SIZE = ctypes.sizeof(RowsArgs)
-_TABLES_ARGS_SIZE = ctypes.sizeof(TablesArgs)
+# The argument blocks of the two calls are packed rather than filled in field by field: a structure's 28 assignments
+# cost 2 us a call, about what a launch does.
+_ROWS_PACK = struct.Struct("@IIiiiiif3P3q2P2q3P2P2q3P").pack
+_TABLES_PACK = struct.Struct("@IIii13P").pack
+_ROWS_ARGS_SIZE, _TABLES_ARGS_SIZE = ctypes.sizeof(RowsArgs), ctypes.sizeof(TablesArgs)
+_ROWS_ERROR, _TABLES_ERROR = "decode_attn_prepare_rows", "decode_attn_step_tables"
 
 
 def _heads(x, rows: int, heads: int, dim: int, dtype):
     """Address and row stride of rows of heads [rows, heads, dim] that lie behind each other within a row."""
     if x is None:
-        return None, 0
-    size, strides = x.shape, x.stride()
-    if x.dtype is not dtype or len(size) != 3 or size[0] < rows or size[1] != heads or size[2] != dim or strides[2] != 1 or \
-            (heads > 1 and strides[1] != dim):
-        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_prepare_rows")
-    return x.data_ptr(), strides[0] if size[0] > 1 else heads * dim
+        return 0, 0
+    size, (row, head, one) = x.shape, x.stride() if x.dim() == 3 else (0, 0, 0)
+    if one != 1 or x.dtype is not dtype or size[1] != heads or size[2] != dim or size[0] < rows or (head != dim and heads > 1):
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, _ROWS_ERROR)
+    return x.data_ptr(), row if size[0] > 1 else heads * dim
 
 
 def _head_weight(w, heads: int, dim: int, dtype):
     if w is None:
-        return None, 0
-    if w.dtype is not dtype or not w.is_contiguous() or w.numel() not in (dim, heads * dim) or w.shape[-1] != dim:
-        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_prepare_rows")
-    return w.data_ptr(), dim if w.dim() > 1 and w.shape[0] == heads and heads > 1 else 0
+        return 0, 0
+    size = w.shape
+    if w.dtype is not dtype or not w.is_contiguous() or (size != (dim,) and size != (heads, dim)):
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, _ROWS_ERROR)
+    return w.data_ptr(), dim if len(size) == 2 and heads > 1 else 0
+
+
+def _vector(x, dtype, need: int, where: str) -> int:
+    """Address of a contiguous tensor of at least `need` values, 0 for None."""
+    if x is None:
+        return 0
+    if x.dtype is not dtype or x.numel() < need or not x.is_contiguous():
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
+    return x.data_ptr()
+
+
+def _dtypes():
+    """(bf16, fp16, fp32, int32, int64) of torch, looked up once."""
+    global _dtypes_known
+    if _dtypes_known is None:
+        import torch
+        _dtypes_known = torch.bfloat16, torch.float16, torch.float32, torch.int32, torch.int64
+    return _dtypes_known
+
+
+_dtypes_known = None
 
 
 def decode_attn_prepare_rows(shape: Shape, q, k, v, slots=None, positions=None, cos_sin=None, q_out=None, k_out=None,
@@ -613,34 +639,30 @@ def decode_attn_prepare_rows(shape: Shape, q, k, v, slots=None, positions=None, 
     slots: int64 [rows]; positions: int32 [rows]; cos_sin: fp32 [positions, rotary_dim]; q_out, k_out like q and k;
     q_weight, k_weight: [head_dim] or [heads, head_dim]; cache_bits 4: k_cache is the pool in 4 bits.  rows: the first so
     many (default: all)."""
-    import torch
-    dtype = torch.float16 if shape.kv_dtype == DA_DTYPE_FP16 else torch.bfloat16
+    bf16, fp16, fp32, i32, i64 = _dtypes()
+    dtype = fp16 if shape.kv_dtype == DA_DTYPE_FP16 else bf16
     hq, hkv, d = shape.num_q_heads, shape.num_kv_heads, shape.head_dim
     if rows is None:
         rows = (q if q is not None else k).shape[0]
-    if (slots is not None and (slots.dtype is not torch.int64 or slots.numel() < rows or not slots.is_contiguous())) or \
-            (positions is not None and (positions.dtype is not torch.int32 or positions.numel() < rows or
-                                        not positions.is_contiguous())) or \
-            (cos_sin is not None and (cos_sin.dtype is not torch.float32 or cos_sin.dim() != 2 or not cos_sin.is_contiguous())) or \
-            (status is not None and status.dtype is not torch.int32):
-        raise DecodeAttnError(DA_ERR_INVALID_ARG, "decode_attn_prepare_rows")
-    a = RowsArgs()
-    a.struct_size = _ROWS_ARGS_SIZE
-    a.rows, a.cache_bits, a.interleaved, a.eps = rows, cache_bits, interleaved, eps
-    a.q, a.q_stride = _heads(q, rows, hq, d, dtype)
-    a.k, a.k_stride = _heads(k, rows, hkv, d, dtype)
-    a.v, a.v_stride = _heads(v, rows, hkv, d, dtype)
-    a.q_out, a.q_out_stride = _heads(q_out, rows, hq, d, dtype)
-    a.k_out, a.k_out_stride = _heads(k_out, rows, hkv, d, dtype)
-    a.q_weight, a.q_weight_stride = _head_weight(q_weight, hq, d, dtype)
-    a.k_weight, a.k_weight_stride = _head_weight(k_weight, hkv, d, dtype)
+    q_ptr, q_stride = _heads(q, rows, hq, d, dtype)
+    k_ptr, k_stride = _heads(k, rows, hkv, d, dtype)
+    v_ptr, v_stride = _heads(v, rows, hkv, d, dtype)
+    q_to, q_to_stride = _heads(q_out, rows, hq, d, dtype)
+    k_to, k_to_stride = _heads(k_out, rows, hkv, d, dtype)
+    q_w, q_w_stride = _head_weight(q_weight, hq, d, dtype)
+    k_w, k_w_stride = _head_weight(k_weight, hkv, d, dtype)
+    far = rotary = turn = 0
     if cos_sin is not None:
-        a.cos_sin, a.max_positions, a.rotary_dim = cos_sin.data_ptr(), cos_sin.shape[0], cos_sin.shape[1]
-    a.positions, a.slots = _ptr(positions), _ptr(slots)
-    a.k_cache, a.v_cache, a.status = _ptr(k_cache), _ptr(v_cache), _ptr(status)
-    rc = _lib.decode_attn_prepare_rows(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
-    if check:
-        _check(rc, "decode_attn_prepare_rows")
+        if cos_sin.dim() != 2:
+            raise DecodeAttnError(DA_ERR_INVALID_ARG, _ROWS_ERROR)
+        turn, (far, rotary) = _vector(cos_sin, fp32, 0, _ROWS_ERROR), cos_sin.shape
+    args = _ROWS_PACK(_ROWS_ARGS_SIZE, 0, rows, cache_bits, rotary, bool(interleaved), far, eps, q_ptr, k_ptr, v_ptr, q_stride,
+                      k_stride, v_stride, q_w, k_w, q_w_stride, k_w_stride, turn, _vector(positions, i32, rows, _ROWS_ERROR),
+                      _vector(slots, i64, rows, _ROWS_ERROR), q_to, k_to, q_to_stride, k_to_stride, _ptr(k_cache) or 0,
+                      _ptr(v_cache) or 0, _vector(status, i32, 1, _ROWS_ERROR))
+    rc = _lib.decode_attn_prepare_rows(shape, args, _stream(stream))
+    if check and rc != DA_OK:
+        _check(rc, _ROWS_ERROR)
     return rc
 
 
@@ -650,27 +672,18 @@ def decode_attn_step_tables(shape: Shape, seq_lens, gains, seq_lens_out, block_t
     """All int32 but slots (int64), contiguous: seq_lens, gains, seq_lens_out [batch]; block_table [batch, pages];
     free_pages [capacity]; free_count, free_count_out [1]; row_starts, page_starts [batch + 1]; slots, positions, row_seq
     [max_rows]; status [1] or None.  seq_lens_out may be seq_lens, free_count_out free_count."""
-    import torch
-    i32, batch, where = torch.int32, shape.batch, "decode_attn_step_tables"
-    max_rows = slots.numel()
-    for x, need in ((seq_lens, batch), (gains, batch), (seq_lens_out, batch), (block_table, batch * shape.max_pages_per_seq),
-                    (free_pages, 0), (free_count, 1), (free_count_out, 1), (row_starts, batch + 1), (page_starts, batch + 1),
-                    (positions, max_rows), (row_seq, max_rows), (status, 1)):
-        if x is not None and (x.dtype is not i32 or x.numel() < need or not x.is_contiguous()):
-            raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
-    if slots.dtype is not torch.int64 or not slots.is_contiguous():
-        raise DecodeAttnError(DA_ERR_INVALID_ARG, where)
-    a = TablesArgs()
-    a.struct_size = _TABLES_ARGS_SIZE
-    a.max_rows, a.free_capacity = max_rows, free_pages.numel()
-    a.seq_lens, a.gains, a.seq_lens_out = _ptr(seq_lens), _ptr(gains), _ptr(seq_lens_out)
-    a.block_table, a.free_pages = _ptr(block_table), _ptr(free_pages)
-    a.free_count, a.free_count_out = _ptr(free_count), _ptr(free_count_out)
-    a.row_starts, a.page_starts = _ptr(row_starts), _ptr(page_starts)
-    a.slots, a.positions, a.row_seq, a.status = _ptr(slots), _ptr(positions), _ptr(row_seq), _ptr(status)
-    rc = _lib.decode_attn_step_tables(ctypes.byref(shape), ctypes.byref(a), _stream(stream))
-    if check:
-        _check(rc, where)
+    _, _, _, i32, i64 = _dtypes()
+    batch, max_rows, at = shape.batch, slots.numel(), _TABLES_ERROR
+    args = _TABLES_PACK(_TABLES_ARGS_SIZE, 0, max_rows, free_pages.numel(), _vector(seq_lens, i32, batch, at),
+                        _vector(gains, i32, batch, at), _vector(seq_lens_out, i32, batch, at),
+                        _vector(block_table, i32, batch * shape.max_pages_per_seq, at), _vector(free_pages, i32, 0, at),
+                        _vector(free_count, i32, 1, at), _vector(free_count_out, i32, 1, at),
+                        _vector(row_starts, i32, batch + 1, at), _vector(page_starts, i32, batch + 1, at),
+                        _vector(slots, i64, 0, at), _vector(positions, i32, max_rows, at), _vector(row_seq, i32, max_rows, at),
+                        _vector(status, i32, 1, at))
+    rc = _lib.decode_attn_step_tables(shape, args, _stream(stream))
+    if check and rc != DA_OK:
+        _check(rc, at)
     return rc
 
 

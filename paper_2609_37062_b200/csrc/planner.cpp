@@ -199,6 +199,131 @@ int64_t units_for_chunk(const std::vector<int64_t>& pages, int64_t c, int max_sp
     return total;
 }
 
+// What the kernel for caches in 4 bits costs, in tiles of 16 tokens as one of its blocks works them off: a unit's end and
+// beginning, the steps that its warps take together, and a combine launch.  (64 sequences x 8 heads x 28,000 to 32,768 tokens,
+// 592 blocks: 470 us dealt by whole units, 419 evenly.)
+struct PackedCost {
+    int32_t unit, round, combine;
+};
+
+PackedCost packed_cost(const decode_attn_shape_t& s, int ctas_per_sm)
+{
+    const bool big = s.num_q_heads / s.num_kv_heads <= 8 && ctas_per_sm < 4;     // blocks of one team of eight warps
+    return big ? PackedCost{16, 16, 30} : PackedCost{8, 8, 15};
+}
+
+// The fullest block's load when chunks of c tiles go to the lightest block, longest first.
+int64_t dealt_whole(const std::vector<int64_t>& pages, int H, int64_t c, int max_splits, int slots, const PackedCost& pc)
+{
+    std::vector<std::pair<int64_t, int64_t>> kinds;          // (cost, units of it)
+    int64_t total = 0, n = 0, most = 0;
+    for (int64_t pg : pages) {
+        if (pg == 0) continue;
+        const int64_t chunk = std::max(c, ceil_div(pg, max_splits)), splits = ceil_div(pg, chunk);
+        const int64_t cost = ceil_div(ceil_div(pg, splits), pc.round) * pc.round + pc.unit;
+        kinds.push_back({cost, splits * H});
+        total += cost * splits * H;
+        n += splits * H;
+        most = std::max(most, cost);
+    }
+    if (n <= slots) return most;
+    if (n > 16 * (int64_t)slots) return ceil_div(total, slots) + most / 2;         // many small shares even out
+    std::sort(kinds.begin(), kinds.end(), std::greater<std::pair<int64_t, int64_t>>());
+    std::priority_queue<int64_t, std::vector<int64_t>, std::greater<int64_t>> loads;
+    for (int i = 0; i < slots; ++i) loads.push(0);
+    int64_t worst = 0;
+    for (const auto& k : kinds)
+        for (int64_t i = 0; i < k.second; ++i) {
+            const int64_t l = loads.top() + k.first;
+            loads.pop();
+            loads.push(l);
+            worst = std::max(worst, l);
+        }
+    return worst;
+}
+
+// One unit after the other to the blocks, every block an equal share of the tiles: what is over the share is cut off and
+// goes to the next block.  Heads of a sequence are cut at places of their own; those with fewer pieces than others get
+// empty ones.  Returns the load of the fullest block, or -1 where a sequence would have more pieces than it may.
+int64_t deal_evenly(const decode_attn_shape_t& s, const int32_t* seq_lens, const std::vector<int64_t>& pages, int slots,
+                    int64_t share, int64_t least, int max_splits, const PackedCost& c, Layout& out, bool commit)
+{
+    const int B = s.batch, H = s.num_kv_heads;
+    int64_t load = 0, worst = 0;
+    int block = 0;
+    std::vector<int32_t> begin(1, 0);              // first unit of every block
+    std::vector<decode_attn_unit_t> units;
+    std::vector<int32_t> pieces((size_t)H);
+    if (commit) {
+        out.splits.assign(B, 1);
+        out.slot_base.assign(B, -1);
+        out.n_slots = 0;
+        out.max_splits_used = B > 0 ? 1 : 0;
+    }
+    for (int b = 0; b < B; ++b) {
+        const size_t first_unit = units.size();
+        const int64_t n = pages[b];
+        for (int g = 0; g < H; ++g) {
+            int64_t at = 0;
+            int32_t k = 0;
+            do {
+                if (block + 1 < slots && load > 0 && n > 0 && share - load - c.unit < std::min(least, n - at)) {
+                    ++block;
+                    load = 0;
+                    begin.push_back((int32_t)units.size());
+                }
+                int64_t take = n - at;
+                if (block + 1 < slots && take > share - load - c.unit)
+                    take = std::max<int64_t>(least, (share - load - c.unit) / c.round * c.round);
+                if (n - at - take < least) take = n - at;        // no scrap is left behind
+                decode_attn_unit_t u;
+                u.seq = b;
+                u.kv_head = g;
+                u.tok_begin = (int32_t)(at * kTileTokens);
+                u.tok_end = (int32_t)std::min<int64_t>((at + take) * kTileTokens, out.visible[b]);
+                u.slot = -1;
+                u.seq_len = seq_lens[b];
+                u.split_index = k++;
+                u.n_splits = 1;
+                units.push_back(u);
+                at += take;
+                load += (take + c.round - 1) / c.round * c.round + c.unit;
+                worst = std::max(worst, load);
+            } while (at < n);
+            pieces[g] = k;
+        }
+        const int32_t S = *std::max_element(pieces.begin(), pieces.end());
+        if (S > max_splits) return -1;
+        if (!commit) continue;
+        out.splits[b] = S;
+        out.max_splits_used = std::max(out.max_splits_used, S);
+        if (S == 1) continue;
+        out.slot_base[b] = (int32_t)out.n_slots;
+        out.n_slots += S;
+        for (size_t i = first_unit; i < units.size(); ++i) {
+            units[i].n_splits = S;
+            units[i].slot = out.slot_base[b] + units[i].split_index;
+        }
+        for (int g = 0; g < H; ++g)
+            for (int32_t k = pieces[g]; k < S; ++k) {
+                decode_attn_unit_t u = units[first_unit];
+                u.kv_head = g;
+                u.tok_begin = u.tok_end = out.visible[b];
+                u.slot = out.slot_base[b] + k;
+                u.split_index = k;
+                units.push_back(u);
+            }
+    }
+    if (commit) {
+        begin.push_back((int32_t)units.size());
+        out.units.swap(units);
+        out.block_begin.swap(begin);
+        out.rank_pos.clear();
+        out.n_front_units = 0;
+    }
+    return worst;
+}
+
 }  // namespace
 
 int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, const int32_t* seq_lens,
@@ -210,6 +335,9 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
     // a time.  The pool's page size only bounds the block table, so a plan does not depend on it.
     const int B = s.batch, P = kTileTokens, H = s.num_kv_heads;
     const int max_splits = max_splits_of(p);
+    const bool packed = p.cache_bits == 4 && p.split_mode == DA_SPLIT_AUTO;
+    const PackedCost pc = packed ? packed_cost(s, ctas_per_sm) : PackedCost{0, 0, 0};
+    if (packed && max_bins <= 0) max_bins = sm_count * ctas_per_sm;              // (its work list follows from its blocks)
     // With a shared prefix the ordinary units cover only what follows it; the prefix itself is
     // cut into chunks attended once for a block of sequences at a time (see below).
     const int64_t prefix_tokens = p.shared_prefix_tokens;
@@ -270,7 +398,8 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
             // 32,768 x 64: 1.28 -> 1.23 ms, 8,192 x 64: 312 -> 308.5 us).
             const int64_t u0 = H * units_for_chunk(pages, c, max_splits);
             const int64_t waves0 = ceil_div(u0, slots);
-            constexpr int64_t kLongChunk = 128, kUnitPages = 3, kCombinePages = 24;
+            constexpr int64_t kLongChunk = 128;
+            const int64_t kUnitPages = packed ? pc.unit : 3, kCombinePages = packed ? pc.combine : 24;
             if (waves0 * slots * 100 > u0 * 106 && c >= 2 * kLongChunk) {
                 const bool split0 = u0 > floor_units;
                 int64_t best = c, best_cost = waves0 * (c + kUnitPages) + (split0 ? kCombinePages : 0);
@@ -286,6 +415,13 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
                 }
                 c = best;
             }
+        }
+        if (packed && B > 0) {
+            // no cut at all, where a combine launch costs more than the cuts save
+            const int64_t longest = std::max<int64_t>(1, *std::max_element(pages.begin(), pages.end()));
+            if (longest > c && longest <= INT32_MAX &&
+                dealt_whole(pages, H, longest, 1, max_bins, pc) <= dealt_whole(pages, H, c, max_splits, max_bins, pc) + pc.combine)
+                c = longest;
         }
         out.chunk_tokens = (int32_t)std::min<int64_t>(c * P, INT32_MAX);
         for (int b = 0; b < B; ++b) {
@@ -454,7 +590,7 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
     // counts four times) plus a fixed charge for the hand-over between units.  Loads are small
     // integers that only grow, so the lightest bin is found with a bucket queue: one list of bins
     // per load, the lightest non-empty list never moves down (ties: the bin that got there first).
-    constexpr int32_t kHandOverPages = 24;
+    const int32_t kHandOverPages = packed ? pc.unit : 24;
     const int bins = (int)std::min<int64_t>((int64_t)(n - first), max_bins);
     std::vector<int32_t>& bin_of = out.scratch_bin_of;
     std::vector<int32_t>& count = out.scratch_bin_count;
@@ -517,6 +653,29 @@ int make_layout(const decode_attn_shape_t& s, const decode_attn_policy_t& p, con
         out.rank_pos[i - first] = pos;
     }
     out.block_begin.push_back((int32_t)out.units.size());
+    if (packed) {
+        int64_t worst = 0;
+        for (int b = 0; b < bins; ++b) {
+            int64_t load = 0;
+            for (int32_t i = out.block_begin[b]; i < out.block_begin[b + 1]; ++i)
+                load += ceil_div(ceil_div(out.units[i].tok_end - out.units[i].tok_begin, P), pc.round) * pc.round + pc.unit;
+            worst = std::max(worst, load);
+        }
+        if (out.n_slots > 0) worst += pc.combine;
+        // what every block would have if all were equal; where the last one is left with more (ends that do not divide), the
+        // others take a little more each
+        int64_t cost_all = 0, even = -1;
+        for (int64_t n : pages)
+            if (n > 0) cost_all += (ceil_div(n, pc.round) * pc.round + pc.unit) * H;
+        int64_t share = ceil_div(cost_all, max_bins) + pc.unit;
+        for (int i = 0; i < 3 && (share + pc.combine) * 100 < worst * 97; ++i) {
+            even = deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, false);
+            if (even <= share + share / 64) break;
+            share += ceil_div(even - share, max_bins) + 1;
+        }
+        if (even >= 0 && (even + pc.combine) * 100 < worst * 97)
+            deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, true);
+    }
     return DA_OK;
 }
 

@@ -33,6 +33,40 @@ def test_plans_are_those_of_sixteen_bits():
             assert [bytes(x) for x in a[0]] == [bytes(x) for x in b[0]] and a[3:] == b[3:]
 
 
+@pytest.mark.parametrize("seed", range(30))
+def test_tiles_dealt_evenly_cover_every_token_once(seed):
+    """Whatever the mix: every KV head's tokens in order, pieces of at least the smallest chunk, slots of their own, and no
+    more records than a capacity plan has room for."""
+    rng = np.random.default_rng(seed)
+    hkv, group, ctas = int(rng.integers(1, 9)), int(rng.integers(1, 17)), int(rng.choice([2, 4]))
+    lens = [int(rng.choice([0, 1, rng.integers(1, 200), rng.integers(1, 40000)])) for _ in range(int(rng.integers(1, 70)))]
+    shape = da.make_kv4_shape(len(lens), hkv * group, hkv, 128, 16, 4096, 1 << 20)
+    least = int(rng.choice([16, 64, 256]))
+    pol = da.make_policy(cache_bits=4, chunk_tokens=least)
+    units, splits, base, n_slots, _ = da.decode_attn_plan_layout(shape, pol, lens, 148, ctas)
+    per, slots = {}, set()
+    for u in units:
+        per.setdefault((u.seq, u.kv_head), []).append(u)
+        assert u.n_splits == splits[u.seq] and u.seq_len == lens[u.seq]
+        assert u.slot == (base[u.seq] + u.split_index if u.n_splits > 1 else -1)
+        if u.slot >= 0:
+            assert (u.slot, u.kv_head) not in slots and u.slot < n_slots
+            slots.add((u.slot, u.kv_head))
+    assert len(per) == len(lens) * hkv
+    for (b, g), mine in per.items():
+        mine.sort(key=lambda u: u.split_index)
+        assert [u.split_index for u in mine] == list(range(splits[b]))
+        at = 0
+        for u in mine:
+            assert u.tok_begin % 16 == 0 or u.tok_begin == u.tok_end
+            if u.tok_end > u.tok_begin:
+                assert u.tok_begin == at
+                at = u.tok_end
+                assert u.n_splits == 1 or u.tok_end - u.tok_begin > least - 16 or lens[b] <= 2 * least
+        assert at == lens[b]
+    assert n_slots <= -(-sum(lens) // least) + len(lens)
+
+
 @pytest.mark.parametrize("kw,want", [
     (dict(cache_bits=8), da.DA_ERR_INVALID_ARG), (dict(cache_bits=-4), da.DA_ERR_INVALID_ARG),
     (dict(cache_bits=4, track_weights=1), da.DA_ERR_UNSUPPORTED), (dict(cache_bits=4, shared_prefix_tokens=64), da.DA_ERR_UNSUPPORTED),
