@@ -1,8 +1,8 @@
 // Pages of a cache in 4 bits to 16-bit pages (decode_attn_expand_kv).
 //
-// Bound by memory: 4.5 bits read and 16 written a value.  A warp takes one tile of one KV head; 16 lanes (8 at head_dim
-// 64) write a row of K or V whole, 16 bytes a lane, from one word of codes each.  All loads of the tile are asked for before
-// the first value is used.
+// Bound by memory: 4.5 bits read and 16 written a value.  A warp takes a tile of one KV head at a time; 16 lanes (8 at
+// head_dim 64) write a row of K or V whole, 16 bytes a lane, from one word of codes each.  All loads of the tile are asked for
+// before the first value is used, and the page ids of a block's tiles before the first tile.
 #include <cstring>
 
 #include "common.cuh"
@@ -43,11 +43,18 @@ __device__ __forceinline__ uint4 expand_word(uint32_t w, __half scale)
 {
     uint32_t c[4], r[4];
     packed_unpack(w, c);
+    const __half2 s2 = __half2half2(scale);
     const float s = __half2float(scale);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&c[i]));
-        r[i] = round_pair<F16>(f.x * s, f.y * s);             // (the products are exact: 2 and 11 significant bits)
+        const __half2 x = *reinterpret_cast<const __half2*>(&c[i]);
+        if (F16) {
+            const __half2 y = __hmul2(x, s2);
+            r[i] = *reinterpret_cast<const uint32_t*>(&y);
+        } else {
+            const float2 f = __half22float2(x);
+            r[i] = round_pair<F16>(f.x * s, f.y * s);         // (the products are exact: 2 and 11 significant bits)
+        }
     }
     return make_uint4(r[0], r[1], r[2], r[3]);
 }
@@ -69,41 +76,53 @@ __global__ void __launch_bounds__(kExpandThreads) decode_attn_expand_kernel(cons
     }
     const int n_tiles = (len + 15) >> 4;
     const int tile0 = blockIdx.x * kExpandTiles;
-    for (int i = threadIdx.x >> 5; i < kExpandTiles * p.num_kv_heads; i += kExpandThreads / 32) {
-        const int tile = tile0 + i / p.num_kv_heads, head = i % p.num_kv_heads;
-        if (tile >= n_tiles) break;
-        const int page_at = tile >> (p.page_shift - 4), in_page = tile & ((1 << (p.page_shift - 4)) - 1);
-        const int src_page = __ldg(p.block_table + (int64_t)b * p.src_width + page_at);
-        const int dst_page = __ldg(p.dst_table + (int64_t)b * p.dst_width + page_at);
-        if ((unsigned)src_page >= (unsigned)p.src_pages || (unsigned)dst_page >= (unsigned)p.num_pages) {
-            if (lane == 0 && p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
-            continue;
+    if (tile0 >= n_tiles) return;
+    // lane i: the pages of the block's tile i
+    int src_id = -1, dst_id = -1;
+    if (lane < kExpandTiles && tile0 + lane < n_tiles) {
+        const int at = (tile0 + lane) >> (p.page_shift - 4);
+        src_id = __ldg(p.block_table + (int64_t)b * p.src_width + at);
+        dst_id = __ldg(p.dst_table + (int64_t)b * p.dst_width + at);
+        if ((unsigned)src_id >= (unsigned)p.src_pages || (unsigned)dst_id >= (unsigned)p.num_pages) {
+            if (p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
+            dst_id = -1;
         }
-        const char* const src = p.pool + src_page * p.src_stride_page + head * p.src_stride_head + in_page * packed_tile_bytes(D);
-        const uint32_t* const kc = reinterpret_cast<const uint32_t*>(src);
-        const uint32_t* const vc = reinterpret_cast<const uint32_t*>(src + packed_v_codes(D));
-        const __half* const ks = reinterpret_cast<const __half*>(src + packed_k_scales(D));
-        const __half* const vs = reinterpret_cast<const __half*>(src + packed_v_scales(D));
-        const int l = lane % L, r0 = lane / L;
-        const int rows = min(16, len - tile * 16);
-        uint32_t kw[N], vw[N];
-        __half kf[N], vf[N];
+    }
+    const int l = lane % L, r0 = lane / L;
+    const int64_t k_step = STEP * p.k_stride_token, v_step = STEP * p.v_stride_token;
+    for (int i = 0; i < kExpandTiles && tile0 + i < n_tiles; ++i) {
+        const int src_page = __shfl_sync(0xffffffffu, src_id, i), dst_page = __shfl_sync(0xffffffffu, dst_id, i);
+        if (dst_page < 0) continue;
+        const int in_page = (tile0 + i) & ((1 << (p.page_shift - 4)) - 1);
+        const int rows = min(16, len - (tile0 + i) * 16);
+        const char* const src = p.pool + src_page * p.src_stride_page + in_page * packed_tile_bytes(D);
+        uint16_t* const kd = p.k + dst_page * p.k_stride_page + (in_page * 16 + r0) * p.k_stride_token + 8 * l;
+        uint16_t* const vd = p.v + dst_page * p.v_stride_page + (in_page * 16 + r0) * p.v_stride_token + 8 * l;
+        for (int head = threadIdx.x >> 5; head < p.num_kv_heads; head += kExpandThreads / 32) {
+            const char* const from = src + head * p.src_stride_head;
+            const uint32_t* const kc = reinterpret_cast<const uint32_t*>(from) + packed_k_word(D, r0, l);
+            const uint32_t* const vc = reinterpret_cast<const uint32_t*>(from + packed_v_codes(D));
+            const __half* const ks = reinterpret_cast<const __half*>(from + packed_k_scales(D)) + packed_k_scale(D, r0, l >> 2);
+            const __half* const vs = reinterpret_cast<const __half*>(from + packed_v_scales(D));
+            uint32_t kw[N], vw[N];
+            __half kf[N], vf[N];
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int r = j * STEP + r0;
-            kw[j] = __ldg(kc + packed_k_word(D, r, l));
-            vw[j] = __ldg(vc + packed_v_word(D, r, l));
-            kf[j] = __ldg(ks + packed_k_scale(D, r, l >> 2));
-            vf[j] = __ldg(vs + packed_v_scale(r, l >> 2));
-        }
-        uint16_t* const kd = p.k + dst_page * p.k_stride_page + (in_page * 16) * p.k_stride_token + head * p.k_stride_head + 8 * l;
-        uint16_t* const vd = p.v + dst_page * p.v_stride_page + (in_page * 16) * p.v_stride_token + head * p.v_stride_head + 8 * l;
+            for (int j = 0; j < N; ++j) {
+                kw[j] = __ldg(kc + packed_k_word(D, j * STEP, 0));
+                vw[j] = __ldg(vc + packed_v_word(D, j * STEP + r0, l));
+                kf[j] = __ldg(ks + packed_k_scale(D, j * STEP, 0));
+                vf[j] = __ldg(vs + packed_v_scale(j * STEP + r0, l >> 2));
+            }
+            uint16_t* kt = kd + head * p.k_stride_head;
+            uint16_t* vt = vd + head * p.v_stride_head;
 #pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int r = j * STEP + r0;
-            if (r < rows) {
-                *reinterpret_cast<uint4*>(kd + r * p.k_stride_token) = expand_word<F16>(kw[j], kf[j]);
-                *reinterpret_cast<uint4*>(vd + r * p.v_stride_token) = expand_word<F16>(vw[j], vf[j]);
+            for (int j = 0; j < N; ++j) {
+                if (j * STEP + r0 < rows) {
+                    __stcs(reinterpret_cast<uint4*>(kt), expand_word<F16>(kw[j], kf[j]));
+                    __stcs(reinterpret_cast<uint4*>(vt), expand_word<F16>(vw[j], vf[j]));
+                }
+                kt += k_step;
+                vt += v_step;
             }
         }
     }

@@ -19,15 +19,19 @@ bool rows_ok(const void* p, int64_t stride, int64_t heads, int64_t D)
 
 typedef void (*rows_kernel_t)(const RowsParams);
 
-template <int D>
-rows_kernel_t kernel_for(bool f16, bool packed, bool halves)
+template <int D, bool F16, bool PACKED>
+rows_kernel_t for_turn(bool halves, bool all)
 {
-    if (packed) {
-        if (halves) return f16 ? decode_attn_rows_kernel<D, true, true, true> : decode_attn_rows_kernel<D, false, true, true>;
-        return f16 ? decode_attn_rows_kernel<D, true, true, false> : decode_attn_rows_kernel<D, false, true, false>;
-    }
-    if (halves) return f16 ? decode_attn_rows_kernel<D, true, false, true> : decode_attn_rows_kernel<D, false, false, true>;
-    return f16 ? decode_attn_rows_kernel<D, true, false, false> : decode_attn_rows_kernel<D, false, false, false>;
+    if (halves) return all ? decode_attn_rows_kernel<D, F16, PACKED, true, true> : decode_attn_rows_kernel<D, F16, PACKED, true, false>;
+    return all ? decode_attn_rows_kernel<D, F16, PACKED, false, true> : decode_attn_rows_kernel<D, F16, PACKED, false, false>;
+}
+
+// halves: pairs are (i, i + rotary_dim / 2); all: every dim turns.
+template <int D>
+rows_kernel_t kernel_for(bool f16, bool packed, bool halves, bool all)
+{
+    if (packed) return f16 ? for_turn<D, true, true>(halves, all) : for_turn<D, false, true>(halves, all);
+    return f16 ? for_turn<D, true, false>(halves, all) : for_turn<D, false, false>(halves, all);
 }
 
 }  // namespace
@@ -102,12 +106,24 @@ extern "C" int decode_attn_prepare_rows(const decode_attn_shape_t* shape, const 
     while ((1 << rp.page_shift) < s.page_size) ++rp.page_shift;
     rp.eps = a->eps;
 
-    const bool f16 = s.kv_dtype == DA_DTYPE_FP16, halves = a->cos_sin != nullptr && !a->interleaved;
-    rows_kernel_t fn = D == 128 ? kernel_for<128>(f16, packed, halves) : kernel_for<64>(f16, packed, halves);
+    const bool f16 = s.kv_dtype == DA_DTYPE_FP16, halves = a->cos_sin != nullptr && !a->interleaved, all = a->rotary_dim == D;
+    rows_kernel_t fn = D == 128 ? kernel_for<128>(f16, packed, halves, all) : kernel_for<64>(f16, packed, halves, all);
+    // A warp a row where rows fill the machine (the resident warps of 148 SMs); fewer rows are shared by warps.
+    const int per_task = 512 / D, tasks = (rp.n_q + per_task - 1) / per_task + (rp.n_k + per_task - 1) / per_task + (rp.n_v + per_task - 1) / per_task;
+    const int64_t wanted = (148 * kRowsBlocks * (kRowsThreads / 32) + a->rows - 1) / a->rows;
+    rp.split = (int32_t)(wanted < tasks ? wanted : tasks);
+    // (numbers of work items stay below 2^31, two rounds of all warps included)
+    if ((int64_t)a->rows * rp.split > INT32_MAX - 4 * 148 * kRowsBlocks * (kRowsThreads / 32)) return DA_ERR_UNSUPPORTED;
+    const int64_t warps = (int64_t)a->rows * rp.split, needed = (warps + kRowsThreads / 32 - 1) / (kRowsThreads / 32);
+    const int64_t blocks = needed < 148 * kRowsBlocks ? needed : 148 * kRowsBlocks;
+    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem) != cudaSuccess) {
+        (void)cudaGetLastError();
+        return DA_ERR_CUDA;
+    }
     cudaLaunchConfig_t cfg;
-    cfg.gridDim = dim3((unsigned)a->rows, 1, 1);
+    cfg.gridDim = dim3((unsigned)blocks, 1, 1);
     cfg.blockDim = dim3(kRowsThreads, 1, 1);
-    cfg.dynamicSmemBytes = 0;
+    cfg.dynamicSmemBytes = kRowsSmem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -1,10 +1,19 @@
 // Rows of new tokens: per-head norms, rotation and the cache write in one pass (decode_attn_prepare_rows).
 //
-// Bound by memory: a row's heads are read once and written once.  A group of D / 8 lanes owns one head of one row, eight
-// dims a lane, held as two runs of four: for the rotation of halves a lane takes four dims of the first half and their
-// partners of the second, so that a pair never leaves its lane; otherwise its eight dims are neighbours.  The mean of
-// squares is a butterfly over the group's lanes.  A block takes one row; its warps walk the row's q, k and v heads.
+// Bound by memory, with issued instructions close behind: a row's heads are read once and written once.  A warp takes one row
+// after the other, or a share of a row's heads where there are few rows.  A group of D / 16 of its lanes owns one head at a
+// time, sixteen dims a lane in two units of eight, a unit being two runs of four: for the rotation of halves a unit is four
+// dims of the first half and their partners of the second, so that a pair never leaves its lane; otherwise its eight dims
+// are neighbours.  What weight and angle do to a pair (a, b) is one 2 x 2 matrix, the same for all heads that share the weight:
+// it is made once a row and kept in registers, a head costs four products a pair and the root of its mean of squares (a butterfly
+// over the group's lanes) two more.
+//
+// A lane copies its own 32 bytes of the heads ahead to a ring in shared memory (cp.async), three tasks of 512 / D heads ahead
+// and across rows, and the angles of the row after this one: held in registers, loads ahead wait for one another (8,192 rows of
+// 48 heads of 128: 54 to 65 us in every arrangement of registers).
 #pragma once
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "packed.cuh"
@@ -12,6 +21,10 @@
 namespace da {
 
 constexpr int kRowsThreads = 256;
+constexpr int kRowsRing = 4;                     // tasks in a warp's ring
+constexpr int kRowsLane = kRowsRing * 32 + 128;  // bytes of shared memory of a lane: the ring, angles of two rows
+constexpr int kRowsSmem = kRowsThreads * kRowsLane;
+constexpr int kRowsBlocks = 2;                   // on an SM
 
 struct RowsParams {
     const uint16_t *q, *k, *v;
@@ -32,6 +45,7 @@ struct RowsParams {
     int32_t rows, n_q, n_k, n_v;      // heads of a row to work on
     int32_t rotary_dim, max_positions;
     int32_t page_shift;
+    int32_t split;                    // warps to a row
     float eps;
 };
 
@@ -54,169 +68,364 @@ __device__ __forceinline__ uint32_t rows_pack(float lo, float hi)
     return *reinterpret_cast<const uint32_t*>(&h);
 }
 
-// Where a lane's two runs of four dims begin.
+template <int BYTES>
+__device__ __forceinline__ void rows_copy(uint32_t dst, const void* src)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(BYTES) : "memory");
+}
+
+// Where the runs of a head's unit i (of D / 8) begin.  With HALVES the units of the dims that turn come first.
 struct RowDims {
     int a, b;
 };
 
 template <bool HALVES>
-__device__ __forceinline__ RowDims row_dims(int l, int rotary_dim)
+__device__ __forceinline__ RowDims row_dims(int i, int rotary_dim)
 {
-    if (!HALVES) return {8 * l, 8 * l + 4};
-    const int n = rotary_dim >> 3;                            // lanes whose dims turn
-    if (l < n) return {4 * l, (rotary_dim >> 1) + 4 * l};
-    return {8 * l, 8 * l + 4};
+    if (HALVES && i < (rotary_dim >> 3)) return {4 * i, (rotary_dim >> 1) + 4 * i};
+    return {8 * i, 8 * i + 4};
+}
+
+// A lane's units are 2 l and 2 l + 1 (NEAR: the runs of the first half that it holds lie behind each other, as do those of the
+// second; a quantised block of 32 dims lies with two lanes), or l and D / 16 + l, where neither matters.
+template <int D, bool NEAR>
+__device__ __forceinline__ int row_unit(int l, int k)
+{
+    return NEAR ? 2 * l + k : l + k * (D / 16);
+}
+
+// A lane's sixteen dims.  wide: 16 bytes at a time (the runs of a half begin at multiples of eight dims).
+template <int D, bool HALVES, bool ALL, bool NEAR>
+__device__ __forceinline__ void row_load(const uint16_t* src, int l, int rotary_dim, bool wide, uint2 (&u)[2][2])
+{
+    if (wide) {
+        const RowDims x = row_dims<HALVES>(row_unit<D, NEAR>(l, 0), rotary_dim), y = row_dims<HALVES>(row_unit<D, NEAR>(l, 1), rotary_dim);
+        const bool halves = HALVES && (ALL || 16 * l < rotary_dim);   // runs a of both units, then runs b; else unit by unit
+        const uint4 p = *reinterpret_cast<const uint4*>(src + x.a), q = *reinterpret_cast<const uint4*>(src + (halves ? x.b : y.a));
+        u[0][0] = make_uint2(p.x, p.y);
+        (halves ? u[1][0] : u[0][1]) = make_uint2(p.z, p.w);
+        (halves ? u[0][1] : u[1][0]) = make_uint2(q.x, q.y);
+        u[1][1] = make_uint2(q.z, q.w);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const RowDims x = row_dims<HALVES>(row_unit<D, NEAR>(l, k), rotary_dim);
+        u[k][0] = *reinterpret_cast<const uint2*>(src + x.a);
+        u[k][1] = *reinterpret_cast<const uint2*>(src + x.b);
+    }
+}
+
+template <int D, bool HALVES, bool ALL, bool NEAR>
+__device__ __forceinline__ void row_store(uint16_t* dst, int l, int rotary_dim, bool wide, const uint2 (&u)[2][2])
+{
+    if (wide) {
+        const RowDims x = row_dims<HALVES>(row_unit<D, NEAR>(l, 0), rotary_dim), y = row_dims<HALVES>(row_unit<D, NEAR>(l, 1), rotary_dim);
+        const bool halves = HALVES && (ALL || 16 * l < rotary_dim);
+        const uint2 second = halves ? u[1][0] : u[0][1], third = halves ? u[0][1] : u[1][0];
+        *reinterpret_cast<uint4*>(dst + x.a) = make_uint4(u[0][0].x, u[0][0].y, second.x, second.y);
+        *reinterpret_cast<uint4*>(dst + (halves ? x.b : y.a)) = make_uint4(third.x, third.y, u[1][1].x, u[1][1].y);
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const RowDims x = row_dims<HALVES>(row_unit<D, NEAR>(l, k), rotary_dim);
+        *reinterpret_cast<uint2*>(dst + x.a) = u[k][0];
+        *reinterpret_cast<uint2*>(dst + x.b) = u[k][1];
+    }
+}
+
+// row_load's reads as copies to the lane's places dst and dst + kRowsPlane, in row_load's order of words.
+constexpr uint32_t kRowsPlane = 512;             // (a plane holds 16 bytes of every lane)
+
+template <int D, bool HALVES, bool ALL, bool NEAR>
+__device__ __forceinline__ void row_fetch(uint32_t dst, const uint16_t* src, int l, int rotary_dim, bool wide)
+{
+    const RowDims x = row_dims<HALVES>(row_unit<D, NEAR>(l, 0), rotary_dim), y = row_dims<HALVES>(row_unit<D, NEAR>(l, 1), rotary_dim);
+    if (wide) {
+        const bool halves = HALVES && (ALL || 16 * l < rotary_dim);
+        rows_copy<16>(dst, src + x.a);
+        rows_copy<16>(dst + kRowsPlane, src + (halves ? x.b : y.a));
+        return;
+    }
+    rows_copy<8>(dst, src + x.a);
+    rows_copy<8>(dst + 8, src + x.b);
+    rows_copy<8>(dst + kRowsPlane, src + y.a);
+    rows_copy<8>(dst + kRowsPlane + 8, src + y.b);
+}
+
+template <bool HALVES, bool ALL>
+__device__ __forceinline__ void row_take(uint32_t at, int l, int rotary_dim, bool wide, uint2 (&u)[2][2])
+{
+    uint4 p, q;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(p.x), "=r"(p.y), "=r"(p.z), "=r"(p.w) : "r"(at));
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(q.x), "=r"(q.y), "=r"(q.z), "=r"(q.w) : "r"(at + kRowsPlane));
+    const bool halves = HALVES && wide && (ALL || 16 * l < rotary_dim);               // runs a of both units, then runs b
+    const uint2 second = make_uint2(p.z, p.w), third = make_uint2(q.x, q.y);
+    u[0][0] = make_uint2(p.x, p.y);
+    u[0][1] = halves ? third : second;
+    u[1][0] = halves ? second : third;
+    u[1][1] = make_uint2(q.z, q.w);
 }
 
 // HALVES: pairs are (i, i + rotary_dim / 2); else neighbours, or nothing turns.
-template <int D, bool F16, bool PACKED, bool HALVES>
-__global__ void __launch_bounds__(kRowsThreads) decode_attn_rows_kernel(const RowsParams p)
+// ALL: all dims turn (rotary_dim is D).
+template <int D, bool F16, bool PACKED, bool HALVES, bool ALL>
+__global__ void __launch_bounds__(kRowsThreads, kRowsBlocks) decode_attn_rows_kernel(const RowsParams p)
 {
-    constexpr int L = D / 8;                                  // lanes of a head
-    constexpr int GROUPS = kRowsThreads / L;
+    constexpr int L = D / 16;                                 // lanes of a head
+    constexpr int HEADS = 32 / L;                             // heads of a task
+    constexpr bool NEAR = HALVES || PACKED;
+    extern __shared__ __align__(128) uint8_t smem[];
     pdl_launch_dependents();
     pdl_wait_primary();
-    const int row = blockIdx.x;
-    const int l = threadIdx.x % L, group = threadIdx.x / L;
-    int pos = 0;
-    if (p.positions != nullptr) {
-        pos = __ldg(p.positions + row);
-        if (pos < 0) return;
-        if (p.cos_sin != nullptr && pos >= p.max_positions) {
-            if (threadIdx.x == 0 && p.status != nullptr) record_status(p.status, DA_ERR_STALE_PLAN);
-            return;
-        }
-    }
-    // the row's place in the cache (page < 0: none)
-    int64_t page = -1;
-    int place = 0;
-    if (p.k_cache != nullptr) {
-        const int64_t slot = __ldg(reinterpret_cast<const long long*>(p.slots) + row);
-        if (slot >= 0) {
-            page = slot >> p.page_shift;
-            place = (int)(slot & ((1 << p.page_shift) - 1));
-            if (page >= p.num_pages) {
-                if (threadIdx.x == 0 && p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
-                page = -1;
+    const int lane = threadIdx.x & 31, l = lane % L, group = lane / L;
+    // the lane's places: tasks' planes, then four planes of angles for even and for odd rows of the warp
+    const uint32_t ring = smem_u32(smem) + (threadIdx.x >> 5) * (32 * kRowsLane) + lane * 16;
+    const uint32_t angles_at = ring + kRowsRing * 2 * kRowsPlane;
+    const int rotary = ALL ? D : p.rotary_dim;
+    const bool wide = !HALVES || ALL || rotary % 16 == 0;
+    // tasks of HEADS heads, those of q first, then k, then v; work item id: row id / split, a share of its tasks
+    const int tq = (p.n_q + HEADS - 1) / HEADS, tk = (p.n_k + HEADS - 1) / HEADS, tv = (p.n_v + HEADS - 1) / HEADS;
+    const int tasks = tq + tk + tv;
+    const unsigned split = p.split, stride = gridDim.x * (kRowsThreads / 32), items = (unsigned)p.rows * split;   // (below 2^31)
+    const unsigned first_id = blockIdx.x * (kRowsThreads / 32) + (threadIdx.x >> 5);
+    if (first_id >= items) return;
+    auto row_of = [&](unsigned id) { return (int)(split == 1 ? id : id / split); };
+    // the first task of share `part`
+    auto cut_at = [&](unsigned part) { return split == 1 ? (part ? tasks : 0) : (int)((unsigned)tasks * part / split); };
+
+    // ---- asking for tasks
+    unsigned i_id = first_id;
+    int i_row = row_of(i_id), i_task = cut_at(i_id - i_row * split), i_end = cut_at(i_id - i_row * split + 1);
+    uint32_t i_slot = 0;
+    auto ask = [&]() {
+        if (i_id < items) {
+            const uint32_t dst = ring + i_slot * (2 * kRowsPlane);
+            if (i_task < tq) {
+                const int h = i_task * HEADS + group;
+                if (h < p.n_q) row_fetch<D, HALVES, ALL, NEAR>(dst, p.q + i_row * p.q_stride + h * D, l, rotary, wide);
+            } else if (i_task < tq + tk) {
+                const int h = (i_task - tq) * HEADS + group;
+                if (h < p.n_k) row_fetch<D, HALVES, ALL, NEAR>(dst, p.k + i_row * p.k_stride + h * D, l, rotary, wide);
+            } else {
+                const int h = (i_task - tq - tk) * HEADS + group;
+                if (h < p.n_v) row_fetch<D, false, ALL, NEAR>(dst, p.v + i_row * p.v_stride + h * D, l, 0, true);
             }
-        }
-    }
-    const RowDims turned = row_dims<HALVES>(l, p.rotary_dim);
-    float c[8], s[8];                                         // HALVES: four pairs; else two of a run, twice
-    const bool turns = p.cos_sin != nullptr && 8 * l < p.rotary_dim;
-    if (turns) {
-        const float* const t = p.cos_sin + (int64_t)pos * p.rotary_dim;
-        // (either way the lane's four pairs are 4 l .. 4 l + 3)
-        const float4 x = __ldg(reinterpret_cast<const float4*>(t) + l);
-        const float4 y = __ldg(reinterpret_cast<const float4*>(t + (p.rotary_dim >> 1)) + l);
-        c[0] = x.x; c[1] = x.y; c[2] = x.z; c[3] = x.w;
-        s[0] = y.x; s[1] = y.y; s[2] = y.z; s[3] = y.w;
-    }
-    const int heads = p.n_q + p.n_k + p.n_v;
-    for (int h0 = 0; h0 < heads; h0 += GROUPS) {
-        const int h = h0 + group;
-        const bool live = h < heads;                          // (the whole warp stays: its lanes exchange values)
-        const int kind = h < p.n_q ? 0 : h < p.n_q + p.n_k ? 1 : 2;
-        const int head = h - (kind == 0 ? 0 : kind == 1 ? p.n_q : p.n_q + p.n_k);
-        const uint16_t* const src = (kind == 0 ? p.q + row * p.q_stride : kind == 1 ? p.k + row * p.k_stride : p.v + row * p.v_stride) + head * D;
-        const uint16_t* const w = kind == 0 ? p.q_weight : kind == 1 ? p.k_weight : nullptr;
-        const RowDims at = kind == 2 ? RowDims{8 * l, 8 * l + 4} : turned;
-        uint2 u = make_uint2(0, 0), v = make_uint2(0, 0);
-        if (live) {
-            u = *reinterpret_cast<const uint2*>(src + at.a);
-            v = *reinterpret_cast<const uint2*>(src + at.b);
-        }
-        float x[8];
-        {
-            const float2 a0 = rows_pair<F16>(u.x), a1 = rows_pair<F16>(u.y), b0 = rows_pair<F16>(v.x), b1 = rows_pair<F16>(v.y);
-            x[0] = a0.x; x[1] = a0.y; x[2] = a1.x; x[3] = a1.y;
-            x[4] = b0.x; x[5] = b0.y; x[6] = b1.x; x[7] = b1.y;
-        }
-        float sum = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum = fmaf(x[i], x[i], sum);
-#pragma unroll
-        for (int off = L / 2; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-        if (live && w != nullptr) {
-            const uint16_t* const wr = w + head * (kind == 0 ? p.q_weight_stride : p.k_weight_stride);
-            const uint2 wu = __ldg(reinterpret_cast<const uint2*>(wr + at.a)), wv = __ldg(reinterpret_cast<const uint2*>(wr + at.b));
-            const float2 w0 = rows_pair<F16>(wu.x), w1 = rows_pair<F16>(wu.y), w2 = rows_pair<F16>(wv.x), w3 = rows_pair<F16>(wv.y);
-            const float r = rsqrtf(sum * (1.0f / D) + p.eps);
-            x[0] *= r * w0.x; x[1] *= r * w0.y; x[2] *= r * w1.x; x[3] *= r * w1.y;
-            x[4] *= r * w2.x; x[5] *= r * w2.y; x[6] *= r * w3.x; x[7] *= r * w3.y;
-        }
-        if (turns && kind < 2) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                float& a = HALVES ? x[i] : x[2 * i];
-                float& b = HALVES ? x[4 + i] : x[2 * i + 1];
-                const float na = a * c[i] - b * s[i];
-                b = fmaf(b, c[i], a * s[i]);
-                a = na;
-            }
-        }
-        uint2 ya, yb;
-        if (kind == 2) {
-            ya = u;
-            yb = v;
-        } else {
-            ya = make_uint2(rows_pack<F16>(x[0], x[1]), rows_pack<F16>(x[2], x[3]));
-            yb = make_uint2(rows_pack<F16>(x[4], x[5]), rows_pack<F16>(x[6], x[7]));
-        }
-        uint16_t* const out = kind == 0   ? p.q_out + row * p.q_out_stride + head * D
-                              : kind == 1 && p.k_out != nullptr ? p.k_out + row * p.k_out_stride + head * D
-                                                                : nullptr;
-        if (live && out != nullptr) {
-            *reinterpret_cast<uint2*>(out + at.a) = ya;
-            *reinterpret_cast<uint2*>(out + at.b) = yb;
-        }
-        if (!PACKED) {
-            if (live && kind > 0 && page >= 0) {
-                uint16_t* const pool = kind == 1 ? static_cast<uint16_t*>(p.k_cache) + page * p.k_stride_page + place * p.k_stride_token + head * p.k_stride_head
-                                                 : static_cast<uint16_t*>(p.v_cache) + page * p.v_stride_page + place * p.v_stride_token + head * p.v_stride_head;
-                *reinterpret_cast<uint2*>(pool + at.a) = ya;
-                *reinterpret_cast<uint2*>(pool + at.b) = yb;
-            }
-        } else {
-            // Eight neighbouring dims to a lane: run g of four dims lies with lane g (its first run), g - n (its second)
-            // or, where nothing turns, lane g / 2.
-            uint32_t z[4] = {ya.x, ya.y, yb.x, yb.y};
-            if (HALVES) {
-                const int n = p.rotary_dim >> 3, base = threadIdx.x & 31 & ~(L - 1);
-#pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const int g = 2 * l + half;
-                    const int from = kind == 2 || g >= 2 * n ? g >> 1 : g < n ? g : g - n;
-                    const bool second = kind == 2 || g >= 2 * n ? (g & 1) : g >= n;
-                    const uint32_t a0 = __shfl_sync(0xffffffffu, ya.x, base + from), a1 = __shfl_sync(0xffffffffu, ya.y, base + from);
-                    const uint32_t b0 = __shfl_sync(0xffffffffu, yb.x, base + from), b1 = __shfl_sync(0xffffffffu, yb.y, base + from);
-                    z[2 * half] = second ? b0 : a0;
-                    z[2 * half + 1] = second ? b1 : a1;
-                }
-            }
-            float y[8], amax = 0.f;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = rows_pair<F16>(z[i]);
-                y[2 * i] = f.x;
-                y[2 * i + 1] = f.y;
-                amax = fmaxf(amax, fmaxf(fabsf(f.x), fabsf(f.y)));
-            }
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));      // the four lanes of a block of 32 dims
-            amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 2));
-            if (live && kind > 0 && page >= 0) {
-                const __half scale = packed_scale(amax);
-                char* const tile = static_cast<char*>(p.k_cache) + page * p.k_stride_page + head * p.k_stride_head +
-                                   (place >> 4) * packed_tile_bytes(D);
-                const int r = place & 15, block = l >> 2;
-                uint32_t* const codes = reinterpret_cast<uint32_t*>(tile + (kind == 1 ? 0 : packed_v_codes(D)));
-                codes[kind == 1 ? packed_k_word(D, r, l) : packed_v_word(D, r, l)] = packed_word(y, scale);
-                if ((l & 3) == 0) {
-                    __half* const scales = reinterpret_cast<__half*>(tile + (kind == 1 ? packed_k_scales(D) : packed_v_scales(D)));
-                    scales[kind == 1 ? packed_k_scale(D, r, block) : packed_v_scale(r, block)] = scale;
+            if (++i_task == i_end) {
+                i_id += stride;
+                if (i_id < items) {
+                    i_row = row_of(i_id);
+                    i_task = cut_at(i_id - i_row * split);
+                    i_end = cut_at(i_id - i_row * split + 1);
                 }
             }
         }
+        asm volatile("cp.async.commit_group;" ::: "memory");  // (a group for every call: the waits below count them)
+        i_slot = (i_slot + 1) % kRowsRing;
+    };
+    // positions and slots are read a row ahead, angles copied a row ahead of their use
+    auto position = [&](unsigned id) { return p.positions != nullptr && id < items ? __ldg(p.positions + row_of(id)) : 0; };
+    auto slot_of = [&](unsigned id) {
+        return p.k_cache != nullptr && id < items ? (int64_t)__ldg(reinterpret_cast<const long long*>(p.slots) + row_of(id)) : -1;
+    };
+    auto copy_angles = [&](int pos, uint32_t to) {
+        if (p.cos_sin == nullptr || pos < 0 || pos >= p.max_positions) return;
+        const float* const angles = p.cos_sin + (int64_t)pos * rotary;
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {                         // either way unit j's four pairs are 4 j .. 4 j + 3
+            const int j = row_unit<D, NEAR>(l, k);
+            if (!ALL && 8 * j >= rotary) continue;
+            rows_copy<16>(to + (2 * k) * kRowsPlane, angles + 4 * j);
+            rows_copy<16>(to + (2 * k + 1) * kRowsPlane, angles + (rotary >> 1) + 4 * j);
+        }
+    };
+    int pos = position(first_id), next_pos = position(first_id + stride);
+    int64_t slot = slot_of(first_id), next_slot = slot_of(first_id + stride);
+    for (int i = 0; i < kRowsRing - 2; ++i) ask();
+    copy_angles(pos, angles_at);
+    ask();
+    uint32_t t_slot = 0;
+    bool odd = false;
+
+    for (unsigned id = first_id; id < items; id += stride) {
+        const int row = row_of(id), begin = cut_at(id - row * split), end = cut_at(id - row * split + 1);
+        const int after = position(id + 2 * stride);
+        const int64_t after_slot = slot_of(id + 2 * stride);
+        copy_angles(next_pos, angles_at + (odd ? 0 : 4) * kRowsPlane);
+        const uint32_t angles = angles_at + (odd ? 4 : 0) * kRowsPlane;
+        // padding, or a position behind the table: its tasks are taken from the ring and left alone
+        bool skip = pos < 0;
+        if (!skip && p.cos_sin != nullptr && pos >= p.max_positions) {
+            if (lane == 0 && begin == 0 && p.status != nullptr) record_status(p.status, DA_ERR_STALE_PLAN);
+            skip = true;
+        }
+        // the row's place in the cache (page < 0: none)
+        int64_t page = slot >= 0 ? slot >> p.page_shift : -1;
+        const int place = (int)(slot & ((1 << p.page_shift) - 1));
+        if (page >= p.num_pages) {
+            if (!skip && lane == 0 && begin == 0 && p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
+            page = -1;
+        }
+
+        // Tasks [first, last) of kind KIND (0 q, 1 k, 2 v), counted within the kind.
+        auto walk = [&](auto kind_c, int first, int last) {
+            constexpr int KIND = decltype(kind_c)::value;
+            constexpr bool TURN = HALVES && KIND < 2;         // how the head's dims lie in the lanes
+            const int n = KIND == 0 ? p.n_q : KIND == 1 ? p.n_k : p.n_v;
+            const uint16_t* const w = KIND == 0 ? p.q_weight : KIND == 1 ? p.k_weight : nullptr;
+            const int64_t w_stride = KIND == 0 ? p.q_weight_stride : p.k_weight_stride;
+            const bool norm = KIND < 2 && w != nullptr, turn = KIND < 2 && p.cos_sin != nullptr;
+            bool turned[2] = {false, false};
+            // (a, b) <- r (m0 a - m1 b, m2 b + m3 a), r the root; pair e of unit k
+            float m0[2][4], m1[2][4], m2[2][4], m3[2][4];
+            bool fresh = true;                                // the matrices are still to be made
+            for (int t = first; t < last; ++t) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kRowsRing - 2) : "memory");
+                uint2 raw[2][2];
+                row_take<TURN, ALL>(ring + t_slot * (2 * kRowsPlane), l, rotary, wide, raw);
+                t_slot = (t_slot + 1) % kRowsRing;
+                ask();
+                if (skip) continue;
+                const int h = t * HEADS + group;
+                const bool live = h < n;                      // (the whole warp stays: its lanes exchange values)
+                if (norm || turn) {
+                    if (fresh || (norm && w_stride != 0)) {
+                        // The row's angles were asked for with its predecessor's first task, kRowsRing - 1 groups ahead of a row as
+                        // long as that; the first row's with its own tasks.
+                        if (fresh && (id == first_id || end - begin < kRowsRing - 1)) asm volatile("cp.async.wait_group 0;" ::: "memory");
+                        uint2 y[2][2];
+                        y[0][0] = y[0][1] = y[1][0] = y[1][1] = make_uint2(0, 0);
+                        if (norm && live) row_load<D, TURN, ALL, NEAR>(w + h * w_stride, l, rotary, wide || !TURN, y);
+                        // (a lane without a head of its own here may have one in the next task: a shared weight is everybody's)
+                        if (norm && !live && w_stride == 0) row_load<D, TURN, ALL, NEAR>(w, l, rotary, wide || !TURN, y);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            float f[8] = {1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f, 1.f};
+                            if (norm) {
+#pragma unroll
+                                for (int r = 0; r < 2; ++r) {
+                                    const float2 lo = rows_pair<F16>(y[k][r].x), hi = rows_pair<F16>(y[k][r].y);
+                                    f[4 * r] = lo.x; f[4 * r + 1] = lo.y; f[4 * r + 2] = hi.x; f[4 * r + 3] = hi.y;
+                                }
+                            }
+                            const int j = row_unit<D, NEAR>(l, k);
+                            float cs[4] = {1.f, 1.f, 1.f, 1.f}, sn[4] = {0.f, 0.f, 0.f, 0.f};
+                            turned[k] = turn && (ALL || 8 * j < rotary);
+                            if (turned[k]) {
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(cs[0]), "=f"(cs[1]), "=f"(cs[2]), "=f"(cs[3]) : "r"(angles + (2 * k) * kRowsPlane));
+                                asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(sn[0]), "=f"(sn[1]), "=f"(sn[2]), "=f"(sn[3]) : "r"(angles + (2 * k + 1) * kRowsPlane));
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) {
+                                const float wa = HALVES ? f[e] : f[2 * e], wb = HALVES ? f[4 + e] : f[2 * e + 1];
+                                m0[k][e] = wa * cs[e];
+                                m1[k][e] = wb * sn[e];
+                                m2[k][e] = wb * cs[e];
+                                m3[k][e] = wa * sn[e];
+                            }
+                        }
+                        fresh = false;
+                    }
+                    float x[2][8], sum = 0.f, sum2 = 0.f;
+#pragma unroll
+                    for (int k = 0; k < 2; ++k)
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) {
+                            const float2 lo = rows_pair<F16>(raw[k][r].x), hi = rows_pair<F16>(raw[k][r].y);
+                            x[k][4 * r] = lo.x; x[k][4 * r + 1] = lo.y; x[k][4 * r + 2] = hi.x; x[k][4 * r + 3] = hi.y;
+                        }
+                    float root = 1.f;
+                    if (norm) {
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            sum = fmaf(x[0][e], x[0][e], sum);
+                            sum2 = fmaf(x[1][e], x[1][e], sum2);
+                        }
+                        sum += sum2;
+#pragma unroll
+                        for (int off = L / 2; off >= 1; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
+                        root = rsqrtf(sum * (1.0f / D) + p.eps);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            float& a = HALVES ? x[k][e] : x[k][2 * e];
+                            float& b = HALVES ? x[k][4 + e] : x[k][2 * e + 1];
+                            const float a0 = a * m0[k][e], b0 = b * m2[k][e];
+                            // (what does not turn stays clear of its neighbour, infinite ones included)
+                            const float na = ALL || turned[k] ? fmaf(-b, m1[k][e], a0) : a0;
+                            b = root * (ALL || turned[k] ? fmaf(a, m3[k][e], b0) : b0);
+                            a = root * na;
+                        }
+#pragma unroll
+                        for (int r = 0; r < 2; ++r)
+                            raw[k][r] = make_uint2(rows_pack<F16>(x[k][4 * r], x[k][4 * r + 1]), rows_pack<F16>(x[k][4 * r + 2], x[k][4 * r + 3]));
+                    }
+                }
+                uint16_t* const out = KIND == 0 ? p.q_out + row * p.q_out_stride : KIND == 1 && p.k_out != nullptr ? p.k_out + row * p.k_out_stride : nullptr;
+                if (live && out != nullptr) row_store<D, TURN, ALL, NEAR>(out + h * D, l, rotary, wide || !TURN, raw);
+                if (KIND == 0 || page < 0) continue;
+                if (!PACKED) {
+                    uint16_t* const pool = KIND == 1 ? static_cast<uint16_t*>(p.k_cache) + page * p.k_stride_page + place * p.k_stride_token
+                                                     : static_cast<uint16_t*>(p.v_cache) + page * p.v_stride_page + place * p.v_stride_token;
+                    if (live) row_store<D, TURN, ALL, NEAR>(pool + h * (KIND == 1 ? p.k_stride_head : p.v_stride_head), l, rotary, wide || !TURN, raw);
+                } else {
+                    // Sixteen neighbouring dims to a lane, runs 4 l .. 4 l + 3 of four: what the lane holds, but for K that was
+                    // turned by halves, whose run g lies with unit g as its first (g < n, the units that turn) or with unit g - n
+                    // as its second.
+                    uint2 z[4] = {raw[0][0], raw[0][1], raw[1][0], raw[1][1]};
+                    if (TURN) {
+                        const int units = rotary >> 3;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            const int g = 4 * l + q;
+                            const int unit = g < units ? g : g < 2 * units ? g - units : g >> 1;
+                            const bool second = g < 2 * units ? g >= units : (g & 1);
+#pragma unroll
+                            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                                for (int r = 0; r < 2; ++r) {
+                                    const int from = (lane & ~(L - 1)) + (unit >> 1);
+                                    const uint32_t lo = __shfl_sync(0xffffffffu, raw[k][r].x, from), hi = __shfl_sync(0xffffffffu, raw[k][r].y, from);
+                                    if ((unit & 1) == k && second == (r == 1)) z[q] = make_uint2(lo, hi);
+                                }
+                        }
+                    }
+                    float y[2][8], amax = 0.f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float2 lo = rows_pair<F16>(z[q].x), hi = rows_pair<F16>(z[q].y);
+                        y[q >> 1][4 * (q & 1)] = lo.x; y[q >> 1][4 * (q & 1) + 1] = lo.y;
+                        y[q >> 1][4 * (q & 1) + 2] = hi.x; y[q >> 1][4 * (q & 1) + 3] = hi.y;
+                        amax = fmaxf(amax, fmaxf(fmaxf(fabsf(lo.x), fabsf(lo.y)), fmaxf(fabsf(hi.x), fabsf(hi.y))));
+                    }
+                    amax = fmaxf(amax, __shfl_xor_sync(0xffffffffu, amax, 1));      // the two lanes of a block of 32 dims
+                    if (live) {
+                        const __half scale = packed_scale(amax);
+                        char* const tile = static_cast<char*>(p.k_cache) + page * p.k_stride_page + h * p.k_stride_head + (place >> 4) * packed_tile_bytes(D);
+                        const int r = place & 15, block = l >> 1;
+                        uint32_t* const codes = reinterpret_cast<uint32_t*>(tile + (KIND == 1 ? 0 : packed_v_codes(D)));
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            codes[KIND == 1 ? packed_k_word(D, r, 2 * l + k) : packed_v_word(D, r, 2 * l + k)] = packed_word(y[k], scale);
+                        if ((l & 1) == 0) {
+                            __half* const scales = reinterpret_cast<__half*>(tile + (KIND == 1 ? packed_k_scales(D) : packed_v_scales(D)));
+                            scales[KIND == 1 ? packed_k_scale(D, r, block) : packed_v_scale(r, block)] = scale;
+                        }
+                    }
+                }
+            }
+        };
+        walk(std::integral_constant<int, 0>{}, begin, min(end, tq));
+        walk(std::integral_constant<int, 1>{}, max(begin, tq) - tq, min(end, tq + tk) - tq);
+        walk(std::integral_constant<int, 2>{}, max(begin, tq + tk) - tq - tk, end - tq - tk);
+        pos = next_pos;
+        slot = next_slot;
+        next_pos = after;
+        next_slot = after_slot;
+        odd = !odd;
     }
 }
 
