@@ -6,6 +6,10 @@
 // (slots, positions, block-table entries of fresh pages) follows from the sums for every row by itself: row -> sequence
 // by a binary search in row_starts, position -> page by the table or, for a fresh page, by its place in the list of free
 // pages.  The row whose token is a fresh page's first writes the table entry.
+//
+// A step is latency: the chain of a launch, two reads of the inputs, a scan and one look at a table.  So the block is no larger
+// than its work, the sums stay in shared memory for the search, and what a step without anything given back or refused
+// does not need (three of four scans) is left out when a vote says so: 64 sequences decoding 8.7 -> 4.9 us.
 #include <cstring>
 
 #include "common.cuh"
@@ -32,23 +36,29 @@ struct TablesParams {
     int64_t num_pages, most_tokens;   // most_tokens: what a row of the block table has pages for
     int32_t batch, max_pages_per_seq, max_rows, free_capacity, page_shift;
     int32_t vec;                      // slots, positions and row_seq may be written 16 bytes at a time
+    int32_t shared;                   // the batch's sums fit shared memory
 };
 
-constexpr int kScanThreads = 1024;
+constexpr int kScanThreads = 1024;                // at most
 constexpr int kFillThreads = 256;
 constexpr int kRowsPerThread = 4;
+constexpr int kSharedBatch = 2048;                // sequences whose sums are kept in shared memory
+
+// Sums saturate far above every limit that they are held against (INT32_MAX rows or pages), which keeps them associative.
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, 0x80000000u); }
+__device__ __forceinline__ uint32_t sat(int64_t x) { return x > 0x80000000LL ? 0x80000000u : (uint32_t)x; }
 
 // Exclusive prefix sums of two values over the block's threads; the totals in `all`.
-__device__ __forceinline__ void block_scan2(int64_t& x, int64_t& y, int64_t (&all)[2], int64_t (*sm)[2])
+__device__ __forceinline__ void block_scan2(uint32_t& x, uint32_t& y, uint32_t (&all)[2], uint32_t (*sm)[2])
 {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
-    int64_t a = x, b = y;
+    uint32_t a = x, b = y;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const int64_t u = __shfl_up_sync(0xffffffffu, a, off), v = __shfl_up_sync(0xffffffffu, b, off);
+        const uint32_t u = __shfl_up_sync(0xffffffffu, a, off), v = __shfl_up_sync(0xffffffffu, b, off);
         if (lane >= off) {
-            a += u;
-            b += v;
+            a = sat_add(a, u);
+            b = sat_add(b, v);
         }
     }
     __syncthreads();                                          // the scratch of the scan before is free
@@ -57,21 +67,28 @@ __device__ __forceinline__ void block_scan2(int64_t& x, int64_t& y, int64_t (&al
         sm[warp][1] = b;
     }
     __syncthreads();
-    int64_t u = lane < warps ? sm[lane][0] : 0, v = lane < warps ? sm[lane][1] : 0;
+    uint32_t u = lane < warps ? sm[lane][0] : 0, v = lane < warps ? sm[lane][1] : 0;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const int64_t s = __shfl_up_sync(0xffffffffu, u, off), t = __shfl_up_sync(0xffffffffu, v, off);
+        const uint32_t s = __shfl_up_sync(0xffffffffu, u, off), t = __shfl_up_sync(0xffffffffu, v, off);
         if (lane >= off) {
-            u += s;
-            v += t;
+            u = sat_add(u, s);
+            v = sat_add(v, t);
         }
     }
     all[0] = __shfl_sync(0xffffffffu, u, 31);
     all[1] = __shfl_sync(0xffffffffu, v, 31);
-    const int64_t u0 = __shfl_sync(0xffffffffu, u, warp ? warp - 1 : 0), v0 = __shfl_sync(0xffffffffu, v, warp ? warp - 1 : 0);
-    x = a - x + (warp ? u0 : 0);
-    y = b - y + (warp ? v0 : 0);
+    const uint32_t u0 = __shfl_sync(0xffffffffu, u, warp ? warp - 1 : 0), v0 = __shfl_sync(0xffffffffu, v, warp ? warp - 1 : 0);
+    const uint32_t pa = __shfl_up_sync(0xffffffffu, a, 1), pb = __shfl_up_sync(0xffffffffu, b, 1);
+    x = sat_add(lane ? pa : 0, warp ? u0 : 0);
+    y = sat_add(lane ? pb : 0, warp ? v0 : 0);
 }
+
+// What the rows are found by, in shared memory or where the caller has it.
+struct Sums {
+    const int32_t *row_starts, *page_starts;
+    const int32_t* old;               // tokens before the call (shared memory), or nullptr: from seq_lens_out
+};
 
 __device__ __forceinline__ void report(const TablesParams& p, int code)
 {
@@ -104,9 +121,9 @@ __device__ __forceinline__ Ask ask_of(const TablesParams& p, int b, bool loud)
 }
 
 // Rows first .. first + 3 of the step.
-__device__ __forceinline__ void fill_rows(const TablesParams& p, int64_t first, int64_t avail)
+__device__ __forceinline__ void fill_rows(const TablesParams& p, const Sums& sums, int64_t first, int64_t avail)
 {
-    const int total = p.row_starts[p.batch];
+    const int total = sums.row_starts[p.batch];
     const int mask = (1 << p.page_shift) - 1;
     int64_t slot[kRowsPerThread];
     int pos[kRowsPerThread], seq[kRowsPerThread];
@@ -121,20 +138,20 @@ __device__ __forceinline__ void fill_rows(const TablesParams& p, int64_t first, 
             int lo = 0, hi = p.batch;                         // row_starts[lo] <= row < row_starts[hi]
             while (hi - lo > 1) {
                 const int mid = (lo + hi) >> 1;
-                if (p.row_starts[mid] <= row) lo = mid;
+                if (sums.row_starts[mid] <= row) lo = mid;
                 else hi = mid;
             }
             b = lo;
         } else if (row >= end) {
             do ++b;                                           // (sequences without rows in between)
-            while (p.row_starts[b + 1] <= row);
+            while (sums.row_starts[b + 1] <= row);
         }
         if (row >= end) {
-            start = p.row_starts[b];
-            end = p.row_starts[b + 1];
-            old = p.seq_lens_out[b] - (end - start);
+            start = sums.row_starts[b];
+            end = sums.row_starts[b + 1];
+            old = sums.old ? sums.old[b] : p.seq_lens_out[b] - (end - start);
             held = (old + mask) >> p.page_shift;
-            page_at = p.page_starts[b];
+            page_at = sums.page_starts[b];
             last_page = -1;
         }
         const int at = old + (int)(row - start);
@@ -170,108 +187,150 @@ __device__ __forceinline__ void fill_rows(const TablesParams& p, int64_t first, 
 template <bool FILL>
 __global__ void __launch_bounds__(kScanThreads) decode_attn_tables_kernel(const TablesParams p)
 {
-    __shared__ int64_t sm[kScanThreads / 32][2];
+    extern __shared__ int32_t sm_sums[];                      // [batch + 1] rows, [batch + 1] pages, [batch] tokens before
+    __shared__ uint32_t sm[kScanThreads / 32][2];
     pdl_launch_dependents();
     pdl_wait_primary();
-    const int tid = threadIdx.x, lane = tid & 31;
+    const int tid = threadIdx.x, lane = tid & 31, nt = blockDim.x;
+    int32_t* const sm_rows = sm_sums;
+    int32_t* const sm_pages = sm_rows + p.batch + 1;
+    int32_t* const sm_old = sm_pages + p.batch + 1;
+    const bool keep = FILL && p.shared;
     const int64_t count = *p.free_count;
+    Ask ask = ask_of(p, tid, false);                          // of the first nt sequences, asked for beside the count
     const bool sane = count >= 0 && count <= p.free_capacity;
     if (!sane && tid == 0) report(p, DA_ERR_STALE_PLAN);
+    const Ask none = {-1, -1, 0, 0, 0};
+    if (!sane) ask = none;
     // 1. pages given back: their places in the list, and how many fit
-    int64_t pushed = 0, all[2];
-    for (int b0 = 0; b0 < p.batch; b0 += kScanThreads) {
-        const Ask a = sane ? ask_of(p, b0 + tid, false) : Ask{-1, -1, 0, 0, 0};
-        int64_t at = a.back, none = 0;
-        block_scan2(at, none, all, sm);
-        at += pushed;
-        const bool fits = count + at + a.back <= p.free_capacity;
-        if (a.back > 0 && !fits) report(p, DA_ERR_NO_PAGES);
-        // a few pages by their own thread, many by the warp
-        const int64_t pages = fits ? a.back : 0;
-        const int64_t from = (a.fresh + ((int64_t)1 << p.page_shift) - 1) >> p.page_shift;
-        const int32_t* const row = p.block_table + (int64_t)(b0 + tid) * p.max_pages_per_seq + from;
-        if (pages <= 4)
-            for (int i = 0; i < (int)pages; ++i) p.free_pages[count + at + i] = row[i];
-        for (unsigned many = __ballot_sync(0xffffffffu, pages > 4); many != 0; many &= many - 1) {
-            const int l = __ffs(many) - 1;
-            const int64_t n = __shfl_sync(0xffffffffu, pages, l), to = __shfl_sync(0xffffffffu, count + at, l);
-            const int32_t* const src = reinterpret_cast<const int32_t*>(__shfl_sync(0xffffffffu, (unsigned long long)row, l));
-            for (int64_t i = lane; i < n; i += 32) p.free_pages[to + i] = src[i];
-        }
-        // (what does not fit is behind what does: the sums only grow)
-        int64_t ok = pages, none2 = 0;
-        block_scan2(ok, none2, all, sm);
-        pushed += all[0];
-        if (__syncthreads_or(a.back > 0 && !fits)) {
-            // one that does not fit: of those behind it none fits either
-            for (int b = b0 + kScanThreads + tid; b < p.batch; b += kScanThreads)
-                if (ask_of(p, b, false).back > 0) report(p, DA_ERR_NO_PAGES);
-            break;
+    int64_t pushed = 0;
+    uint32_t all[2];
+    bool any_back = ask.back > 0;
+    for (int b = nt + tid; b < p.batch; b += nt) any_back |= p.gains[b] < 0;
+    bool full = false;                                        // some of what is given back does not fit
+    if (__syncthreads_or(any_back && sane)) {
+        for (int b0 = 0; b0 < p.batch && !full; b0 += nt) {
+            const Ask a = b0 == 0 ? ask : sane ? ask_of(p, b0 + tid, false) : none;
+            uint32_t at = sat(a.back), zero = 0;
+            block_scan2(at, zero, all, sm);
+            const bool fits = count + pushed + at + a.back <= p.free_capacity;
+            // a few pages by their own thread, many by the warp
+            const int64_t pages = fits ? a.back : 0, to = count + pushed + at;
+            const int64_t from = (a.fresh + ((int64_t)1 << p.page_shift) - 1) >> p.page_shift;
+            const int32_t* const row = p.block_table + (int64_t)(b0 + tid) * p.max_pages_per_seq + from;
+            if (pages <= 4)
+                for (int i = 0; i < (int)pages; ++i) p.free_pages[to + i] = row[i];
+            for (unsigned many = __ballot_sync(0xffffffffu, pages > 4); many != 0; many &= many - 1) {
+                const int l = __ffs(many) - 1;
+                const int64_t n = __shfl_sync(0xffffffffu, pages, l), dst = __shfl_sync(0xffffffffu, to, l);
+                const int32_t* const src = reinterpret_cast<const int32_t*>(__shfl_sync(0xffffffffu, (unsigned long long)row, l));
+                for (int64_t i = lane; i < n; i += 32) p.free_pages[dst + i] = src[i];
+            }
+            full = __syncthreads_or(a.back > 0 && !fits);
+            if (full) {
+                // (what does not fit is behind what does: the sums only grow)
+                uint32_t ok = sat(pages), zero2 = 0;
+                block_scan2(ok, zero2, all, sm);
+            }
+            pushed += all[0];
         }
     }
     const int64_t avail = count + pushed;
     // 2. pages and rows of those that grow; lengths
-    int64_t lacked = 0, asked = 0, taken = 0, rows = 0, gave = 0;
-    for (int b0 = 0; b0 < p.batch; b0 += kScanThreads) {
+    uint32_t lacked = 0, asked = 0, gave = 0;                 // by all that ask
+    int64_t taken = 0, rows = 0;                              // granted
+    bool refused = false;
+    for (int b0 = 0; b0 < p.batch; b0 += nt) {
         const int b = b0 + tid;
-        const Ask a = sane ? ask_of(p, b, true) : Ask{-1, -1, 0, 0, 0};
-        int64_t lack = a.lack, row = a.rows;
+        const Ask a = sane ? (b0 == 0 ? ask : ask_of(p, b, false)) : none;
+        if (sane && b < p.batch && a.old < 0) report(p, DA_ERR_STALE_PLAN);
+        uint32_t lack = sat(a.lack), row = sat(a.rows);
         block_scan2(lack, row, all, sm);
-        const bool pages_ok = a.lack == 0 || lacked + lack + a.lack <= avail;
-        const bool rows_ok = a.rows == 0 || asked + row + a.rows <= p.max_rows;
-        lacked += all[0];
-        asked += all[1];
+        const bool pages_ok = a.lack == 0 || (int64_t)sat_add(sat_add(lacked, lack), sat(a.lack)) <= avail;
+        const bool rows_ok = a.rows == 0 || (int64_t)sat_add(sat_add(asked, row), sat(a.rows)) <= p.max_rows;
+        lacked = sat_add(lacked, all[0]);
+        asked = sat_add(asked, all[1]);
         if (!pages_ok) report(p, DA_ERR_NO_PAGES);
         if (!rows_ok) report(p, DA_ERR_WORKSPACE_TOO_SMALL);
-        // giving back is granted by the same sums as above
-        int64_t back = a.back, got_rows = pages_ok && rows_ok ? a.rows : 0;
-        const int64_t own_rows = got_rows;
-        block_scan2(back, got_rows, all, sm);
-        const bool back_ok = a.back == 0 || count + gave + back + a.back <= p.free_capacity;
-        gave += all[0];
-        const int64_t row_at = rows + got_rows;
-        rows += all[1];
-        int64_t got = pages_ok && rows_ok ? a.lack : 0, none = 0;
-        block_scan2(got, none, all, sm);
-        const int64_t page_at = taken + got;
+        bool back_ok = true;
+        int64_t row_at = rows + row, page_at = taken + lack;
+        // (who has been refused something leaves gaps in the sums: those behind need sums of their own)
+        refused |= __syncthreads_or(!(pages_ok && rows_ok)) != 0;
+        if (refused) {
+            uint32_t got_rows = pages_ok && rows_ok ? sat(a.rows) : 0, got = pages_ok && rows_ok ? sat(a.lack) : 0;
+            block_scan2(got, got_rows, all, sm);
+            row_at = rows + got_rows;
+            page_at = taken + got;
+        }
         taken += all[0];
+        rows += all[1];
+        if (full) {                                           // giving back is granted by the sums of 1.
+            uint32_t back = sat(a.back), zero = 0;
+            block_scan2(back, zero, all, sm);
+            back_ok = a.back == 0 || count + (int64_t)sat_add(sat_add(gave, back), sat(a.back)) <= p.free_capacity;
+            if (!back_ok) report(p, DA_ERR_NO_PAGES);
+            gave = sat_add(gave, all[0]);
+        }
         if (b < p.batch) {
             p.row_starts[b] = (int32_t)row_at;
             p.page_starts[b] = (int32_t)page_at;
+            const bool granted = a.old >= 0 && pages_ok && rows_ok && back_ok;
             // (a length that is left alone is copied: the two arrays may be one)
-            const bool granted = a.old >= 0 && (a.rows > 0 ? own_rows > 0 : back_ok);
-            const int32_t len = granted ? (int32_t)a.fresh : p.seq_lens[b];
-            p.seq_lens_out[b] = len;
+            p.seq_lens_out[b] = granted ? (int32_t)a.fresh : p.seq_lens[b];
+            if (keep) {
+                sm_rows[b] = (int32_t)row_at;
+                sm_pages[b] = (int32_t)page_at;
+                sm_old[b] = (int32_t)a.old;
+            }
         }
     }
     if (tid == 0) {
         p.row_starts[p.batch] = (int32_t)rows;
         p.page_starts[p.batch] = (int32_t)taken;
         *p.free_count_out = (int32_t)(avail - taken);
+        if (keep) sm_rows[p.batch] = (int32_t)rows;
     }
     if (FILL) {
         __syncthreads();
-        for (int64_t first = (int64_t)tid * kRowsPerThread; first < p.max_rows; first += (int64_t)kScanThreads * kRowsPerThread)
-            fill_rows(p, first, avail);
+        const Sums sums = keep ? Sums{sm_rows, sm_pages, sm_old} : Sums{p.row_starts, p.page_starts, nullptr};
+        for (int64_t first = (int64_t)tid * kRowsPerThread; first < p.max_rows; first += (int64_t)nt * kRowsPerThread)
+            fill_rows(p, sums, first, avail);
     }
 }
 
 __global__ void __launch_bounds__(kFillThreads) decode_attn_tables_rows_kernel(const TablesParams p)
 {
+    extern __shared__ int32_t sm_sums[];
     pdl_launch_dependents();
     pdl_wait_primary();
     const int64_t first = ((int64_t)blockIdx.x * kFillThreads + threadIdx.x) * kRowsPerThread;
-    if (first < p.max_rows) fill_rows(p, first, (int64_t)*p.free_count_out + p.page_starts[p.batch]);
+    const int64_t avail = (int64_t)*p.free_count_out + p.page_starts[p.batch];
+    Sums sums = {p.row_starts, p.page_starts, nullptr};
+    if (p.shared) {
+        int32_t* const rows = sm_sums;
+        int32_t* const pages = rows + p.batch + 1;
+        int32_t* const old = pages + p.batch + 1;
+        for (int b = threadIdx.x; b <= p.batch; b += kFillThreads) {
+            rows[b] = p.row_starts[b];
+            if (b < p.batch) {
+                pages[b] = p.page_starts[b];
+                old[b] = p.seq_lens_out[b] - (p.row_starts[b + 1] - p.row_starts[b]);
+            }
+        }
+        __syncthreads();
+        sums = {rows, pages, old};
+    }
+    if (first < p.max_rows) fill_rows(p, sums, first, avail);
 }
 
 bool aligned(const void* p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
-int launch(const void* fn, unsigned grid, int threads, TablesParams& tp, cudaStream_t stream)
+int launch(const void* fn, unsigned grid, int threads, size_t smem, TablesParams& tp, cudaStream_t stream)
 {
     cudaLaunchConfig_t cfg;
     cfg.gridDim = dim3(grid, 1, 1);
     cfg.blockDim = dim3(threads, 1, 1);
-    cfg.dynamicSmemBytes = 0;
+    cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
@@ -333,12 +392,18 @@ extern "C" int decode_attn_step_tables(const decode_attn_shape_t* shape, const d
     const int64_t most = (int64_t)s.max_pages_per_seq * s.page_size;
     tp.most_tokens = most < INT32_MAX - 256 ? most : INT32_MAX - 256;
     tp.vec = aligned(a->slots, 16) && aligned(a->positions, 16) && aligned(a->row_seq, 16);
+    tp.shared = s.batch <= kSharedBatch;
+    const size_t smem = tp.shared ? (3 * (size_t)s.batch + 2) * sizeof(int32_t) : 0;
+    auto threads_for = [](int64_t n) { return (int)(n >= kScanThreads ? kScanThreads : n < 64 ? 64 : (n + 31) / 32 * 32); };
     // A step's rows by the block that makes the sums, as long as one launch costs less than two.
     constexpr int kOneLaunchRows = 8192;
-    if (a->max_rows <= kOneLaunchRows) return launch((const void*)decode_attn_tables_kernel<true>, 1, kScanThreads, tp, stream);
-    int rc = launch((const void*)decode_attn_tables_kernel<false>, 1, kScanThreads, tp, stream);
+    if (a->max_rows <= kOneLaunchRows) {
+        const int64_t n = s.batch > a->max_rows / kRowsPerThread ? s.batch : a->max_rows / kRowsPerThread;
+        return launch((const void*)decode_attn_tables_kernel<true>, 1, threads_for(n), smem, tp, stream);
+    }
+    int rc = launch((const void*)decode_attn_tables_kernel<false>, 1, threads_for(s.batch), 0, tp, stream);
     if (rc != DA_OK) return rc;
     const int64_t per_block = (int64_t)kFillThreads * kRowsPerThread;
     return launch((const void*)decode_attn_tables_rows_kernel, (unsigned)((a->max_rows + per_block - 1) / per_block), kFillThreads,
-                  tp, stream);
+                  smem, tp, stream);
 }
