@@ -58,6 +58,14 @@ __device__ __forceinline__ void copy_16(uint32_t dst, const void* src, uint64_t 
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(l2_policy) : "memory");
 }
 
+// Hints to L2: nothing to wait for.
+__device__ __forceinline__ void prefetch_tile(const void* src, uint32_t bytes)
+{
+    asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(src), "r"(bytes) : "memory");
+}
+
+__device__ __forceinline__ void prefetch_line(const void* src) { asm volatile("prefetch.global.L2 [%0];" ::"l"(src) : "memory"); }
+
 __device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
 template <int N>
@@ -151,6 +159,24 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
     float* const sm_wm = sm_wo + W * Cfg::kCols * D;                                                  // [W][kCols]
     float* const sm_wl = sm_wm + W * Cfg::kCols;
     decode_attn_unit_t u = load_unit(p.units, ubeg);
+    {
+        // Hints, while the kernel before this one drains: the tiles of every warp's first steps and the lines that its
+        // critical path reads are asked into L2.  What is read for it here may be about to change; it steers prefetches only
+        // and is read again behind the wait.
+        const WindowCut cut = EXT ? window_cut(u.seq_len, p.window, p.sinks) : WindowCut{0, 0, 0};
+        const int tile = 2 * (warp + W * (lane >> 1)) + (lane & 1), at = (u.tok_begin >> 4) + tile;
+        const bool masked = p.run_mask != nullptr && __ldcg(p.run_mask + u.seq) == 0;
+        if (!masked && lane < 2 * NS && tile < (u.tok_end - u.tok_begin + 15) >> 4) {
+            const int where = EXT ? window_tile(cut, at) : at;
+            const int page = __ldcg(p.block_table + (int64_t)u.seq * p.max_pages_per_seq + (where >> p.tile_shift));
+            if ((unsigned)page < (unsigned)p.num_pages)
+                prefetch_tile(reinterpret_cast<const char*>(p.k) + page * p.k_stride_page + u.kv_head * p.k_stride_head +
+                                  (where & ((1 << p.tile_shift) - 1)) * Cfg::kTile, Cfg::kTile);
+        }
+        if (warp == 0 && lane >= 16 && (lane - 16) * 128 < heads * D * 2)
+            prefetch_line(reinterpret_cast<const char*>(p.q + ((int64_t)u.seq * p.num_q_heads + u.kv_head * G + head0) * D) + (lane - 16) * 128);
+        if (warp == 0 && lane == 15) prefetch_line(p.seq_lens + u.seq);
+    }
     pdl_wait_primary();
 
     auto cut_of = [&](const decode_attn_unit_t& x) { return EXT ? window_cut(x.seq_len, p.window, p.sinks) : WindowCut{0, 0, 0}; };
