@@ -328,3 +328,78 @@ def test_expanding_reports_what_does_not_fit():
     call()
     assert int(status) == da.DA_ERR_STALE_PLAN
     assert (k[3:] == 7).all() and not (k[0] == 7).all()
+
+
+# ------------------------------------------------------------------------------------------------ many rows
+
+@pytest.mark.parametrize("hq,hkv,d,parts", [(4, 1, 128, "q"), (1, 1, 64, "qkv"), (9, 1, 128, "qkv"), (32, 8, 128, "qkv"), (2, 2, 64, "kv")])
+@pytest.mark.parametrize("n", [2367, 2369, 9001])
+def test_more_rows_than_warps(hq, hkv, d, parts, n):
+    """Warps go from row to row: few and many tasks a row, rows of padding and bad positions among them."""
+    r = Rows(n, hq, hkv, d, far=700, page=64, seed=n + hq)
+    gen = torch.Generator().manual_seed(n)
+    dead = torch.rand(n, generator=gen) < 0.1
+    r.positions[dead] = -1
+    lost = torch.rand(n, generator=gen) < 0.02
+    r.positions[lost & ~dead] = 700 + 5
+    q_out, (k_pool, v_pool), k_out = r.q_out(7.0), r.pools(7.0), torch.full((n, hkv, d), 7.0, dtype=r.dtype, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    args = dict(status=status)
+    args |= dict(q_out=q_out) if "q" in parts else dict(q=None, q_weight=None)
+    args |= dict(k_out=k_out, k_cache=k_pool, v_cache=v_pool) if "kv" in parts else dict(k=None, v=None, k_weight=None, slots=None)
+    r.call(**args)
+    assert int(status) == da.DA_ERR_STALE_PLAN
+    live = ~dead & ~lost
+    r.positions[~live] = 0
+    q, k, v = r.expect()
+    keep = live.numpy()
+    if "q" in parts:
+        close(q_out[live.cuda()], q[keep], r.dtype, "q")
+        assert (q_out[~live.cuda()] == 7.0).all()
+    if "kv" in parts:
+        close(k_out[live.cuda()], k[keep], r.dtype, "k")
+        assert torch.equal(of_slots(k_pool, r.slots[live]), k_out[live.cuda()])
+        assert torch.equal(of_slots(v_pool, r.slots[live]).cpu(), list(r.split(r.qkv))[2][live])
+        assert (of_slots(v_pool, r.slots[~live]) == 7.0).all()
+
+
+def test_fewer_rows_than_the_tensors_hold():
+    r = Rows(40, 8, 2, 128, seed=12)
+    q_out, (k_pool, v_pool) = r.q_out(7.0), r.pools(7.0)
+    r.call(q_out=q_out, k_cache=k_pool, v_cache=v_pool, rows=17)
+    close(q_out[:17], r.expect()[0][:17], r.dtype)
+    assert (q_out[17:] == 7.0).all() and (of_slots(v_pool, r.slots[17:]) == 7.0).all()
+
+
+@pytest.mark.parametrize("cache_bits", [16, 4])
+def test_pools_beyond_32_bits(cache_bits):
+    """Slots whose bytes lie past 2^32 (and whose elements lie past 2^31)."""
+    r = Rows(30, 4, 2, 128, page=16, seed=13)
+    head = da.decode_attn_packed_head_bytes(128, 16)
+    r.num_pages = (5 << 30) // (2 * head) if cache_bits == 4 else (5 << 30) // (16 * 2 * 128 * 2)
+    r.slots = torch.arange(30) * 7 + (r.num_pages - 20) * 16
+    q_out = r.q_out()
+    k_out = torch.zeros((30, 2, 128), dtype=r.dtype, device="cuda")
+    if cache_bits == 4:
+        pool = torch.empty((r.num_pages, 2, head), dtype=torch.uint8, device="cuda")
+        pool[-20:] = 0
+        r.call(4, q_out=q_out, k_out=k_out, k_cache=pool)
+        r.slots -= (r.num_pages - 20) * 16
+        got_k, got_v = stored(r, pool[-20:])
+        code, scale = ref.encode(k_out.double().cpu().numpy())
+        assert np.array_equal(got_k, ref.values(code, scale))
+        # the same pages expanded, through a table that names them
+        table = torch.arange(r.num_pages - 20, r.num_pages, dtype=torch.int32, device="cuda")[None]
+        k, v = (torch.zeros((20, 16, 2, 128), dtype=r.dtype, device="cuda") for _ in range(2))
+        shape = da.make_shape(1, 4, 2, 128, 16, 20, 20, (16 * 256, 256, 128))
+        packed = da.make_kv4_shape(1, 4, 2, 128, 16, 20, r.num_pages)
+        da.decode_attn_expand_kv(shape, packed, pool, table, torch.tensor([320], dtype=torch.int32).cuda(),
+                                 torch.arange(20, dtype=torch.int32, device="cuda")[None].contiguous(), k, v)
+        assert torch.equal(of_slots(k, r.slots).cpu(), torch.from_numpy(got_k).to(r.dtype))
+        assert torch.equal(of_slots(v, r.slots).cpu(), torch.from_numpy(got_v).to(r.dtype))
+    else:
+        k_pool, v_pool = (torch.empty((r.num_pages, 16, 2, 128), dtype=r.dtype, device="cuda") for _ in range(2))
+        r.call(q_out=q_out, k_out=k_out, k_cache=k_pool, v_cache=v_pool)
+        assert torch.equal(of_slots(k_pool, r.slots), k_out)
+        assert torch.equal(of_slots(v_pool, r.slots).cpu(), list(r.split(r.qkv))[2])
+    close(k_out, r.expect()[1], r.dtype)

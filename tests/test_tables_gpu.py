@@ -171,3 +171,31 @@ def test_many_steps_in_a_graph_lose_no_page():
                 assert int(t["slots"][starts[b] + i]) == table[b][p // page] * page + p % page
     assert int(t["status"]) == da.DA_OK
     del graph
+
+
+@pytest.mark.parametrize("rows", [500, 20000])
+def test_nothing_is_written_beside_the_buffers(rows):
+    s = Step(*mixed(200, 9, grow=rows // 60), seed=4)
+    s.max_rows += 13
+    s.put()
+    held = {}
+    for name in ("seq_lens_out", "block_table", "free_pages", "free_count_out", "row_starts", "page_starts", "slots", "positions",
+                 "row_seq", "status"):
+        x = s.t[name]
+        big = torch.full((x.numel() + 64,), 1234567, dtype=x.dtype, device="cuda")
+        big[32:32 + x.numel()] = x.reshape(-1)
+        held[name] = big
+        s.t[name] = big[32:32 + x.numel()].view(x.shape)
+    s.call().check()
+    for name, big in held.items():
+        assert (big[:32] == 1234567).all() and (big[-32:] == 1234567).all(), name
+
+
+def test_a_batch_larger_than_shared_memory():
+    n = 5000
+    rng = random.Random(3)
+    lens = [rng.randint(0, 90) for _ in range(n)]
+    for rows, gains in ((0, [rng.choice([0, 1, 1, 3]) for _ in range(n)]), (20000, [rng.randint(0, 9) for _ in range(n)])):
+        s = Step(lens, gains, seed=rows)
+        s.max_rows += rows
+        assert s.put().call().check()["status"] == da.DA_OK
