@@ -595,10 +595,13 @@ def _heads(x, rows: int, heads: int, dim: int, dtype):
     """Address and row stride of rows of heads [rows, heads, dim] that lie behind each other within a row."""
     if x is None:
         return 0, 0
-    size, (row, head, one) = x.shape, x.stride() if x.dim() == 3 else (0, 0, 0)
-    if one != 1 or x.dtype is not dtype or size[1] != heads or size[2] != dim or size[0] < rows or (head != dim and heads > 1):
+    size = x.shape
+    if len(size) != 3 or x.dtype is not dtype:
         raise DecodeAttnError(DA_ERR_INVALID_ARG, _ROWS_ERROR)
-    return x.data_ptr(), row if size[0] > 1 else heads * dim
+    (n, h, d), (row, head, one) = size, x.stride()
+    if one != 1 or h != heads or d != dim or n < rows or (head != dim and heads > 1):
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, _ROWS_ERROR)
+    return x.data_ptr(), row if n > 1 else heads * dim
 
 
 def _head_weight(w, heads: int, dim: int, dtype):
@@ -674,13 +677,14 @@ def decode_attn_step_tables(shape: Shape, seq_lens, gains, seq_lens_out, block_t
     [max_rows]; status [1] or None.  seq_lens_out may be seq_lens, free_count_out free_count."""
     _, _, _, i32, i64 = _dtypes()
     batch, max_rows, at = shape.batch, slots.numel(), _TABLES_ERROR
-    args = _TABLES_PACK(_TABLES_ARGS_SIZE, 0, max_rows, free_pages.numel(), _vector(seq_lens, i32, batch, at),
-                        _vector(gains, i32, batch, at), _vector(seq_lens_out, i32, batch, at),
-                        _vector(block_table, i32, batch * shape.max_pages_per_seq, at), _vector(free_pages, i32, 0, at),
-                        _vector(free_count, i32, 1, at), _vector(free_count_out, i32, 1, at),
-                        _vector(row_starts, i32, batch + 1, at), _vector(page_starts, i32, batch + 1, at),
-                        _vector(slots, i64, 0, at), _vector(positions, i32, max_rows, at), _vector(row_seq, i32, max_rows, at),
-                        _vector(status, i32, 1, at))
+    ptrs = []
+    for x, need in ((seq_lens, batch), (gains, batch), (seq_lens_out, batch), (block_table, batch * shape.max_pages_per_seq),
+                    (free_pages, 0), (free_count, 1), (free_count_out, 1), (row_starts, batch + 1), (page_starts, batch + 1)):
+        if x.dtype is not i32 or x.numel() < need or not x.is_contiguous():
+            raise DecodeAttnError(DA_ERR_INVALID_ARG, at)
+        ptrs.append(x.data_ptr())
+    args = _TABLES_PACK(_TABLES_ARGS_SIZE, 0, max_rows, free_pages.numel(), *ptrs, _vector(slots, i64, 0, at),
+                        _vector(positions, i32, max_rows, at), _vector(row_seq, i32, max_rows, at), _vector(status, i32, 1, at))
     rc = _lib.decode_attn_step_tables(shape, args, _stream(stream))
     if check and rc != DA_OK:
         _check(rc, at)

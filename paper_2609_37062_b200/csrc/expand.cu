@@ -7,6 +7,7 @@
 #include <cstring>
 
 #include "common.cuh"
+#include "opt_in.h"
 #include "packed.cuh"
 #include "planner.h"
 
@@ -215,10 +216,8 @@ extern "C" int decode_attn_expand_kv(const decode_attn_shape_t* shape, const dec
     auto fn = s.head_dim == 128 ? (f16 ? decode_attn_expand_kernel<128, true> : decode_attn_expand_kernel<128, false>)
                                 : (f16 ? decode_attn_expand_kernel<64, true> : decode_attn_expand_kernel<64, false>);
     const int smem = kExpandThreads / 32 * kExpandRing * packed_tile_bytes(s.head_dim);
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, smem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return DA_ERR_CUDA;
-    }
+    rc = opt_in_shared_memory((const void*)fn, smem);
+    if (rc != DA_OK) return rc;
     cudaLaunchConfig_t cfg;
     cfg.gridDim = dim3((unsigned)blocks, (unsigned)s.batch, 1);
     cfg.blockDim = dim3(kExpandThreads, 1, 1);

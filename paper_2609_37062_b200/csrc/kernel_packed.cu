@@ -1,6 +1,7 @@
 // Launches of the kernel for caches in 4 bits.
 #include "kernel_packed.cuh"
 #include "kernel_packed.h"
+#include "opt_in.h"
 
 namespace da {
 
@@ -13,11 +14,11 @@ struct PackedVariant {
     int threads, smem;
 };
 
-template <int D, bool F16, bool EXT, int W, int TEAMS>
+template <int D, bool F16, bool EXT, int W, int NT>
 PackedVariant variant(bool dup)
 {
-    using Cfg = PackedCfg<D, W, TEAMS>;
-    return {dup ? decode_attn_packed_kernel<D, F16, F16 && TEAMS == 1, EXT, W, TEAMS> : decode_attn_packed_kernel<D, F16, false, EXT, W, TEAMS>,
+    using Cfg = PackedCfg<D, W, NT>;
+    return {dup ? decode_attn_packed_kernel<D, F16, F16 && NT == 1, EXT, W, NT> : decode_attn_packed_kernel<D, F16, false, EXT, W, NT>,
             Cfg::kThreads, Cfg::kSmem};
 }
 
@@ -39,11 +40,7 @@ PackedVariant for_type(int G, bool f16, bool ext, bool big)
 int prepare(int D, int G, bool f16, bool ext, bool big, PackedVariant* v)
 {
     *v = D == 128 ? for_type<128>(G, f16, ext, big) : for_type<64>(G, f16, ext, big);
-    if (cudaFuncSetAttribute(v->fn, cudaFuncAttributeMaxDynamicSharedMemorySize, v->smem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return DA_ERR_CUDA;
-    }
-    return DA_OK;
+    return opt_in_shared_memory((const void*)v->fn, v->smem);
 }
 
 }  // namespace

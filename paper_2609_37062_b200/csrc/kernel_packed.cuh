@@ -6,13 +6,11 @@
 // are 144 bytes at head_dim 128 instead of 512, so at the same DRAM rate 3.6 times as many values have to be unpacked and
 // multiplied, and the kernel is bound by issued instructions as much as by memory.
 //
-// A team of W warps (4 or 8) works on a unit for up to 8 query heads; a block is one team, or two for groups of 9 to 16
-// heads, which then read the same tiles for 8 heads each (two tiles of heads in one warp leave too few registers, and
-// the second reading comes from L2).  Every warp has a ring of its own and works in steps of two tiles (32 tokens): step w of
+// A block is W warps, 4 or 8.  Every warp has a ring of its own and works in steps of two tiles (32 tokens): step w of
 // a unit belongs to warp w mod W.  Its lanes copy a step's tiles (cp.async, 16 bytes a lane, contiguous in the pool) as soon
 // as the warp is done with the step that lay there, across the ends of units.  (Bulk copies cost more here: one takes its
 // operands from uniform registers, and two lanes issuing one each are two passes through some thirty instructions.)  No
-// warp waits for another but at the end of a unit, where the partial states of its team are merged.
+// warp waits for another but at the end of a unit, where the partial states of its warps are merged.
 //
 //   S^T[16 x 8] = sum over blocks b of 32 dims:  k_scale[16, b] * (K codes[16 x 32] . Q^T[32 x 8])
 //   O^T[D x 8] += (V codes * v_scale)^T[D x 16] . P^T[16 x 8]
@@ -38,18 +36,21 @@
 
 namespace da {
 
-// W: warps of a team; TEAMS: 1, or 2 for groups of more than 8 heads.
-template <int D, int W, int TEAMS>
+// W: warps of a block; NT: 8-column tiles of query heads, 2 for groups of more than 8.
+template <int D, int W, int NT>
 struct PackedCfg {
-    static constexpr int kThreads = 32 * W * TEAMS;
+    static constexpr int kThreads = 32 * W;
+    static constexpr int kBlocks = (NT == 1 ? 16 : 12) / W;   // on an SM: 128 registers a thread, or 168
     static constexpr int kTile = packed_tile_bytes(D);
     static constexpr int kStep = 2 * kTile;                   // what a warp takes at a time: two tiles
     static constexpr int kStages = D == 128 ? 2 : 4;          // steps in the ring of a warp
-    static constexpr int kScratchOff = TEAMS * W * kStages * kStep;
+    static constexpr int kScratchOff = W * kStages * kStep;
     static constexpr int kCols = 4;                            // heads that meet in the scratch at a time
-    static constexpr int kScratch = W * kCols * D * 4 + 2 * W * kCols * 4;      // of a team
-    static constexpr int kFlagOff = kScratchOff + TEAMS * kScratch;
-    static constexpr int kSmem = kFlagOff + 16;
+    static constexpr int kScratch = W * kCols * D * 4 + 2 * W * kCols * 4;
+    static constexpr int kQOff = kScratchOff + kScratch;       // NT 2: Q^T as B operands, then what logits are multiplied with
+    static constexpr int kQ = NT == 1 ? 0 : (D / 32) * NT * 32 * 16 + NT * 8 * 4;
+    static constexpr int kSmem = (kQOff + kQ + 15) / 16 * 16;
+    // blocks whose warps merge records in the fused form need its scratch
     static_assert(kScratchOff % 128 == 0 && kScratch % 16 == 0 && kTile % 128 == 0, "shared memory layout");
 };
 
@@ -121,26 +122,28 @@ __device__ __forceinline__ void lds_words(uint32_t addr, uint32_t (&w)[N])
         asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
 }
 
-// DUP: fp16 inputs, groups of up to 4; EXT: windowed plans.  16 warps on an SM.
-template <int D, bool F16, bool DUP, bool EXT, int W, int TEAMS>
-__global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_packed_kernel(const KernelParams p, const int G)
+// DUP: fp16 inputs, groups of up to 4; EXT: windowed plans.
+template <int D, bool F16, bool DUP, bool EXT, int W, int NT>
+__global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_attn_packed_kernel(const KernelParams p, const int G)
 {
-    using Cfg = PackedCfg<D, W, TEAMS>;
+    using Cfg = PackedCfg<D, W, NT>;
     constexpr int NB = D / 32;                                // blocks of 32 dims: K words of a lane and row
     constexpr int NW = D / 64;                                // V words of a lane and token
     constexpr int NS = Cfg::kStages;
     constexpr int MT = D / 16;                                // 16-row tiles of O^T
-    constexpr int kTeam = 32 * W;                             // threads
     constexpr bool LOW = F16 && !DUP;                         // the weights' second part takes an mma of its own
-    static_assert(F16 || !DUP, "duplicated columns: small groups of fp16");
+    static_assert((F16 && NT == 1) || !DUP, "duplicated columns: small groups of fp16");
     extern __shared__ __align__(128) uint8_t smem[];
     const uint32_t base = smem_u32(smem);
-    int* const sm_flag = reinterpret_cast<int*>(smem + Cfg::kFlagOff);                        // of merge blocks
+    float* const sm_wo = reinterpret_cast<float*>(smem + Cfg::kScratchOff);      // [W][kCols][D]
+    float* const sm_wm = sm_wo + W * Cfg::kCols * D;                              // [W][kCols]
+    float* const sm_wl = sm_wm + W * Cfg::kCols;
+    __shared__ int sm_flag;                                   // of merge blocks
 
     if (p.fused && (int)blockIdx.x >= p.n_work_blocks) {
         pdl_launch_dependents();
         pdl_wait_primary();
-        fused_merge_blocks<D>(p, G, Cfg::kThreads, reinterpret_cast<float*>(smem + Cfg::kScratchOff), sm_flag);
+        fused_merge_blocks<D>(p, G, Cfg::kThreads, sm_wo, &sm_flag);
         return;
     }
     const int ubeg = __ldg(p.block_begin + blockIdx.x), uend = __ldg(p.block_begin + blockIdx.x + 1);
@@ -148,16 +151,11 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
         if (blockIdx.x == 0) pdl_wait_primary();
         return;
     }
-    const int team = TEAMS == 1 ? 0 : (int)threadIdx.x / kTeam;
-    const int tid = TEAMS == 1 ? (int)threadIdx.x : (int)threadIdx.x % kTeam;
-    const int lane = tid & 31, warp = tid >> 5;               // of the team
-    const int bar = team == 0 ? 1 : 3;                        // its barrier
-    const int head0 = 8 * team, heads = TEAMS == 1 ? G : min(8, G - head0);                   // its query heads
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int g = lane >> 2, t = lane & 3;                    // mma row / column group, and lane within it
-    const uint32_t ring = base + (team * W + warp) * NS * Cfg::kStep;
-    float* const sm_wo = reinterpret_cast<float*>(smem + Cfg::kScratchOff + team * Cfg::kScratch);   // [W][kCols][D]
-    float* const sm_wm = sm_wo + W * Cfg::kCols * D;                                                  // [W][kCols]
-    float* const sm_wl = sm_wm + W * Cfg::kCols;
+    const uint32_t ring = base + warp * NS * Cfg::kStep;
+    const uint32_t q_at = base + Cfg::kQOff + lane * 16;
+    float* const sm_mult = reinterpret_cast<float*>(smem + Cfg::kQOff + NB * NT * 32 * 16);          // [NT][8]
     decode_attn_unit_t u = load_unit(p.units, ubeg);
     {
         // Hints, while the kernel before this one drains: the tiles of every warp's first steps and the lines that its
@@ -173,9 +171,9 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
                 prefetch_tile(reinterpret_cast<const char*>(p.k) + page * p.k_stride_page + u.kv_head * p.k_stride_head +
                                   (where & ((1 << p.tile_shift) - 1)) * Cfg::kTile, Cfg::kTile);
         }
-        if (warp == 0 && lane >= 16 && (lane - 16) * 128 < heads * D * 2)
-            prefetch_line(reinterpret_cast<const char*>(p.q + ((int64_t)u.seq * p.num_q_heads + u.kv_head * G + head0) * D) + (lane - 16) * 128);
-        if (warp == 0 && lane == 15) prefetch_line(p.seq_lens + u.seq);
+        if (warp == 0 && lane * 128 < G * D * 2)
+            prefetch_line(reinterpret_cast<const char*>(p.q + ((int64_t)u.seq * p.num_q_heads + u.kv_head * G) * D) + lane * 128);
+        if (warp == 1 && lane == 31) prefetch_line(p.seq_lens + u.seq);
     }
     pdl_wait_primary();
 
@@ -257,12 +255,11 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
         v_off[j] = packed_v_codes(D) + (4 * t + (j ^ t)) * (D / 2) + (D == 128 ? (8 * g) ^ (32 * (t >> 1)) : 4 * g);
     uint32_t at = ring;                                       // the step that is worked on
 
-    // a head's query, 8 dims of every block of 32 to a lane
-    const int q_head = DUP ? (g & 3) : g;
+    // a head's query, 8 dims of every block of 32 to a lane (NT 2: this warp's of the two tiles)
+    const int q_head = DUP ? (g & 3) : NT == 1 ? g : (warp & 1) * 8 + g;
     auto load_q = [&](const decode_attn_unit_t& x, uint4 (&w)[NB]) {
-        const bool live = q_head < heads;
-        const uint4* const row = reinterpret_cast<const uint4*>(
-            p.q + ((int64_t)x.seq * p.num_q_heads + x.kv_head * G + head0 + (live ? q_head : 0)) * D);
+        const bool live = q_head < G;
+        const uint4* const row = reinterpret_cast<const uint4*>(p.q + ((int64_t)x.seq * p.num_q_heads + x.kv_head * G + (live ? q_head : 0)) * D);
 #pragma unroll
         for (int b = 0; b < NB; ++b) w[b] = live ? __ldg(row + 4 * b + t) : make_uint4(0, 0, 0, 0);
     };
@@ -279,7 +276,7 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
         if (n_tiles == 0) {
             if (last_unit) pdl_launch_dependents();
             if (stale && tid == 0) record_status(p.status, DA_ERR_STALE_PLAN);
-            if (team == 0) block_finish_empty<D>(p, u, G, tid, kTeam);
+            block_finish_empty<D>(p, u, G, tid, Cfg::kThreads);
             if (!last_unit) {
                 u = load_unit(p.units, uid + 1);
                 load_q(u, q_raw);
@@ -288,8 +285,8 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
             continue;
         }
         // ---- Q^T as B operands, every head's largest magnitude brought to [1, 2); mult: what a logit is multiplied with
-        uint32_t qb[NB][4];
-        float mult[2];
+        uint32_t qb[NB][4];                                   // (NT 2: prepared here, read from shared memory)
+        float mult[NT][2];
         {
             float amax = 0.f;
             float2 f[NB][4];
@@ -316,12 +313,33 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
                     qb[b][i] = *reinterpret_cast<const uint32_t*>(&h);
                 }
             const float own = p.scale_log2 * up;              // of column g; the accumulators hold columns 2 t, 2 t + 1
-            mult[0] = __shfl_sync(0xffffffffu, own, 8 * t);
-            mult[1] = __shfl_sync(0xffffffffu, own, 8 * t + 4);
-        }
-        float oacc[MT][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
+            if (NT == 1) {
+                mult[0][0] = __shfl_sync(0xffffffffu, own, 8 * t);
+                mult[0][1] = __shfl_sync(0xffffffffu, own, 8 * t + 4);
+            } else {
+                // (the barriers at the end of the unit before say that everybody is done with its queries)
+                if (warp < NT) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i) oacc[i][0] = oacc[i][1] = oacc[i][2] = oacc[i][3] = 0.f;
+                    for (int b = 0; b < NB; ++b)
+                        *reinterpret_cast<uint4*>(smem + Cfg::kQOff + ((b * NT + warp) * 32 + lane) * 16) = make_uint4(qb[b][0], qb[b][1], qb[b][2], qb[b][3]);
+                    if (t == 0) sm_mult[warp * 8 + g] = own;
+                }
+                block_sync(1, Cfg::kThreads);
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) {
+                    mult[nt][0] = sm_mult[nt * 8 + 2 * t];
+                    mult[nt][1] = sm_mult[nt * 8 + 2 * t + 1];
+                }
+            }
+        }
+        float oacc[MT][NT][4], m_run[NT][2], l_run[NT][2];
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt) {
+            m_run[nt][0] = m_run[nt][1] = -INFINITY;
+            l_run[nt][0] = l_run[nt][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) oacc[i][nt][0] = oacc[i][nt][1] = oacc[i][nt][2] = oacc[i][nt][3] = 0.f;
+        }
         for (int tile0 = 2 * warp; tile0 < n_tiles; tile0 += 2 * W) {
             copy_wait<NS - 1>();
             __syncwarp();                                     // every lane's copies of the step are there
@@ -344,7 +362,7 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
             auto step = [&](auto masked) {
                 constexpr bool MASKED = decltype(masked)::value;
                 // ---- S^T (the second tile may not be there: what lies in its place is not used)
-                float sacc[2][4];
+                float sacc[2][NT][4];
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     const uint32_t tile = at + i * Cfg::kTile;
@@ -353,7 +371,8 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
                     lds_words<NB>(tile + k_off + k_two, kb);
                     lds_words<NB / 2>(tile + ks_off, sa);
                     lds_words<NB / 2>(tile + ks_off + ks_two, sb);
-                    sacc[i][0] = sacc[i][1] = sacc[i][2] = sacc[i][3] = 0.f;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) sacc[i][nt][0] = sacc[i][nt][1] = sacc[i][nt][2] = sacc[i][nt][3] = 0.f;
 #pragma unroll
                     for (int b = 0; b < NB; ++b) {
                         uint32_t ha[4], hb[4];
@@ -361,13 +380,23 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
                         packed_unpack(kb[b], hb);
                         const __half2 xa = *reinterpret_cast<const __half2*>(&sa[b / 2]), xb = *reinterpret_cast<const __half2*>(&sb[b / 2]);
                         const float fa = b & 1 ? __high2float(xa) : __low2float(xa), fb = b & 1 ? __high2float(xb) : __low2float(xb);
-                        float c[4];
-                        packed_mma0(c, ha[0], hb[0], ha[1], hb[1], qb[b][0], qb[b][1]);
-                        packed_mma(c, ha[2], hb[2], ha[3], hb[3], qb[b][2], qb[b][3]);
-                        sacc[i][0] = fmaf(c[0], fa, sacc[i][0]);
-                        sacc[i][1] = fmaf(c[1], fa, sacc[i][1]);
-                        sacc[i][2] = fmaf(c[2], fb, sacc[i][2]);
-                        sacc[i][3] = fmaf(c[3], fb, sacc[i][3]);
+#pragma unroll
+                        for (int nt = 0; nt < NT; ++nt) {
+                            uint32_t q[4];
+                            if (NT > 1) {
+                                lds_words<4>(q_at + (b * NT + nt) * 512, q);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < 4; ++k) q[k] = qb[b][k];
+                            }
+                            float c[4];
+                            packed_mma0(c, ha[0], hb[0], ha[1], hb[1], q[0], q[1]);
+                            packed_mma(c, ha[2], hb[2], ha[3], hb[3], q[2], q[3]);
+                            sacc[i][nt][0] = fmaf(c[0], fa, sacc[i][nt][0]);
+                            sacc[i][nt][1] = fmaf(c[1], fa, sacc[i][nt][1]);
+                            sacc[i][nt][2] = fmaf(c[2], fb, sacc[i][nt][2]);
+                            sacc[i][nt][3] = fmaf(c[3], fb, sacc[i][nt][3]);
+                        }
                     }
                 }
                 // ---- softmax: rows (tokens) row_a, row_b of each tile, columns (heads) 2 t, 2 t + 1
@@ -375,51 +404,62 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
 #pragma unroll
                     for (int i = 0; i < 2; ++i)
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (!seen(i, k < 2 ? row_a : row_b)) sacc[i][k] = -INFINITY;
-                }
-                float top[2];
+                        for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
-                    top[k] = fmaxf(fmaxf(sacc[0][k], sacc[0][k + 2]), fmaxf(sacc[1][k], sacc[1][k + 2])) * mult[k];
-                if (__any_sync(0xffffffffu, top[0] > m_run[0] + 8.f || top[1] > m_run[1] + 8.f)) {
+                            for (int k = 0; k < 4; ++k)
+                                if (!seen(i, k < 2 ? row_a : row_b)) sacc[i][nt][k] = -INFINITY;
+                }
+                float top[NT][2];
+                bool ahead = false;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
                     for (int k = 0; k < 2; ++k) {
-#pragma unroll
-                        for (int off = 4; off <= 16; off <<= 1) top[k] = fmaxf(top[k], __shfl_xor_sync(0xffffffffu, top[k], off));
-                        const float m = fmaxf(m_run[k], top[k]), al = ex2f(m_run[k] - m);
-                        m_run[k] = m;
-                        l_run[k] *= al;
-#pragma unroll
-                        for (int r = 0; r < MT; ++r) {
-                            oacc[r][k] *= al;
-                            oacc[r][k + 2] *= al;
-                        }
+                        top[nt][k] = fmaxf(fmaxf(sacc[0][nt][k], sacc[0][nt][k + 2]), fmaxf(sacc[1][nt][k], sacc[1][nt][k + 2])) * mult[nt][k];
+                        ahead |= top[nt][k] > m_run[nt][k] + 8.f;
                     }
+                if (__any_sync(0xffffffffu, ahead)) {
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+#pragma unroll
+                            for (int off = 4; off <= 16; off <<= 1) top[nt][k] = fmaxf(top[nt][k], __shfl_xor_sync(0xffffffffu, top[nt][k], off));
+                            const float m = fmaxf(m_run[nt][k], top[nt][k]), al = ex2f(m_run[nt][k] - m);
+                            m_run[nt][k] = m;
+                            l_run[nt][k] *= al;
+#pragma unroll
+                            for (int r = 0; r < MT; ++r) {
+                                oacc[r][nt][k] *= al;
+                                oacc[r][nt][k + 2] *= al;
+                            }
+                        }
                 }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
                     if (MASKED && i == 1 && left <= 16) break;
                     const uint32_t tile = at + i * Cfg::kTile;
-                    uint32_t pb[2], pl[2];
+                    uint32_t pb[NT][2], pl[NT][2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float p0 = ex2f(fmaf(sacc[i][2 * h], mult[0], -m_run[0]));
-                        const float p1 = ex2f(fmaf(sacc[i][2 * h + 1], mult[1], -m_run[1]));
-                        l_run[0] += p0;
-                        l_run[1] += p1;
-                        __half2 x = __floats2half2_rn(p0, p1);
-                        if (F16) {
-                            const float2 y = __half22float2(x);
-                            const __half2 z = __floats2half2_rn(p0 - y.x, p1 - y.y);
-                            if (DUP) {
-                                if (t >= 2) x = z;
-                            } else {
-                                pl[h] = packed_transpose(*reinterpret_cast<const uint32_t*>(&z));
+                    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            const float p0 = ex2f(fmaf(sacc[i][nt][2 * h], mult[nt][0], -m_run[nt][0]));
+                            const float p1 = ex2f(fmaf(sacc[i][nt][2 * h + 1], mult[nt][1], -m_run[nt][1]));
+                            l_run[nt][0] += p0;
+                            l_run[nt][1] += p1;
+                            __half2 x = __floats2half2_rn(p0, p1);
+                            if (F16) {
+                                const float2 y = __half22float2(x);
+                                const __half2 z = __floats2half2_rn(p0 - y.x, p1 - y.y);
+                                if (DUP) {
+                                    if (t >= 2) x = z;
+                                } else {
+                                    pl[nt][h] = packed_transpose(*reinterpret_cast<const uint32_t*>(&z));
+                                }
                             }
+                            pb[nt][h] = packed_transpose(*reinterpret_cast<const uint32_t*>(&x));
                         }
-                        pb[h] = packed_transpose(*reinterpret_cast<const uint32_t*>(&x));
-                    }
                     // ---- O^T: the lane's tokens 4 t + (j ^ t), its dims (D / 8) g ..
                     uint32_t v[4][NW], vs[2];
                     lds_words<2>(tile + vs_off, vs);
@@ -446,8 +486,11 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
                         for (int m = 0; m < 4; ++m) {
                             const uint32_t a0 = half2_mul(l1[m], vs[0]), a1 = half2_mul(h1[m], vs[0]);
                             const uint32_t a2 = half2_mul(l2[m], vs[1]), a3 = half2_mul(h2[m], vs[1]);
-                            packed_mma(oacc[4 * w + m], a0, a1, a2, a3, pb[0], pb[1]);
-                            if (LOW) packed_mma(oacc[4 * w + m], a0, a1, a2, a3, pl[0], pl[1]);
+#pragma unroll
+                            for (int nt = 0; nt < NT; ++nt) {
+                                packed_mma(oacc[4 * w + m][nt], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
+                                if (LOW) packed_mma(oacc[4 * w + m][nt], a0, a1, a2, a3, pl[nt][0], pl[nt][1]);
+                            }
                         }
                     }
                 }
@@ -473,49 +516,46 @@ __global__ void __launch_bounds__(32 * W * TEAMS, 16 / (W * TEAMS)) decode_attn_
         // ------------------------------------------------------------ end of the unit
         if (stale && tid == 0) record_status(p.status, DA_ERR_STALE_PLAN);
 #pragma unroll
-        for (int off = 4; off <= 16; off <<= 1) {
-            l_run[0] += __shfl_xor_sync(0xffffffffu, l_run[0], off);
-            l_run[1] += __shfl_xor_sync(0xffffffffu, l_run[1], off);
-        }
-        if (stale) {
-            m_run[0] = m_run[1] = -INFINITY;
-            l_run[0] = l_run[1] = 0.f;
+        for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+            for (int off = 4; off <= 16; off <<= 1) {
+                l_run[nt][0] += __shfl_xor_sync(0xffffffffu, l_run[nt][0], off);
+                l_run[nt][1] += __shfl_xor_sync(0xffffffffu, l_run[nt][1], off);
+            }
+            if (stale) {
+                m_run[nt][0] = m_run[nt][1] = -INFINITY;
+                l_run[nt][0] = l_run[nt][1] = 0.f;
+            }
         }
         if (DUP) {                                            // columns 4 to 7 carried the second parts of heads 0 to 3
 #pragma unroll
             for (int r = 0; r < MT; ++r)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) oacc[r][k] += __shfl_down_sync(0xffffffffu, oacc[r][k], 2);
+                for (int k = 0; k < 4; ++k) oacc[r][0][k] += __shfl_down_sync(0xffffffffu, oacc[r][0][k], 2);
         }
 #pragma unroll
-        for (int q = 0; q < (DUP ? 1 : 2); ++q) {              // four heads at a time
-            if (4 * q >= heads) break;
-            block_sync(bar, kTeam);                           // the scratch is free
-            if ((t >> 1) == q) {
+        for (int q = 0; q < (DUP ? 1 : 2 * NT); ++q) {         // four heads at a time
+            if (4 * q >= G) break;
+            const int nt = q >> 1;
+            block_sync(1, Cfg::kThreads);                     // the scratch is free
+            if ((t >> 1) == (q & 1)) {
                 const int lc = 2 * (t & 1);
                 if (g == 0) {
-                    sm_wm[warp * Cfg::kCols + lc] = m_run[0];
-                    sm_wm[warp * Cfg::kCols + lc + 1] = m_run[1];
-                    sm_wl[warp * Cfg::kCols + lc] = l_run[0];
-                    sm_wl[warp * Cfg::kCols + lc + 1] = l_run[1];
+                    sm_wm[warp * Cfg::kCols + lc] = m_run[nt][0];
+                    sm_wm[warp * Cfg::kCols + lc + 1] = m_run[nt][1];
+                    sm_wl[warp * Cfg::kCols + lc] = l_run[nt][0];
+                    sm_wl[warp * Cfg::kCols + lc + 1] = l_run[nt][1];
                 }
                 float* const wo = sm_wo + (warp * Cfg::kCols + lc) * D + g * (D / 8);
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    *reinterpret_cast<float2*>(wo + 2 * i) = make_float2(oacc[i][0], oacc[i][2]);
-                    *reinterpret_cast<float2*>(wo + D + 2 * i) = make_float2(oacc[i][1], oacc[i][3]);
+                    *reinterpret_cast<float2*>(wo + 2 * i) = make_float2(oacc[i][nt][0], oacc[i][nt][2]);
+                    *reinterpret_cast<float2*>(wo + D + 2 * i) = make_float2(oacc[i][nt][1], oacc[i][nt][3]);
                 }
             }
-            block_sync(bar, kTeam);
-            block_finish<D, W, Cfg::kCols, false>(p, done, G, sm_wo, sm_wm, sm_wl, tid, kTeam, bar, head0 + 4 * q,
-                                                  min(4, heads - 4 * q), TEAMS == 1 && (DUP || 4 * (q + 1) >= heads));
-        }
-        if (TEAMS > 1 && p.fused && done.slot >= 0) {          // both teams' parts of the record are written: it is published
-            block_sync(4, Cfg::kThreads);
-            if (threadIdx.x == 0) {
-                __threadfence();
-                atomicAdd(p.tickets + (int64_t)done.seq * p.num_kv_heads + done.kv_head, 1);
-            }
+            block_sync(1, Cfg::kThreads);
+            block_finish<D, W, Cfg::kCols, false>(p, done, G, sm_wo, sm_wm, sm_wl, tid, Cfg::kThreads, 1, 4 * q, min(4, G - 4 * q),
+                                                  DUP || 4 * (q + 1) >= G);
         }
     }
 }

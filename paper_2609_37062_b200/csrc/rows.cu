@@ -2,6 +2,7 @@
 #include <cmath>
 #include <cstring>
 
+#include "opt_in.h"
 #include "planner.h"
 #include "rows.cuh"
 
@@ -116,10 +117,8 @@ extern "C" int decode_attn_prepare_rows(const decode_attn_shape_t* shape, const 
     if ((int64_t)a->rows * rp.split > INT32_MAX - 4 * 148 * kRowsBlocks * (kRowsThreads / 32)) return DA_ERR_UNSUPPORTED;
     const int64_t warps = (int64_t)a->rows * rp.split, needed = (warps + kRowsThreads / 32 - 1) / (kRowsThreads / 32);
     const int64_t blocks = needed < 148 * kRowsBlocks ? needed : 148 * kRowsBlocks;
-    if (cudaFuncSetAttribute(fn, cudaFuncAttributeMaxDynamicSharedMemorySize, kRowsSmem) != cudaSuccess) {
-        (void)cudaGetLastError();
-        return DA_ERR_CUDA;
-    }
+    rc = opt_in_shared_memory((const void*)fn, kRowsSmem);
+    if (rc != DA_OK) return rc;
     cudaLaunchConfig_t cfg;
     cfg.gridDim = dim3((unsigned)blocks, 1, 1);
     cfg.blockDim = dim3(kRowsThreads, 1, 1);
