@@ -677,14 +677,20 @@ def decode_attn_step_tables(shape: Shape, seq_lens, gains, seq_lens_out, block_t
     [max_rows]; status [1] or None.  seq_lens_out may be seq_lens, free_count_out free_count."""
     _, _, _, i32, i64 = _dtypes()
     batch, max_rows, at = shape.batch, slots.numel(), _TABLES_ERROR
-    ptrs = []
-    for x, need in ((seq_lens, batch), (gains, batch), (seq_lens_out, batch), (block_table, batch * shape.max_pages_per_seq),
-                    (free_pages, 0), (free_count, 1), (free_count_out, 1), (row_starts, batch + 1), (page_starts, batch + 1)):
+    lists = [(seq_lens, batch), (gains, batch), (seq_lens_out, batch), (block_table, batch * shape.max_pages_per_seq),
+             (row_starts, batch + 1), (page_starts, batch + 1), (positions, max_rows), (free_pages, 0)]
+    if row_seq is not None:
+        lists.append((row_seq, max_rows))
+    for x, need in lists:
         if x.dtype is not i32 or x.numel() < need or not x.is_contiguous():
             raise DecodeAttnError(DA_ERR_INVALID_ARG, at)
-        ptrs.append(x.data_ptr())
-    args = _TABLES_PACK(_TABLES_ARGS_SIZE, 0, max_rows, free_pages.numel(), *ptrs, _vector(slots, i64, 0, at),
-                        _vector(positions, i32, max_rows, at), _vector(row_seq, i32, max_rows, at), _vector(status, i32, 1, at))
+    if free_count.dtype is not i32 or free_count_out.dtype is not i32 or free_count.numel() < 1 or free_count_out.numel() < 1 or \
+            (status is not None and (status.dtype is not i32 or status.numel() < 1)) or slots.dtype is not i64 or not slots.is_contiguous():
+        raise DecodeAttnError(DA_ERR_INVALID_ARG, at)
+    args = _TABLES_PACK(_TABLES_ARGS_SIZE, 0, max_rows, free_pages.numel(), seq_lens.data_ptr(), gains.data_ptr(),
+                        seq_lens_out.data_ptr(), block_table.data_ptr(), free_pages.data_ptr(), free_count.data_ptr(),
+                        free_count_out.data_ptr(), row_starts.data_ptr(), page_starts.data_ptr(), slots.data_ptr(),
+                        positions.data_ptr(), 0 if row_seq is None else row_seq.data_ptr(), 0 if status is None else status.data_ptr())
     rc = _lib.decode_attn_step_tables(shape, args, _stream(stream))
     if check and rc != DA_OK:
         _check(rc, at)
