@@ -738,6 +738,7 @@ static int run_impl(const decode_attn_plan_t* pl, const decode_attn_run_args_t* 
         if (!a->workspace || !aligned(a->workspace, 256)) return DA_ERR_INVALID_ARG;
         if (a->workspace_bytes < pl->workspace_bytes) return DA_ERR_WORKSPACE_TOO_SMALL;
     }
+    if (pl->kernel == DA_KERNEL_PACKED && !on_its_device(pl)) return DA_ERR_INVALID_ARG;
     const bool umma = pl->kernel == DA_KERNEL_UMMA_PREFIX;
     if (pl->grid == 0 && !(umma && pl->layout.n_front_units > 0)) return DA_OK;
     {
