@@ -265,10 +265,10 @@ int decode_attn_plan_destroy(decode_attn_plan_t *plan);
  * list while that work drains, but what it computes with - q, K/V, seq_lens,
  * block_table and run_mask - is read only after it has completed, so ordinary
  * stream order holds for every caller-visible buffer.  One thing happens
- * earlier in the tensor-core kernel: block_table and run_mask are also read
- * before that point to choose a few K/V lines to prefetch into L2, and the
- * lines of q, seq_lens and block_table that the first unit of every block
- * needs are asked into L2 as well.  The early values are used for nothing
+ * earlier in the tensor-core kernels (of 16-bit and 4-bit caches):
+ * block_table and run_mask are also read before that point to choose a few
+ * K/V lines to prefetch into L2, and the lines of q, seq_lens and block_table
+ * that the first unit of every block needs are asked into L2 as well.  The early values are used for nothing
  * else and everything is read again afterwards (L2 is where the writes of
  * the kernel before arrive, so a line brought in early is never stale), so a
  * kernel that is still writing these buffers does no harm; they only have to
@@ -472,7 +472,9 @@ int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan,
  * windows with sinks, RUN masks (by the planner's packing: masked rows are
  * skipped, running ones not dealt out again), capacity plans and fused
  * combine are served; new_k / new_v, shared prefixes, track_weights and the
- * calls that move 16-bit rows (append, gather, evict) are not.  Products with
+ * calls that move 16-bit rows (append, gather, evict) are not.  Calls that
+ * take a shape and neither plan nor policy (decode_attn_merge_shards,
+ * decode_attn_validate_block_table) want one of 16-bit pools.  Products with
  * K are exact up to fp32 sums; weights and values are rounded once to fp16
  * ahead of the product with V.
  * ------------------------------------------------------------------------- */
@@ -579,7 +581,8 @@ int decode_attn_prepare_rows(const decode_attn_shape_t *shape, const decode_attn
  * outside the pool gives its tokens the slot -1 (DA_ERR_BAD_PAGE).  A
  * free_count outside [0, free_capacity] leaves all as it was (DA_ERR_STALE_PLAN,
  * no rows).  What is met is recorded in `status` when one is given.
- * One or two launches on `stream`, nothing is allocated, capture-safe.
+ * Calls that share tables or a list of free pages run one behind the other:
+ * on one stream, or ordered by the caller's events.  One or two launches on `stream`, nothing is allocated, capture-safe.
  * ------------------------------------------------------------------------- */
 typedef struct {
     uint32_t struct_size;       /* sizeof(decode_attn_tables_args_t) */

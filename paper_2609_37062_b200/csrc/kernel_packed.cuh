@@ -4,7 +4,10 @@
 // and a run of 16-token tiles; its result goes to `out` or to a record of the workspace in the same format, and the
 // combine kernel and the merge blocks of fused launches are shared.  What differs is what a byte costs: a token and KV head
 // are 144 bytes at head_dim 128 instead of 512, so at the same DRAM rate 3.6 times as many values have to be unpacked and
-// multiplied, and the kernel is bound by issued instructions as much as by memory.
+// multiplied, and the kernel is bound by issued instructions as much as by memory: 263 of them a tile and warp, issued at
+// 0.62 a cycle and scheduler, of which the conversions from e2m1 and the half-precision products take a pipe two cycles each.
+// 64 sequences of 28,000 to 32,768 tokens, 32 / 8 heads of 128: 2.2 GB in 372 us, 5.96 TB/s (405 to 436 us where the same step
+// runs without a pause and the power limit lowers the clock).
 //
 // A block is W warps, 4 or 8.  Every warp has a ring of its own and works in steps of two tiles (32 tokens): step w of
 // a unit belongs to warp w mod W.  Its lanes copy a step's tiles (cp.async, 16 bytes a lane, contiguous in the pool) as soon
@@ -50,7 +53,6 @@ struct PackedCfg {
     static constexpr int kQOff = kScratchOff + kScratch;       // NT 2: Q^T as B operands, then what logits are multiplied with
     static constexpr int kQ = NT == 1 ? 0 : (D / 32) * NT * 32 * 16 + NT * 8 * 4;
     static constexpr int kSmem = (kQOff + kQ + 15) / 16 * 16;
-    // blocks whose warps merge records in the fused form need its scratch
     static_assert(kScratchOff % 128 == 0 && kScratch % 16 == 0 && kTile % 128 == 0, "shared memory layout");
 };
 
@@ -176,11 +178,12 @@ __global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_a
         if (warp == 1 && lane == 31) prefetch_line(p.seq_lens + u.seq);
     }
     pdl_wait_primary();
+    // (What the kernels before may have written is read by ordinary loads: the wait makes their writes visible to those.)
 
     auto cut_of = [&](const decode_attn_unit_t& x) { return EXT ? window_cut(x.seq_len, p.window, p.sinks) : WindowCut{0, 0, 0}; };
     // tiles of a unit that this launch reads
     auto tiles_of = [&](const decode_attn_unit_t& x) {
-        if (p.run_mask != nullptr && __ldg(p.run_mask + x.seq) == 0) return 0;
+        if (p.run_mask != nullptr && p.run_mask[x.seq] == 0) return 0;
         return (x.tok_end - x.tok_begin + 15) >> 4;
     };
 
@@ -200,7 +203,7 @@ __global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_a
         i_where = 0;
         if (tile < i_tiles) {
             const int at = EXT ? window_tile(i_cut, i_tile0 + tile) : i_tile0 + tile;
-            int page = __ldg(i_row + (at >> p.tile_shift));
+            int page = i_row[at >> p.tile_shift];
             if ((unsigned)page >= (unsigned)p.num_pages) {
                 record_status(p.status, DA_ERR_BAD_PAGE);
                 page = 0;
@@ -261,11 +264,11 @@ __global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_a
         const bool live = q_head < G;
         const uint4* const row = reinterpret_cast<const uint4*>(p.q + ((int64_t)x.seq * p.num_q_heads + x.kv_head * G + (live ? q_head : 0)) * D);
 #pragma unroll
-        for (int b = 0; b < NB; ++b) w[b] = live ? __ldg(row + 4 * b + t) : make_uint4(0, 0, 0, 0);
+        for (int b = 0; b < NB; ++b) w[b] = live ? row[4 * b + t] : make_uint4(0, 0, 0, 0);
     };
     uint4 q_raw[NB];
     load_q(u, q_raw);
-    int dev_len = __ldg(p.seq_lens + u.seq);
+    int dev_len = p.seq_lens[u.seq];
 
     for (int uid = ubeg; uid < uend; ++uid) {
         const bool last_unit = uid + 1 >= uend;
@@ -280,7 +283,7 @@ __global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_a
             if (!last_unit) {
                 u = load_unit(p.units, uid + 1);
                 load_q(u, q_raw);
-                dev_len = __ldg(p.seq_lens + u.seq);
+                dev_len = p.seq_lens[u.seq];
             }
             continue;
         }
@@ -510,7 +513,7 @@ __global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_a
         if (!last_unit) {                                     // in flight during this unit's end
             u = load_unit(p.units, uid + 1);
             load_q(u, q_raw);
-            dev_len = __ldg(p.seq_lens + u.seq);
+            dev_len = p.seq_lens[u.seq];
         }
 
         // ------------------------------------------------------------ end of the unit

@@ -112,6 +112,22 @@ def test_heads_and_rows(hq, hkv, n):
     close(of_slots(k_pool, r.slots), k, r.dtype)
 
 
+@pytest.mark.parametrize("normed", ["q", "k"])
+@pytest.mark.parametrize("rotary", [128, 0])
+@pytest.mark.parametrize("n", [3, 1500])
+def test_one_of_the_norms_alone(normed, rotary, n):
+    r = Rows(n, 10, 2, 128, rotary=rotary, seed=n)
+    if normed == "q":
+        r.k_weight = None
+    else:
+        r.q_weight = None
+    q_out, (k_pool, v_pool) = r.q_out(), r.pools()
+    r.call(q_out=q_out, k_cache=k_pool, v_cache=v_pool)
+    q, k, _ = r.expect()
+    close(q_out, q, r.dtype, "q")
+    close(of_slots(k_pool, r.slots), k, r.dtype, "k")
+
+
 @pytest.mark.parametrize("size", [0.0, 1e-4, 300.0])
 def test_magnitudes(size):
     r = Rows(5, 4, 2, 64, seed=1, size=size)
