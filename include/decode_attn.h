@@ -495,8 +495,7 @@ int64_t decode_attn_packed_head_bytes(int32_t head_dim, int32_t page_size);
  * Rows behind a sequence's end are left as they were.  A length that does not
  * fit either table leaves its sequence out (DA_ERR_STALE_PLAN), a page id
  * outside its pool the tile (DA_ERR_BAD_PAGE).  Destination pages are named
- * once.  One launch on `stream`, nothing is allocated, capture-safe; its grid
- * covers the narrower of the two tables. */
+ * once.  One launch on `stream`, nothing is allocated, capture-safe. */
 int decode_attn_expand_kv(const decode_attn_shape_t *shape, const decode_attn_shape_t *packed_shape, const void *pool,
                           const int32_t *block_table, const int32_t *seq_lens, const int32_t *dst_block_table,
                           void *k_cache, void *v_cache, int32_t *status_or_null, cudaStream_t stream);

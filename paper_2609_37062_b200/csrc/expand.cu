@@ -1,9 +1,14 @@
 // Pages of a cache in 4 bits to 16-bit pages (decode_attn_expand_kv).
 //
-// Bound by memory: 4.5 bits read and 16 written a value.  A warp takes tiles of one KV head (2,304 contiguous bytes at head_dim
-// 128): it copies them to a ring of its own (cp.async, two tiles ahead), and 16 lanes (8 at head_dim 64) write a row of K or V
-// whole, 16 bytes a lane, from one word of codes each.  (96,000 tokens of 8 heads of 128: 502 MB in 90 us, 5.56 TB/s; a plain
-// copy's rate would be 77 us.  With the tiles in registers instead, 128 of them, the same.)
+// Bound by memory: 4.5 bits read and 16 written a value.  A task is a tile of one KV head (2,304 contiguous bytes at head_dim
+// 128).  A warp copies its tasks to a ring of its own (cp.async, one task ahead), and 16 lanes (8 at head_dim 64) write a row of
+// K or V whole, 16 bytes a lane, from one word of codes each.
+//
+// The lengths are on the device, so the grid cannot follow them: it is bounded by what the machine holds, every block makes the
+// sums of the sequences' tiles, and the grid's warps go through the tasks together.  96,000 tokens of 8 heads of 128, 502 MB: 85 us,
+// 5.9 TB/s (a plain copy's rate would be 77).  Blocks over the width of the tables, eight tiles each, took 90 on lengths of 8,000 to
+// 30,000, since their SMs were not equally full, and had thousands of empty blocks where tables are wide; with no more blocks than fit
+// at a time 89 (24 warps an SM: 96), with eight times as many 84.6: warps that start together also read and write together.
 #include <cstring>
 
 #include "common.cuh"
@@ -16,8 +21,10 @@ using namespace da;
 namespace {
 
 constexpr int kExpandThreads = 256;
-constexpr int kExpandTiles = 8;        // tiles of a sequence that a block takes, all KV heads of them
-constexpr int kExpandRing = 3;         // tiles in a warp's ring
+constexpr int kExpandBlocks = 6;       // on an SM
+constexpr int kExpandRing = 2;         // tasks in a warp's ring
+constexpr int kExpandWaves = 4;        // blocks launched for one that fits at a time
+constexpr int kExpandBatch = kExpandThreads;         // sequences that the sums are made for at a time
 
 struct ExpandParams {
     const char* pool;
@@ -27,7 +34,7 @@ struct ExpandParams {
     int64_t src_stride_page, src_stride_head, src_pages, num_pages;
     int64_t k_stride_page, k_stride_token, k_stride_head;
     int64_t v_stride_page, v_stride_token, v_stride_head;
-    int32_t num_kv_heads, src_width, dst_width, page_shift;
+    int32_t batch, num_kv_heads, src_width, dst_width, page_shift;
 };
 
 template <bool F16>
@@ -63,98 +70,123 @@ __device__ __forceinline__ uint4 expand_word(uint32_t w, __half scale)
 }
 
 template <int D, bool F16>
-__global__ void __launch_bounds__(kExpandThreads) decode_attn_expand_kernel(const ExpandParams p)
+__global__ void __launch_bounds__(kExpandThreads, kExpandBlocks) decode_attn_expand_kernel(const ExpandParams p)
 {
     constexpr int L = D / 8;                                  // lanes of a row
     constexpr int STEP = 32 / L;                              // rows at a time
     constexpr int N = 16 / STEP;
     constexpr int TILE = packed_tile_bytes(D);
+    constexpr int W = kExpandThreads / 32;
     extern __shared__ __align__(128) uint8_t smem[];
+    __shared__ int64_t sm_upto[kExpandBatch];                 // tiles of the sequences up to and with this one
+    __shared__ int32_t sm_len[kExpandBatch];
+    __shared__ int64_t sm_warp[W];
     pdl_launch_dependents();
     pdl_wait_primary();
-    const int b = blockIdx.y, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int len = p.seq_lens[b];
-    const int64_t fits = (int64_t)(p.src_width < p.dst_width ? p.src_width : p.dst_width) << p.page_shift;
-    if (len < 0 || len > fits) {
-        if (blockIdx.x == 0 && threadIdx.x == 0 && p.status != nullptr) record_status(p.status, DA_ERR_STALE_PLAN);
-        return;
-    }
-    const int tile0 = blockIdx.x * kExpandTiles, here = min(kExpandTiles, ((len + 15) >> 4) - tile0);
-    if (here <= 0) return;
-    // lane i: the pages of the block's tile i
-    int src_id = 0, dst_id = -1;
-    if (lane < here) {
-        const int at = (tile0 + lane) >> (p.page_shift - 4);
-        src_id = p.block_table[(int64_t)b * p.src_width + at];
-        dst_id = p.dst_table[(int64_t)b * p.dst_width + at];
-        if ((unsigned)src_id >= (unsigned)p.src_pages || (unsigned)dst_id >= (unsigned)p.num_pages) {
-            if (p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
-            src_id = 0;                                       // (nothing outside the pool is read)
-            dst_id = -1;
-        }
-    }
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t fits = (int64_t)min(p.src_width, p.dst_width) << p.page_shift;
+    const int tile_mask = (1 << (p.page_shift - 4)) - 1;
     const uint32_t ring = smem_u32(smem) + warp * (kExpandRing * TILE);
-    // this warp's tasks: head h of tile i, every eighth one
-    int i_tile = 0, i_head = warp;
-    uint32_t i_at = ring;
-    auto settle = [&](int& tile, int& head) {
-        while (head >= p.num_kv_heads) {
-            head -= p.num_kv_heads;
-            ++tile;
-        }
-    };
-    settle(i_tile, i_head);
-    auto ask = [&]() {
-        if (i_tile < here) {
-            const int page = __shfl_sync(0xffffffffu, src_id, i_tile);
-            const int in_page = (tile0 + i_tile) & ((1 << (p.page_shift - 4)) - 1);
-            const char* const src = p.pool + page * p.src_stride_page + i_head * p.src_stride_head + in_page * TILE + lane * 16;
-#pragma unroll
-            for (int c = 0; c <= TILE / 512; ++c)
-                if (c < TILE / 512 || lane * 16 < TILE % 512)
-                    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(i_at + lane * 16 + c * 512), "l"(src + c * 512) : "memory");
-            i_head += kExpandThreads / 32;
-            settle(i_tile, i_head);
-        }
-        asm volatile("cp.async.commit_group;" ::: "memory");  // (a group for every call: the waits below count them)
-        i_at = i_at + TILE == ring + kExpandRing * TILE ? ring : i_at + TILE;
-    };
-    for (int s = 0; s < kExpandRing - 1; ++s) ask();
-
     const int l = lane % L, r0 = lane / L;
     const int64_t k_step = STEP * p.k_stride_token, v_step = STEP * p.v_stride_token;
-    int tile = 0, head = warp;
-    settle(tile, head);
-    uint32_t at = ring;
-    while (tile < here) {
-        asm volatile("cp.async.wait_group %0;" ::"n"(kExpandRing - 2) : "memory");
-        __syncwarp();                                         // every lane's copies are there, and the tile before is read
-        ask();
-        const int page = __shfl_sync(0xffffffffu, dst_id, tile);
-        if (page >= 0) {
-            const int in_page = (tile0 + tile) & ((1 << (p.page_shift - 4)) - 1);
-            const int rows = min(16, len - (tile0 + tile) * 16);
-            const uint8_t* const from = smem + (at - smem_u32(smem));
-            const uint32_t* const kc = reinterpret_cast<const uint32_t*>(from) + packed_k_word(D, r0, l);
-            const uint32_t* const vc = reinterpret_cast<const uint32_t*>(from + packed_v_codes(D));
-            const __half* const ks = reinterpret_cast<const __half*>(from + packed_k_scales(D)) + packed_k_scale(D, r0, l >> 2);
-            const __half* const vs = reinterpret_cast<const __half*>(from + packed_v_scales(D));
-            uint16_t* kt = p.k + page * p.k_stride_page + (in_page * 16 + r0) * p.k_stride_token + head * p.k_stride_head + 8 * l;
-            uint16_t* vt = p.v + page * p.v_stride_page + (in_page * 16 + r0) * p.v_stride_token + head * p.v_stride_head + 8 * l;
+    const int64_t stride = (int64_t)gridDim.x * W;            // warps of the grid
+
+    for (int b0 = 0; b0 < p.batch; b0 += kExpandBatch) {
+        const int here = min(kExpandBatch, p.batch - b0);
+        // ---- sums of the tiles
+        if (b0 > 0) __syncthreads();                          // the sums before are read
+        int len = (int)threadIdx.x < here ? p.seq_lens[b0 + threadIdx.x] : 0;
+        if (len < 0 || len > fits) {
+            if (blockIdx.x == 0 && p.status != nullptr) record_status(p.status, DA_ERR_STALE_PLAN);
+            len = 0;
+        }
+        sm_len[threadIdx.x] = len;
+        int64_t upto = ((int64_t)len + 15) >> 4;
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                if (j * STEP + r0 < rows) {
-                    *reinterpret_cast<uint4*>(kt) = expand_word<F16>(kc[packed_k_word(D, j * STEP, 0)], ks[packed_k_scale(D, j * STEP, 0)]);
-                    *reinterpret_cast<uint4*>(vt) =
-                        expand_word<F16>(vc[packed_v_word(D, j * STEP + r0, l)], vs[packed_v_scale(j * STEP + r0, l >> 2)]);
+        for (int off = 1; off < 32; off <<= 1) {
+            const int64_t x = __shfl_up_sync(0xffffffffu, upto, off);
+            if (lane >= off) upto += x;
+        }
+        if (lane == 31) sm_warp[warp] = upto;
+        __syncthreads();
+        for (int w = 0; w < warp; ++w) upto += sm_warp[w];
+        sm_upto[threadIdx.x] = upto;
+        __syncthreads();
+        const int64_t tasks = sm_upto[here - 1] * p.num_kv_heads;
+
+        for (int64_t first = (int64_t)blockIdx.x * W + warp; first < tasks; first += 32 * stride) {
+            // ---- lane i: where this warp's task i lies
+            const int64_t task = first + lane * stride;
+            const int n = __popc(__ballot_sync(0xffffffffu, task < tasks));
+            int64_t src_at = 0;
+            int dst_id = -1, place = 0;                       // place: tile of the page * 16 + rows - 1
+            int head = 0;
+            if (task < tasks) {
+                const int64_t flat = task / p.num_kv_heads;
+                head = (int)(task - flat * p.num_kv_heads);
+                int lo = 0, hi = here - 1;                    // the first sequence whose sum is larger
+                while (lo < hi) {
+                    const int mid = (lo + hi) >> 1;
+                    if (sm_upto[mid] > flat) hi = mid;
+                    else lo = mid + 1;
                 }
-                kt += k_step;
-                vt += v_step;
+                const int tile = (int)(flat - (lo > 0 ? sm_upto[lo - 1] : 0)), page = tile >> (p.page_shift - 4);
+                int src_id = p.block_table[(int64_t)(b0 + lo) * p.src_width + page];
+                dst_id = p.dst_table[(int64_t)(b0 + lo) * p.dst_width + page];
+                if ((unsigned)src_id >= (unsigned)p.src_pages || (unsigned)dst_id >= (unsigned)p.num_pages) {
+                    if (p.status != nullptr) record_status(p.status, DA_ERR_BAD_PAGE);
+                    src_id = 0;                               // (nothing outside the pool is read)
+                    dst_id = -1;
+                }
+                place = (tile & tile_mask) * 16 + min(16, sm_len[lo] - tile * 16) - 1;
+                src_at = src_id * p.src_stride_page + head * p.src_stride_head + (tile & tile_mask) * TILE;
+            }
+            __syncwarp();                                     // the tasks before are read
+            int asked = 0;
+            uint32_t ask_at = ring, at = ring;
+            auto ask = [&]() {
+                if (asked < n) {
+                    const char* const src = p.pool + __shfl_sync(0xffffffffu, src_at, asked) + lane * 16;
+#pragma unroll
+                    for (int c = 0; c <= TILE / 512; ++c)
+                        if (c < TILE / 512 || lane * 16 < TILE % 512)
+                            asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(ask_at + lane * 16 + c * 512), "l"(src + c * 512) : "memory");
+                    ++asked;
+                }
+                asm volatile("cp.async.commit_group;" ::: "memory");          // (a group for every call: the waits below count them)
+                ask_at = ask_at + TILE == ring + kExpandRing * TILE ? ring : ask_at + TILE;
+            };
+            for (int s = 0; s < kExpandRing - 1; ++s) ask();
+            for (int i = 0; i < n; ++i) {
+                asm volatile("cp.async.wait_group %0;" ::"n"(kExpandRing - 2) : "memory");
+                __syncwarp();                                 // every lane's copies are there, and the task before is read
+                ask();
+                const int page = __shfl_sync(0xffffffffu, dst_id, i), where = __shfl_sync(0xffffffffu, place, i);
+                const int h = __shfl_sync(0xffffffffu, head, i);
+                if (page >= 0) {
+                    const int rows = (where & 15) + 1, row = (where & ~15) + r0;
+                    const uint8_t* const from = smem + (at - smem_u32(smem));
+                    const uint32_t* const kc = reinterpret_cast<const uint32_t*>(from) + packed_k_word(D, r0, l);
+                    const uint32_t* const vc = reinterpret_cast<const uint32_t*>(from + packed_v_codes(D));
+                    const __half* const ks = reinterpret_cast<const __half*>(from + packed_k_scales(D)) + packed_k_scale(D, r0, l >> 2);
+                    const __half* const vs = reinterpret_cast<const __half*>(from + packed_v_scales(D));
+                    uint16_t* kt = p.k + page * p.k_stride_page + row * p.k_stride_token + h * p.k_stride_head + 8 * l;
+                    uint16_t* vt = p.v + page * p.v_stride_page + row * p.v_stride_token + h * p.v_stride_head + 8 * l;
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        if (j * STEP + r0 < rows) {
+                            *reinterpret_cast<uint4*>(kt) =
+                                expand_word<F16>(kc[packed_k_word(D, j * STEP, 0)], ks[packed_k_scale(D, j * STEP, 0)]);
+                            *reinterpret_cast<uint4*>(vt) =
+                                expand_word<F16>(vc[packed_v_word(D, j * STEP + r0, l)], vs[packed_v_scale(j * STEP + r0, l >> 2)]);
+                        }
+                        kt += k_step;
+                        vt += v_step;
+                    }
+                }
+                at = at + TILE == ring + kExpandRing * TILE ? ring : at + TILE;
             }
         }
-        at = at + TILE == ring + kExpandRing * TILE ? ring : at + TILE;
-        head += kExpandThreads / 32;
-        settle(tile, head);
     }
 }
 
@@ -189,7 +221,6 @@ extern "C" int decode_attn_expand_kv(const decode_attn_shape_t* shape, const dec
     if (!aligned(pool, 16) || !aligned(k_cache, 16) || !aligned(v_cache, 16) || !aligned(block_table, 4) || !aligned(seq_lens, 4) ||
         !aligned(dst_block_table, 4) || !aligned(status_or_null, 4))
         return DA_ERR_INVALID_ARG;
-    if (s.batch > 65535) return DA_ERR_UNSUPPORTED;
     ExpandParams p;
     std::memset(&p, 0, sizeof p);
     p.pool = static_cast<const char*>(pool);
@@ -205,13 +236,17 @@ extern "C" int decode_attn_expand_kv(const decode_attn_shape_t* shape, const dec
     p.num_pages = s.num_pages;
     p.k_stride_page = s.k_stride_page; p.k_stride_token = s.k_stride_token; p.k_stride_head = s.k_stride_head;
     p.v_stride_page = s.v_stride_page; p.v_stride_token = s.v_stride_token; p.v_stride_head = s.v_stride_head;
+    p.batch = s.batch;
     p.num_kv_heads = s.num_kv_heads;
     p.src_width = f.max_pages_per_seq;
     p.dst_width = s.max_pages_per_seq;
     while ((1 << p.page_shift) < s.page_size) ++p.page_shift;
-    const int64_t tiles = (int64_t)width * (s.page_size / 16);
-    const int64_t blocks = (tiles + kExpandTiles - 1) / kExpandTiles;
-    if (blocks > 0x7fffffffLL || tiles * 16 > INT32_MAX) return DA_ERR_UNSUPPORTED;
+    // (a few for every one that 148 SMs hold at a time, or as many as the tables have room for)
+    constexpr int64_t kMost = 148 * kExpandBlocks * kExpandWaves;
+    constexpr int64_t kWarps = kExpandThreads / 32;
+    const int64_t tiles = (int64_t)width * (s.page_size / 16) * s.batch;
+    const int64_t most = tiles > INT32_MAX ? INT32_MAX : tiles * s.num_kv_heads, needed = (most + kWarps - 1) / kWarps;
+    const int64_t blocks = needed < kMost ? needed : kMost;
     const bool f16 = s.kv_dtype == DA_DTYPE_FP16;
     auto fn = s.head_dim == 128 ? (f16 ? decode_attn_expand_kernel<128, true> : decode_attn_expand_kernel<128, false>)
                                 : (f16 ? decode_attn_expand_kernel<64, true> : decode_attn_expand_kernel<64, false>);
@@ -219,7 +254,7 @@ extern "C" int decode_attn_expand_kv(const decode_attn_shape_t* shape, const dec
     rc = opt_in_shared_memory((const void*)fn, smem);
     if (rc != DA_OK) return rc;
     cudaLaunchConfig_t cfg;
-    cfg.gridDim = dim3((unsigned)blocks, (unsigned)s.batch, 1);
+    cfg.gridDim = dim3((unsigned)blocks, 1, 1);
     cfg.blockDim = dim3(kExpandThreads, 1, 1);
     cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;

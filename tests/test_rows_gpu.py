@@ -321,6 +321,55 @@ def test_expanded_pages(d, page, dtype):
     assert torch.equal(k.cpu(), want_k) and torch.equal(v.cpu(), want_v)
 
 
+@pytest.mark.parametrize("n,hkv,d,page", [(700, 3, 64, 16), (257, 1, 128, 16), (256, 8, 128, 64)])
+def test_expanding_many_sequences(n, hkv, d, page):
+    """More sequences than one block sums up at a time, some of them empty, read from a few pages that they share."""
+    gen = torch.Generator().manual_seed(n)
+    lens = torch.randint(3 * page + 1, (n,), generator=gen).int()
+    lens[torch.randint(n, (n // 5,), generator=gen)] = 0
+    expand_shared(lens, hkv, d, page, 3, gen)
+
+
+def test_expanding_more_tiles_than_a_round_of_all_warps():
+    gen = torch.Generator().manual_seed(0)
+    expand_shared(torch.tensor([7400 * 256 - 3, 1, 7377 * 256] + [7400 * 256 - 129] * 6).int(), 1, 64, 256, 7400, gen)
+
+
+def expand_shared(lens, hkv, d, page, width, gen):
+    """Sequences whose source pages are drawn from eight; expected: those eight, expanded one sequence each."""
+    n, few = len(lens), 8
+    head = da.decode_attn_packed_head_bytes(d, page)
+    pool = torch.randint(256, (few, hkv, head), generator=gen, dtype=torch.uint8)
+    tiles = pool.view(few, hkv, page // 16, -1)
+    scales = (0.5 + torch.rand(tiles[..., 16 * d:].shape[:-1] + (d // 16 * 16,), generator=gen)).half()
+    tiles[..., 16 * d:] = scales.contiguous().view(torch.uint8)
+    pool = pool.cuda()
+    table = torch.randint(few, (n, width), generator=gen).int().cuda()
+    held = (lens + page - 1) // page
+    live = (torch.arange(width)[None] < held[:, None]).cuda()
+    total = int(held.sum())
+    dst = torch.full((n, width), -1, dtype=torch.int32, device="cuda")
+    dst[live] = torch.randperm(total, generator=gen).int().cuda()
+    row = hkv * d
+    pages = lambda m: [torch.full((m, page, hkv, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    shapes = lambda b, w, m: (da.make_shape(b, hkv, hkv, d, page, w, m, (page * row, row, d)), da.make_kv4_shape(b, hkv, hkv, d, page, w, few))
+    one = torch.arange(few, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    few_kv, kv = pages(few), pages(total)
+    da.decode_attn_expand_kv(*shapes(few, 1, few), pool, one, torch.full((few,), page, dtype=torch.int32, device="cuda"), one, *few_kv)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    da.decode_attn_expand_kv(*shapes(n, width, total), pool, table, lens.cuda(), dst, *kv, status)
+    assert int(status) == da.DA_OK
+    src = torch.empty(total, dtype=torch.long, device="cuda")
+    src[dst[live].long()] = table[live].long()
+    rows = torch.empty(total, dtype=torch.long, device="cuda")                 # of every destination page
+    rows[dst[live].long()] = (lens.cuda()[:, None] - torch.arange(width, device="cuda") * page).clamp(max=page)[live].long()
+    for got, of in zip(kv, few_kv):
+        for at in range(0, total, 4096):
+            want = of[src[at:at + 4096]]
+            want[torch.arange(page, device="cuda")[None] >= rows[at:at + 4096, None]] = 7.0
+            assert torch.equal(got[at:at + 4096], want)
+
+
 def test_expanding_reports_what_does_not_fit():
     from packed_util import Cache
     c = Cache([40, 40, 40], 2, 1, 64, seed=3)
