@@ -36,15 +36,19 @@ __device__ __forceinline__ uint32_t packed_pair(float lo, float hi)
     return r;
 }
 
-// Eight codes of the values x, whose block has the scale s.  The quotients are IEEE divisions: the codes are those of the
-// definition, not of an approximation.
+// Eight codes of the values x (of a 16-bit type), whose block has the scale s: those of the definition, without a division a
+// value.  A quotient lies between two codes at one of the ties b = 1/4, 3/4, .. 5 or, since b * s has 14 significant bits and x has
+// at most 11, at least 2^-14 of b beside it.  The product with the reciprocal is off by at most 2^-23; rounded to 19 bits it is a tie
+// itself where the quotient is, and on the quotient's side of it elsewhere.
 __device__ __forceinline__ uint32_t packed_word(const float (&x)[8], __half s)
 {
     const float f = __half2float(s);
     if (f == 0.f) return 0u;
+    const float r = __frcp_rn(f);
+    auto quotient = [&](float v) { return __uint_as_float((__float_as_uint(v * r) + 16u) & ~31u); };
     uint32_t w = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w |= packed_pair(__fdiv_rn(x[2 * i], f), __fdiv_rn(x[2 * i + 1], f)) << (8 * i);
+    for (int i = 0; i < 4; ++i) w |= packed_pair(quotient(x[2 * i]), quotient(x[2 * i + 1])) << (8 * i);
     return w;
 }
 

@@ -387,6 +387,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocks) decode_attn_rows_ke
                             for (int k = 0; k < 2; ++k)
 #pragma unroll
                                 for (int r = 0; r < 2; ++r) {
+                                    if (ALL && k != (q & 1)) continue;        // (the number of units is even)
                                     const int from = (lane & ~(L - 1)) + (unit >> 1);
                                     const uint32_t lo = __shfl_sync(0xffffffffu, raw[k][r].x, from), hi = __shfl_sync(0xffffffffu, raw[k][r].y, from);
                                     if ((unit & 1) == k && second == (r == 1)) z[q] = make_uint2(lo, hi);

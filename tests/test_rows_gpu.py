@@ -272,6 +272,44 @@ def test_quantised_on_the_way_as_by_a_second_call(rotary, interleaved):
     close(k_out, r.expect()[1], r.dtype)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp16"])
+def test_quotients_at_and_beside_the_ties(dtype):
+    """Scales of many mantissas and exponents; values at the ties between codes and one step of the type to either side."""
+    dt = KINDS[dtype][1]
+    bits = 11 if dtype == "fp16" else 8
+    mantissas = torch.arange(2 ** (bits - 4), 2 ** (bits - 3)).double() / 2 ** (bits - 4)     # 3 * m and 7 * m are values of the type
+    scales = torch.cat([mantissas * 2.0 ** e for e in (-9, -1, 0, 5)])
+    ties = torch.tensor([0.25, 0.75, 1.25, 1.75, 2.5, 3.5, 5.0]).double()
+    at = (scales[:, None] * ties).to(dt)
+    assert torch.equal(at.double(), scales[:, None] * ties) and torch.equal((6 * scales).to(dt).double(), 6 * scales)
+    near = [torch.nextafter(at, torch.full_like(at, to)) for to in (float("inf"), 0.0)]
+    x = torch.zeros((len(scales), 64), dtype=dt)
+    for i, part in enumerate([at, *near]):
+        x[:, 8 * i:8 * i + 7] = part
+        x[:, 32 + 8 * i:32 + 8 * i + 7] = -part
+    x[:, 7], x[:, 39] = (6 * scales).to(dt), (-6 * scales).to(dt)
+    r = Rows(len(scales), 1, 1, 64, dtype, norm=False, rotary=0, seed=2)
+    pool = torch.zeros((r.num_pages, 1, da.decode_attn_packed_head_bytes(64, 16)), dtype=torch.uint8, device="cuda")
+    r.call(4, q=None, k=x[:, None].cuda(), v=x[:, None].cuda(), positions=None, k_cache=pool)
+    code, scale = ref.encode(x.double().numpy())
+    assert np.array_equal(scale.astype(np.float64), np.repeat(scales[:, None].numpy(), 2, 1).reshape(scale.shape))
+    want = ref.values(code, scale)
+    for got in stored(r, pool):
+        assert np.array_equal(got[:, 0], want)
+
+
+@pytest.mark.parametrize("rotary", [64, 32])
+def test_quantised_on_the_way_small_heads(rotary):
+    r = Rows(45, 6, 3, 64, "fp16", rotary=rotary, page=32, seed=rotary)
+    pool = lambda: torch.zeros((r.num_pages, 3, da.decode_attn_packed_head_bytes(64, 32)), dtype=torch.uint8, device="cuda")
+    fused, apart, q_out = pool(), pool(), r.q_out()
+    k_out = torch.zeros((45, 3, 64), dtype=r.dtype, device="cuda")
+    r.call(4, q_out=q_out, k_out=k_out, k_cache=fused)
+    r.call(4, q=None, q_weight=None, k=k_out, k_weight=None, positions=None, cos_sin=None, k_cache=apart)
+    assert torch.equal(fused, apart)
+    close(k_out, r.expect()[1], r.dtype)
+
+
 def test_values_at_the_borders():
     """Ties between codes, zeros, tiny and huge blocks, infinities."""
     r = Rows(6, 1, 1, 64, "fp16", norm=False, rotary=0, seed=1)
