@@ -476,7 +476,8 @@ int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan,
  * take a shape and neither plan nor policy (decode_attn_merge_shards,
  * decode_attn_validate_block_table) want one of 16-bit pools.  Products with
  * K are exact up to fp32 sums; weights and values are rounded once to fp16
- * ahead of the product with V.
+ * ahead of the product with V, so V beyond 65,504 in magnitude (which bf16 rows
+ * can hold) makes what attends it infinite or NaN.
  * ------------------------------------------------------------------------- */
 
 /* Bytes of one KV head of one page of a cache in 4 bits; 0 for a head_dim or
