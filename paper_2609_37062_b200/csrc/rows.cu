@@ -35,6 +35,32 @@ rows_kernel_t kernel_for(bool f16, bool packed, bool halves, bool all)
     return f16 ? for_turn<D, true, false>(halves, all) : for_turn<D, false, false>(halves, all);
 }
 
+// Shares of a row's tasks: as many as 148 SMs have resident warps for, so that every warp has one; a share costs its tasks and
+// about one and a half to begin.  Where rows are more than half of the warps, another number may fill the last round of warps
+// better.  (32 + 8 + 8 heads of 128, us: 256 rows 5.3 with shares for a little more than the resident warps, 4.0 so; 600 rows 7.2
+// and 5.2; 1,777 rows 12.8 and 11.2; 1,200 rows 10.1 whole and 9.1 in three shares, 3,000 rows 19.5 whole and 18.0 in two.)
+constexpr int kRowsWarps = 148 * kRowsBlocks * (kRowsThreads / 32);
+
+int split_of(int rows, int tasks)
+{
+    auto cost = [&](int split) {
+        const int64_t rounds = ((int64_t)rows * split + kRowsWarps - 1) / kRowsWarps;
+        return rounds * (2 * ((tasks + split - 1) / split) + 3);
+    };
+    int best = rows < kRowsWarps ? kRowsWarps / rows : 1;
+    if (best > tasks) best = tasks;
+    if (best > 2) return best;
+    int64_t least = cost(best);
+    for (int split = 1; split <= tasks && split <= 4; ++split) {
+        const int64_t c = cost(split);
+        if (c * 100 < least * 95) {
+            best = split;
+            least = c;
+        }
+    }
+    return best;
+}
+
 }  // namespace
 
 extern "C" int decode_attn_prepare_rows(const decode_attn_shape_t* shape, const decode_attn_rows_args_t* a, cudaStream_t stream)
@@ -109,12 +135,10 @@ extern "C" int decode_attn_prepare_rows(const decode_attn_shape_t* shape, const 
 
     const bool f16 = s.kv_dtype == DA_DTYPE_FP16, halves = a->cos_sin != nullptr && !a->interleaved, all = a->rotary_dim == D;
     rows_kernel_t fn = D == 128 ? kernel_for<128>(f16, packed, halves, all) : kernel_for<64>(f16, packed, halves, all);
-    // A warp a row where rows fill the machine (the resident warps of 148 SMs); fewer rows are shared by warps.
     const int per_task = 512 / D, tasks = (rp.n_q + per_task - 1) / per_task + (rp.n_k + per_task - 1) / per_task + (rp.n_v + per_task - 1) / per_task;
-    const int64_t wanted = (148 * kRowsBlocks * (kRowsThreads / 32) + a->rows - 1) / a->rows;
-    rp.split = (int32_t)(wanted < tasks ? wanted : tasks);
+    rp.split = split_of(a->rows, tasks);
     // (numbers of work items stay below 2^31, two rounds of all warps included)
-    if ((int64_t)a->rows * rp.split > INT32_MAX - 4 * 148 * kRowsBlocks * (kRowsThreads / 32)) return DA_ERR_UNSUPPORTED;
+    if ((int64_t)a->rows * rp.split > INT32_MAX - 4 * kRowsWarps) return DA_ERR_UNSUPPORTED;
     const int64_t warps = (int64_t)a->rows * rp.split, needed = (warps + kRowsThreads / 32 - 1) / (kRowsThreads / 32);
     const int64_t blocks = needed < 148 * kRowsBlocks ? needed : 148 * kRowsBlocks;
     rc = opt_in_shared_memory((const void*)fn, kRowsSmem);
