@@ -542,7 +542,9 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
         if (rc != DA_OK) return rc;
     }
     const bool prefix = policy->shared_prefix_tokens > 0;
-    pl->big_blocks = packed_big_blocks((int64_t)std::max(shape->batch, policy->capacity_batch) * shape->num_kv_heads, pl->sm_count);
+    // (the order of the sums follows the number of warps, so DETERMINISTIC has one for every batch)
+    pl->big_blocks = policy->split_mode != DA_SPLIT_DETERMINISTIC &&
+                     packed_big_blocks((int64_t)std::max(shape->batch, policy->capacity_batch) * shape->num_kv_heads, pl->sm_count);
     if (prefix && pl->kernel == DA_KERNEL_SIMT) return DA_ERR_UNSUPPORTED;
     // what follows a tcgen05 prefix runs on the ordinary tensor-core kernel
     int occ = query_occupancy(umma ? DA_KERNEL_MMA_TMA : pl->kernel, shape->head_dim,

@@ -177,6 +177,19 @@ def test_page_order_and_batch_do_not_change_deterministic_bits():
     assert torch.equal(out, fused) and torch.equal(lse, fused_lse)
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_deterministic_bits_beside_many_others(d):
+    """A sequence alone and in a batch of more (sequence, KV head) pairs than the device has multiprocessors."""
+    pol = da.make_policy(split_mode=da.DA_SPLIT_DETERMINISTIC, cache_bits=4)
+    lens = [1300, 700] + [5] * 40
+    c, one = Cache(lens, 8, 8, d, seed=4), Cache(lens, 8, 8, d, seed=4)
+    out, lse, _ = run(c, pol)
+    for b in (0, 1, 20):
+        one.lens, one.table, one.q = lens[b:b + 1], c.table[b:b + 1], c.q[b:b + 1]
+        alone, alone_lse, _ = run(one, pol)
+        assert torch.equal(out[b:b + 1], alone) and torch.equal(lse[b:b + 1], alone_lse)
+
+
 def test_capacity_plan_in_a_graph():
     a, b = Cache([40, 900, 3], 8, 2, 128, seed=31, width=70), Cache([1000, 16], 8, 2, 128, seed=32, width=70)
     for c in (a, b):
