@@ -559,6 +559,22 @@ int decode_attn_plan(const decode_attn_shape_t* shape, const decode_attn_policy_
     if (pl->kernel != DA_KERNEL_SIMT) pl->max_bins = pl->sm_count * pl->ctas_per_sm;
     rc = make_layout(*shape, pl->policy, pl->seq_lens.data(), pl->sm_count, pl->ctas_per_sm, pl->layout, pl->max_bins);
     if (rc != DA_OK) return rc;
+    if (pl->kernel == DA_KERNEL_PACKED && packed_either_size(*shape, *policy, pl->sm_count)) {
+        int threads = 0, smem = 0;
+        occ = query_occupancy(pl->kernel, shape->head_dim, pl->group, &threads, &smem, true, policy->window_tokens > 0);
+        if (occ <= 0) return DA_ERR_CUDA;
+        Layout other;
+        rc = make_layout(*shape, pl->policy, pl->seq_lens.data(), pl->sm_count, occ, other, pl->sm_count * occ);
+        if (rc != DA_OK) return rc;
+        if (other.packed_time < pl->layout.packed_time) {
+            pl->big_blocks = true;
+            pl->block_threads = threads;
+            pl->dyn_smem = smem;
+            pl->ctas_per_sm = occ;
+            pl->max_bins = pl->sm_count * occ;
+            pl->layout = std::move(other);
+        }
+    }
 
     if (policy->capacity_batch > 0) {
         pl->max_batch = policy->capacity_batch;

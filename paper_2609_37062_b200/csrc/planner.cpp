@@ -205,12 +205,44 @@ int64_t units_for_chunk(const std::vector<int64_t>& pages, int64_t c, int max_sp
 // 592 blocks: 438 us dealt by whole units, 372 evenly; the host plans them in 64 us.)
 struct PackedCost {
     int32_t unit, round, combine;
+    int32_t change;                   // a unit's end and beginning on an SM full of warps, what packed_time counts
 };
 
 PackedCost packed_cost(const decode_attn_shape_t& s, int ctas_per_sm)
 {
     const bool big = s.num_q_heads / s.num_kv_heads <= 8 && ctas_per_sm < 4;     // blocks of one team of eight warps
-    return big ? PackedCost{16, 16, 30} : PackedCost{8, 8, 15};
+    return big ? PackedCost{16, 16, 30, 32} : PackedCost{8, 8, 15, 20};
+}
+
+// How long a layout runs, in the time in which an SM full of warps works off a tile (58 ns at head_dim 128).  Blocks come to the
+// SMs in turn, and those that share one slow each other down: with 4, 8, 12 and 16 warps at work an SM does 0.39, 0.68, 0.88 and 1
+// of its most.  (Rates and costs from uniform batches; estimates for 24 batches are 0 to 50 % too long, most where units are
+// cut, and 9 of the 10 between which there is a choice fall to the faster size.)
+double packed_time(const Layout& out, int sm_count, int ctas_per_sm, const PackedCost& pc)
+{
+    static const double kRate[5] = {0, 0.39, 0.68, 0.88, 1};
+    constexpr double kCombineLaunch = 53;
+    const int blocks = (int)out.block_begin.size() - 1, step = ctas_per_sm >= 4 ? 1 : 2;      // (8 warps a block)
+    std::vector<double> load(ctas_per_sm);
+    double worst = 0;
+    for (int sm = 0; sm < sm_count && sm < blocks; ++sm) {
+        int n = 0;
+        for (int b = sm; b < blocks && n < ctas_per_sm; b += sm_count) {
+            int64_t tiles = 0;
+            for (int32_t i = out.block_begin[b]; i < out.block_begin[b + 1]; ++i)
+                tiles += ceil_div(ceil_div(out.units[i].tok_end - out.units[i].tok_begin, kTileTokens), pc.round) * pc.round + pc.change;
+            load[n++] = (double)tiles;
+        }
+        std::sort(load.begin(), load.begin() + n);
+        double t = 0, done = 0;
+        for (int i = 0; i < n; ++i) {                         // n - i blocks work until the next one ends
+            const int active = n - i;
+            t += (load[i] - done) * active / kRate[std::min(4, active * step)];
+            done = load[i];
+        }
+        worst = std::max(worst, t);
+    }
+    return worst + (out.n_slots > 0 ? kCombineLaunch : 0);
 }
 
 // The fullest block's load when chunks of c tiles go to the lightest block, longest first: dealt out where there are at most
@@ -340,7 +372,7 @@ int make_layout_of(const decode_attn_shape_t& s, const decode_attn_policy_t& p, 
     const int B = s.batch, P = kTileTokens, H = s.num_kv_heads;
     const int max_splits = max_splits_of(p);
     const bool packed = p.cache_bits == 4 && p.split_mode == DA_SPLIT_AUTO;
-    const PackedCost pc = packed ? packed_cost(s, ctas_per_sm) : PackedCost{0, 0, 0};
+    const PackedCost pc = packed ? packed_cost(s, ctas_per_sm) : PackedCost{0, 0, 0, 0};
     if (packed && max_bins <= 0) max_bins = sm_count * ctas_per_sm;              // (its work list follows from its blocks)
     // With a shared prefix the ordinary units cover only what follows it; the prefix itself is
     // cut into chunks attended once for a block of sequences at a time (see below).
@@ -679,6 +711,7 @@ int make_layout_of(const decode_attn_shape_t& s, const decode_attn_policy_t& p, 
         }
         if (even >= 0 && (even + pc.combine) * 100 < worst * 97)
             deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, true);
+        out.packed_time = packed_time(out, sm_count, ctas_per_sm, pc);
     }
     return DA_OK;
 }

@@ -29,6 +29,7 @@ struct Layout {
     int64_t n_slots = 0;
     int32_t chunk_tokens = 0;
     int32_t max_splits_used = 0;
+    double packed_time = 0;                 // estimate, of AUTO plans for a cache in 4 bits; comparable between two sizes of blocks
     int32_t prefix_chunks = 0;              // chunks the shared prefix is cut into (0: no shared prefix)
     int32_t n_front_units = 0;              // shared-prefix units kept at the front, outside the bins, for a
                                             // kernel of their own (policy kernel DA_KERNEL_UMMA_PREFIX)

@@ -190,6 +190,20 @@ def test_deterministic_bits_beside_many_others(d):
         assert torch.equal(out[b:b + 1], alone) and torch.equal(lse[b:b + 1], alone_lse)
 
 
+@pytest.mark.parametrize("lens", [[900] * 20, [100] * 20, [1000, 17, 640] + [33] * 30])
+@pytest.mark.parametrize("hq,dtype", [(8, "bf16"), (32, "fp16")])
+def test_batches_of_either_size_of_blocks(lens, hq, dtype):
+    """As many (sequence, KV head) pairs as the device has multiprocessors, or more, and fewer than it has small blocks."""
+    c = Cache(lens, hq, 8, 128, dtype=dtype, seed=len(lens))
+    out, lse, status = run(c)
+    assert status == da.DA_OK
+    check(c, out, lse, "either")
+    pol = da.make_policy(cache_bits=4)
+    sizes = {da.decode_attn_plan(da.make_kv4_shape(len(x), hq, 8, 128, 16, 70, 2000), pol, x).info().ctas_per_sm
+             for x in ([900] * 20, [100] * 20)}
+    assert len(sizes) == 2                             # (both kinds occur among these)
+
+
 def test_capacity_plan_in_a_graph():
     a, b = Cache([40, 900, 3], 8, 2, 128, seed=31, width=70), Cache([1000, 16], 8, 2, 128, seed=32, width=70)
     for c in (a, b):
