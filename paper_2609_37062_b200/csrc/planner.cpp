@@ -222,7 +222,7 @@ double packed_time(const Layout& out, int sm_count, int ctas_per_sm, const Packe
 {
     static const double kRate[5] = {0, 0.39, 0.68, 0.88, 1};
     constexpr double kCombineLaunch = 53;
-    const int blocks = (int)out.block_begin.size() - 1, step = ctas_per_sm >= 4 ? 1 : 2;      // (8 warps a block)
+    const int blocks = (int)out.block_begin.size() - 1, step = pc.round / 8;      // (a block's warps, in fours)
     std::vector<double> load(ctas_per_sm);
     double worst = 0;
     for (int sm = 0; sm < sm_count && sm < blocks; ++sm) {
@@ -709,9 +709,33 @@ int make_layout_of(const decode_attn_shape_t& s, const decode_attn_policy_t& p, 
             if (even <= share + share / 64) break;
             share += ceil_div(even - share, max_bins) + 1;
         }
-        if (even >= 0 && (even + pc.combine) * 100 < worst * 97)
-            deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, true);
         out.packed_time = packed_time(out, sm_count, ctas_per_sm, pc);
+        if (even >= 0 && (even + pc.combine) * 100 < worst * 97) {
+            // Equal shares mean more units, whose change-over the loads above count too low where SMs are full: by the estimate
+            // that has it (a little on the dear side there) they must not lose.  (us, whole and even: 150 rows of 1,000 to 3,000 tokens,
+            // 8 heads, 70.5 and 78.7; 200 of 1,000 to 4,000 113 and 118; 64 of 4,000 61.3 and 58.8, estimated as equal.)
+            Layout whole;
+            whole.units = std::move(out.units);
+            whole.block_begin = std::move(out.block_begin);
+            whole.splits = out.splits;
+            whole.slot_base = out.slot_base;
+            whole.rank_pos = std::move(out.rank_pos);
+            whole.n_slots = out.n_slots;
+            whole.max_splits_used = out.max_splits_used;
+            deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, true);
+            const double time = packed_time(out, sm_count, ctas_per_sm, pc);
+            if (time > out.packed_time * 1.1) {
+                out.units = std::move(whole.units);
+                out.block_begin = std::move(whole.block_begin);
+                out.splits = std::move(whole.splits);
+                out.slot_base = std::move(whole.slot_base);
+                out.rank_pos = std::move(whole.rank_pos);
+                out.n_slots = whole.n_slots;
+                out.max_splits_used = whole.max_splits_used;
+            } else {
+                out.packed_time = time;
+            }
+        }
     }
     return DA_OK;
 }
