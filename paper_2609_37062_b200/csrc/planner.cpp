@@ -218,19 +218,20 @@ PackedCost packed_cost(const decode_attn_shape_t& s, int ctas_per_sm)
 // SMs in turn, and those that share one slow each other down: with 4, 8, 12 and 16 warps at work an SM does 0.39, 0.68, 0.88 and 1
 // of its most.  (Rates and costs from uniform batches; estimates for 24 batches are 0 to 50 % too long, most where units are
 // cut, and 9 of the 10 between which there is a choice fall to the faster size.)
-double packed_time(const Layout& out, int sm_count, int ctas_per_sm, const PackedCost& pc)
+double packed_time(const std::vector<decode_attn_unit_t>& units, const std::vector<int32_t>& block_begin, bool combine, int sm_count,
+                   int ctas_per_sm, const PackedCost& pc)
 {
     static const double kRate[5] = {0, 0.39, 0.68, 0.88, 1};
     constexpr double kCombineLaunch = 53;
-    const int blocks = (int)out.block_begin.size() - 1, step = pc.round / 8;      // (a block's warps, in fours)
+    const int blocks = (int)block_begin.size() - 1, step = pc.round / 8;      // (a block's warps, in fours)
     std::vector<double> load(ctas_per_sm);
     double worst = 0;
     for (int sm = 0; sm < sm_count && sm < blocks; ++sm) {
         int n = 0;
         for (int b = sm; b < blocks && n < ctas_per_sm; b += sm_count) {
             int64_t tiles = 0;
-            for (int32_t i = out.block_begin[b]; i < out.block_begin[b + 1]; ++i)
-                tiles += ceil_div(ceil_div(out.units[i].tok_end - out.units[i].tok_begin, kTileTokens), pc.round) * pc.round + pc.change;
+            for (int32_t i = block_begin[b]; i < block_begin[b + 1]; ++i)
+                tiles += ceil_div(ceil_div(units[i].tok_end - units[i].tok_begin, kTileTokens), pc.round) * pc.round + pc.change;
             load[n++] = (double)tiles;
         }
         std::sort(load.begin(), load.begin() + n);
@@ -242,7 +243,7 @@ double packed_time(const Layout& out, int sm_count, int ctas_per_sm, const Packe
         }
         worst = std::max(worst, t);
     }
-    return worst + (out.n_slots > 0 ? kCombineLaunch : 0);
+    return worst + (combine ? kCombineLaunch : 0);
 }
 
 // The fullest block's load when chunks of c tiles go to the lightest block, longest first: dealt out where there are at most
@@ -277,26 +278,34 @@ int64_t dealt_whole(const std::vector<int64_t>& pages, int H, int64_t c, int max
     return worst;
 }
 
+// The fields of a Layout that dealing the units evenly replaces.
+struct Dealt {
+    std::vector<decode_attn_unit_t> units;
+    std::vector<int32_t> block_begin, splits, slot_base;
+    int64_t n_slots = 0;
+    int32_t max_splits_used = 0;
+};
+
 // One unit after the other to the blocks, every block an equal share of the tiles: what is over the share is cut off and
 // goes to the next block.  Heads of a sequence are cut at places of their own; those with fewer pieces than others get
-// empty ones.  Returns the load of the fullest block, or -1 where a sequence would have more pieces than it may.
-int64_t deal_evenly(const decode_attn_shape_t& s, const int32_t* seq_lens, const std::vector<int64_t>& pages, int slots,
-                    int64_t share, int64_t least, int max_splits, const PackedCost& c, Layout& out, bool commit)
+// empty ones.  Returns the load of the fullest block, or -1 where a sequence would have more pieces than it may (another share
+// may cut it into more or fewer); `out` (or nullptr: the load alone) is complete only where that is not so.
+int64_t deal_evenly(const decode_attn_shape_t& s, const int32_t* seq_lens, const std::vector<int32_t>& visible,
+                    const std::vector<int64_t>& pages, int slots, int64_t share, int64_t least, int max_splits, const PackedCost& c,
+                    Dealt* out)
 {
     const int B = s.batch, H = s.num_kv_heads;
     int64_t load = 0, worst = 0;
     int block = 0;
-    std::vector<int32_t> begin(1, 0);              // first unit of every block
-    std::vector<decode_attn_unit_t> units;
     std::vector<int32_t> pieces((size_t)H);
-    if (commit) {
-        out.splits.assign(B, 1);
-        out.slot_base.assign(B, -1);
-        out.n_slots = 0;
-        out.max_splits_used = B > 0 ? 1 : 0;
+    if (out) {
+        out->block_begin.assign(1, 0);              // first unit of every block
+        out->splits.assign(B, 1);
+        out->slot_base.assign(B, -1);
+        out->max_splits_used = B > 0 ? 1 : 0;
     }
     for (int b = 0; b < B; ++b) {
-        const size_t first_unit = units.size();
+        const size_t first_unit = out ? out->units.size() : 0;
         const int64_t n = pages[b];
         for (int g = 0; g < H; ++g) {
             int64_t at = 0;
@@ -305,23 +314,23 @@ int64_t deal_evenly(const decode_attn_shape_t& s, const int32_t* seq_lens, const
                 if (block + 1 < slots && load > 0 && n > 0 && share - load - c.unit < std::min(least, n - at)) {
                     ++block;
                     load = 0;
-                    if (commit) begin.push_back((int32_t)units.size());
+                    if (out) out->block_begin.push_back((int32_t)out->units.size());
                 }
                 int64_t take = n - at;
                 if (block + 1 < slots && take > share - load - c.unit)
                     take = std::max<int64_t>(least, (share - load - c.unit) / c.round * c.round);
                 if (n - at - take < least) take = n - at;        // no scrap is left behind
-                if (commit) {
+                if (out) {
                     decode_attn_unit_t u;
                     u.seq = b;
                     u.kv_head = g;
                     u.tok_begin = (int32_t)(at * kTileTokens);
-                    u.tok_end = (int32_t)std::min<int64_t>((at + take) * kTileTokens, out.visible[b]);
+                    u.tok_end = (int32_t)std::min<int64_t>((at + take) * kTileTokens, visible[b]);
                     u.slot = -1;
                     u.seq_len = seq_lens[b];
                     u.split_index = k;
                     u.n_splits = 1;
-                    units.push_back(u);
+                    out->units.push_back(u);
                 }
                 ++k;
                 at += take;
@@ -332,33 +341,27 @@ int64_t deal_evenly(const decode_attn_shape_t& s, const int32_t* seq_lens, const
         }
         const int32_t S = *std::max_element(pieces.begin(), pieces.end());
         if (S > max_splits) return -1;
-        if (!commit) continue;
-        out.splits[b] = S;
-        out.max_splits_used = std::max(out.max_splits_used, S);
+        if (!out) continue;
+        out->splits[b] = S;
+        out->max_splits_used = std::max(out->max_splits_used, S);
         if (S == 1) continue;
-        out.slot_base[b] = (int32_t)out.n_slots;
-        out.n_slots += S;
-        for (size_t i = first_unit; i < units.size(); ++i) {
-            units[i].n_splits = S;
-            units[i].slot = out.slot_base[b] + units[i].split_index;
+        out->slot_base[b] = (int32_t)out->n_slots;
+        out->n_slots += S;
+        for (size_t i = first_unit; i < out->units.size(); ++i) {
+            out->units[i].n_splits = S;
+            out->units[i].slot = out->slot_base[b] + out->units[i].split_index;
         }
         for (int g = 0; g < H; ++g)
             for (int32_t k = pieces[g]; k < S; ++k) {
-                decode_attn_unit_t u = units[first_unit];
+                decode_attn_unit_t u = out->units[first_unit];
                 u.kv_head = g;
-                u.tok_begin = u.tok_end = out.visible[b];
-                u.slot = out.slot_base[b] + k;
+                u.tok_begin = u.tok_end = visible[b];
+                u.slot = out->slot_base[b] + k;
                 u.split_index = k;
-                units.push_back(u);
+                out->units.push_back(u);
             }
     }
-    if (commit) {
-        begin.push_back((int32_t)units.size());
-        out.units.swap(units);
-        out.block_begin.swap(begin);
-        out.rank_pos.clear();
-        out.n_front_units = 0;
-    }
+    if (out) out->block_begin.push_back((int32_t)out->units.size());
     return worst;
 }
 
@@ -705,34 +708,27 @@ int make_layout_of(const decode_attn_shape_t& s, const decode_attn_policy_t& p, 
             if (n > 0) cost_all += (ceil_div(n, pc.round) * pc.round + pc.unit) * H;
         int64_t share = ceil_div(cost_all, max_bins) + pc.unit;
         for (int i = 0; i < 3 && (share + pc.combine) * 100 < worst * 97; ++i) {
-            even = deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, false);
+            even = deal_evenly(s, seq_lens, visible, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, nullptr);
             if (even <= share + share / 64) break;
             share += ceil_div(even - share, max_bins) + 1;
         }
-        out.packed_time = packed_time(out, sm_count, ctas_per_sm, pc);
+        out.packed_time = packed_time(out.units, out.block_begin, out.n_slots > 0, sm_count, ctas_per_sm, pc);
         if (even >= 0 && (even + pc.combine) * 100 < worst * 97) {
+            // (the share may be one that was not tried: what it gives is looked at again)
+            Dealt dealt;
+            even = deal_evenly(s, seq_lens, visible, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, &dealt);
             // Equal shares mean more units, whose change-over the loads above count too low where SMs are full: by the estimate
             // that has it (a little on the dear side there) they must not lose.  (us, whole and even: 150 rows of 1,000 to 3,000 tokens,
             // 8 heads, 70.5 and 78.7; 200 of 1,000 to 4,000 113 and 118; 64 of 4,000 61.3 and 58.8, estimated as equal.)
-            Layout whole;
-            whole.units = std::move(out.units);
-            whole.block_begin = std::move(out.block_begin);
-            whole.splits = out.splits;
-            whole.slot_base = out.slot_base;
-            whole.rank_pos = std::move(out.rank_pos);
-            whole.n_slots = out.n_slots;
-            whole.max_splits_used = out.max_splits_used;
-            deal_evenly(s, seq_lens, pages, max_bins, share, min_chunk_pages(s, p), max_splits, pc, out, true);
-            const double time = packed_time(out, sm_count, ctas_per_sm, pc);
-            if (time > out.packed_time * 1.1) {
-                out.units = std::move(whole.units);
-                out.block_begin = std::move(whole.block_begin);
-                out.splits = std::move(whole.splits);
-                out.slot_base = std::move(whole.slot_base);
-                out.rank_pos = std::move(whole.rank_pos);
-                out.n_slots = whole.n_slots;
-                out.max_splits_used = whole.max_splits_used;
-            } else {
+            const double time = even < 0 ? 0 : packed_time(dealt.units, dealt.block_begin, dealt.n_slots > 0, sm_count, ctas_per_sm, pc);
+            if (even >= 0 && time <= out.packed_time * 1.1) {
+                out.units.swap(dealt.units);
+                out.block_begin.swap(dealt.block_begin);
+                out.splits.swap(dealt.splits);
+                out.slot_base.swap(dealt.slot_base);
+                out.n_slots = dealt.n_slots;
+                out.max_splits_used = dealt.max_splits_used;
+                out.rank_pos.clear();
                 out.packed_time = time;
             }
         }
