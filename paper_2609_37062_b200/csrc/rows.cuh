@@ -247,6 +247,10 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocks) decode_attn_rows_ke
     ask();
     uint32_t t_slot = 0;
     bool odd = false;
+    // The angles of a work item are asked for with the first task of the item before it, so the waits for tasks cover them where that
+    // one had kRowsRing - 1 tasks or more (a row's shares differ by one, and a warp's next item may be another part); the first item's
+    // were asked for with its own tasks.
+    bool angles_late = true;
 
     for (unsigned id = first_id; id < items; id += stride) {
         const int row = row_of(id), begin = cut_at(id - row * split), end = cut_at(id - row * split + 1);
@@ -291,9 +295,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocks) decode_attn_rows_ke
                 const bool live = h < n;                      // (the whole warp stays: its lanes exchange values)
                 if (norm || turn) {
                     if (fresh || (norm && w_stride != 0)) {
-                        // The row's angles were asked for with its predecessor's first task, kRowsRing - 1 groups ahead of a row as
-                        // long as that; the first row's with its own tasks.
-                        if (fresh && (id == first_id || end - begin < kRowsRing - 1)) asm volatile("cp.async.wait_group 0;" ::: "memory");
+                        if (fresh && angles_late) asm volatile("cp.async.wait_group 0;" ::: "memory");
                         uint2 y[2][2];
                         y[0][0] = y[0][1] = y[1][0] = y[1][1] = make_uint2(0, 0);
                         if (norm && live) row_load<D, TURN, ALL, NEAR>(w + h * w_stride, l, rotary, wide || !TURN, y);
@@ -427,6 +429,7 @@ __global__ void __launch_bounds__(kRowsThreads, kRowsBlocks) decode_attn_rows_ke
         next_pos = after;
         next_slot = after_slot;
         odd = !odd;
+        angles_late = end - begin < kRowsRing - 1;
     }
 }
 
