@@ -45,9 +45,15 @@ constexpr int kFillThreads = 256;
 constexpr int kRowsPerThread = 4;
 constexpr int kSharedBatch = 2048;                // sequences whose sums are kept in shared memory
 
-// Sums saturate far above every limit that they are held against (INT32_MAX rows or pages), which keeps them associative.
-__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return min(a + b, 0x80000000u); }
-__device__ __forceinline__ uint32_t sat(int64_t x) { return x > 0x80000000LL ? 0x80000000u : (uint32_t)x; }
+// Sums saturate above every limit that they are held against (INT32_MAX rows or pages), which keeps them associative.  (Two that
+// have saturated are 2^32, which 32 bits do not hold.)
+constexpr uint32_t kSaturated = 0x80000000u;
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b)
+{
+    const uint32_t sum = a + b;
+    return sum < a ? kSaturated : min(sum, kSaturated);
+}
+__device__ __forceinline__ uint32_t sat(int64_t x) { return x > kSaturated ? kSaturated : (uint32_t)x; }
 
 // Exclusive prefix sums of two values over the block's threads; the totals in `all`.
 __device__ __forceinline__ void block_scan2(uint32_t& x, uint32_t& y, uint32_t (&all)[2], uint32_t (*sm)[2])
