@@ -445,7 +445,8 @@ int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan,
  * e2m1 (a sign and a magnitude of 0, .5, 1, 1.5, 2, 3, 4 or 6; 4 bits) times
  * the fp16 scale of the 32 dims that it lies in, 4.5 bits a value.  The scale
  * of 32 values is the largest magnitude among them over 6, rounded to fp16
- * (to at most 65,504), a code the nearest to value / scale, ties to the even
+ * (to at most 65,504; 10,912 instead of 10,920, so that 65,504 is held as a
+ * value that fp16 has), a code the nearest to value / scale, ties to the even
  * code, 6 at most.  K and V are finite: infinities are held as 6 * 65,504
  * over the zeros and small values beside them, NaN as anything.  Values whose
  * block stays below 6 * 2^-14 in magnitude are held more coarsely, below
@@ -476,7 +477,7 @@ int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan,
  * take a shape and neither plan nor policy (decode_attn_merge_shards,
  * decode_attn_validate_block_table) want one of 16-bit pools.  Products with
  * K are exact up to fp32 sums; weights and values are rounded once to fp16
- * ahead of the product with V, so V beyond 65,504 in magnitude (which bf16 rows
+ * ahead of the product with V, so V beyond 65,536 in magnitude (which bf16 rows
  * can hold) makes what attends it infinite or NaN.
  * ------------------------------------------------------------------------- */
 

@@ -21,8 +21,13 @@ __device__ __forceinline__ void packed_unpack(uint32_t w, uint32_t (&r)[4])
         : "r"(w));
 }
 
-// The scale of 32 values whose largest magnitude is amax: amax / 6 in fp16, finite.
-__device__ __forceinline__ __half packed_scale(float amax) { return __float2half_rn(fminf(__fdiv_rn(amax, 6.0f), 65504.0f)); }
+// The scale of 32 values whose largest magnitude is amax: amax / 6 in fp16, finite.  65,504, the largest fp16 value, would have the
+// scale 10,920 and be held as 65,520, which fp16 (of expanded pages, of the operands of V) rounds to infinity: its scale is 10,912.
+__device__ __forceinline__ __half packed_scale(float amax)
+{
+    const float s = __half2float(__float2half_rn(fminf(__fdiv_rn(amax, 6.0f), 65504.0f)));
+    return __float2half_rn(s == 10920.0f ? 10912.0f : s);
+}
 
 // Two codes from a value's quotients: nearest, ties to the even code, at most 6.
 __device__ __forceinline__ uint32_t packed_pair(float lo, float hi)
