@@ -23,7 +23,8 @@
 // operand: a pair of tokens' codes times their pair of scales, rounded to fp16 (half a step of 2^-11).  A lane's V operand wants
 // pairs of tokens of one dim while bytes hold pairs of dims of one token: words of two tokens are interleaved by nibbles
 // ahead of the conversion, half an instruction per pair.  Queries are brought to a largest magnitude in [1, 2) by a power of two
-// (exact) so that bf16 values fit fp16's range.
+// so that bf16 values fit fp16's range: exact, but for dims below 2^-14 of the head's largest, which are subnormal there and off by
+// up to 2^-25 of it (bf16 ones from 2^-17 on).  Next to the largest dim these matter only where K is that much larger in them.
 //
 // Softmax runs on the accumulators in fp32, base 2.  The running maximum of a head is renewed only when a logit runs more
 // than 8 above it (weights stay below 2^8, representable with the same relative step), so that most steps need no
