@@ -558,7 +558,7 @@ __global__ void __launch_bounds__(32 * W, PackedCfg<D, W, NT>::kBlocks) decode_a
                 }
             }
             block_sync(1, Cfg::kThreads);
-            block_finish<D, W, Cfg::kCols, false>(p, done, G, sm_wo, sm_wm, sm_wl, tid, Cfg::kThreads, 1, 4 * q, min(4, G - 4 * q),
+            block_finish<D, W, Cfg::kCols, false, W>(p, done, G, sm_wo, sm_wm, sm_wl, tid, Cfg::kThreads, 1, 4 * q, min(4, G - 4 * q),
                                                   DUP || 4 * (q + 1) >= G);
         }
     }
