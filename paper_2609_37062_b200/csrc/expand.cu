@@ -4,11 +4,12 @@
 // 128).  A warp copies its tasks to a ring of its own (cp.async, one task ahead), and 16 lanes (8 at head_dim 64) write a row of
 // K or V whole, 16 bytes a lane, from one word of codes each.
 //
-// The lengths are on the device, so the grid cannot follow them: it is bounded by what the machine holds, every block makes the
+// The lengths are on the device, so the grid cannot follow them: it is bounded by the machine, every block makes the
 // sums of the sequences' tiles, and the grid's warps go through the tasks together.  96,000 tokens of 8 heads of 128, 502 MB: 85 us,
-// 5.9 TB/s (a plain copy's rate would be 77).  Blocks over the width of the tables, eight tiles each, took 90 on lengths of 8,000 to
-// 30,000, since their SMs were not equally full, and had thousands of empty blocks where tables are wide; with no more blocks than fit
-// at a time 89 (24 warps an SM: 96), with eight times as many 84.6: warps that start together also read and write together.
+// 5.9 TB/s (a plain copy's rate would be 77), with 24 blocks launched for every SM.  Blocks over the width of the tables, eight tiles
+// each, took 90 on lengths of 8,000 to 30,000, since their SMs were not equally full, and had thousands of empty blocks where
+// tables are wide; 3, 6, 12, 20 and 48 blocks for every SM took 96, 89, 88, 88 and 84.6: warps that start together also read and write
+// together.
 #include <cstring>
 
 #include "common.cuh"
@@ -21,9 +22,11 @@ using namespace da;
 namespace {
 
 constexpr int kExpandThreads = 256;
-constexpr int kExpandBlocks = 6;       // on an SM
 constexpr int kExpandRing = 2;         // tasks in a warp's ring
-constexpr int kExpandWaves = 4;        // blocks launched for one that fits at a time
+constexpr int kExpandGrid = 148 * 24;  // blocks at most
+// Blocks that registers leave room for on an SM, 40 a thread.  At head_dim 64 six are resident, at 128 five: 41,024 bytes of shared
+// memory each, the system's 1 KB included.  (With the 48 registers of five: the same, 3.7 us instead of 3.6 for 500 tokens.)
+constexpr int kExpandBlocks = 6;
 constexpr int kExpandBatch = kExpandThreads;         // sequences that the sums are made for at a time
 
 struct ExpandParams {
@@ -241,12 +244,10 @@ extern "C" int decode_attn_expand_kv(const decode_attn_shape_t* shape, const dec
     p.src_width = f.max_pages_per_seq;
     p.dst_width = s.max_pages_per_seq;
     while ((1 << p.page_shift) < s.page_size) ++p.page_shift;
-    // (a few for every one that 148 SMs hold at a time, or as many as the tables have room for)
-    constexpr int64_t kMost = 148 * kExpandBlocks * kExpandWaves;
     constexpr int64_t kWarps = kExpandThreads / 32;
     const int64_t tiles = (int64_t)width * (s.page_size / 16) * s.batch;
     const int64_t most = tiles > INT32_MAX ? INT32_MAX : tiles * s.num_kv_heads, needed = (most + kWarps - 1) / kWarps;
-    const int64_t blocks = needed < kMost ? needed : kMost;
+    const int64_t blocks = needed < kExpandGrid ? needed : kExpandGrid;    // (no more than the tables have room for)
     const bool f16 = s.kv_dtype == DA_DTYPE_FP16;
     auto fn = s.head_dim == 128 ? (f16 ? decode_attn_expand_kernel<128, true> : decode_attn_expand_kernel<128, false>)
                                 : (f16 ? decode_attn_expand_kernel<64, true> : decode_attn_expand_kernel<64, false>);
