@@ -574,12 +574,14 @@ def decode_attn_validate_evict(shape: Shape, budget_tokens: int, sink_tokens: in
 def decode_attn_expand_kv(shape: Shape, packed_shape: Shape, pool, block_table, seq_lens, dst_block_table, k_cache, v_cache,
                           status=None, stream=None, check: bool = True) -> int:
     """The cached tokens of a cache in 4 bits (packed_shape, pool, block_table) as 16-bit pages (shape, k_cache, v_cache,
-    dst_block_table); status: int32 [1] or None."""
-    rc = _lib.decode_attn_expand_kv(ctypes.byref(shape), ctypes.byref(packed_shape), _ptr(pool), _ptr(block_table),
-                                    _ptr(seq_lens), _ptr(dst_block_table), _ptr(k_cache), _ptr(v_cache), _ptr(status),
-                                    _stream(stream))
+    dst_block_table); tables and lengths int32, contiguous; status: int32 [1] or None."""
+    i32, batch, at = _dtypes()[3], shape.batch, "decode_attn_expand_kv"
+    rc = _lib.decode_attn_expand_kv(ctypes.byref(shape), ctypes.byref(packed_shape), _ptr(pool),
+                                    _vector(block_table, i32, batch * packed_shape.max_pages_per_seq, at), _vector(seq_lens, i32, batch, at),
+                                    _vector(dst_block_table, i32, batch * shape.max_pages_per_seq, at), _ptr(k_cache), _ptr(v_cache),
+                                    _vector(status, i32, 1, at), _stream(stream))
     if check:
-        _check(rc, "decode_attn_expand_kv")
+        _check(rc, at)
     return rc
 
 
