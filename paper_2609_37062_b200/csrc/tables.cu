@@ -107,16 +107,13 @@ struct Ask {
     int64_t old, fresh, back, lack, rows;
 };
 
-__device__ __forceinline__ Ask ask_of(const TablesParams& p, int b, bool loud)
+__device__ __forceinline__ Ask ask_of(const TablesParams& p, int b)
 {
     Ask a = {-1, -1, 0, 0, 0};
     if (b >= p.batch) return a;
     const int64_t old = p.seq_lens[b], gain = p.gains[b];
     const int64_t fresh = old + gain > 0 ? old + gain : 0;
-    if (old < 0 || old > p.most_tokens || fresh > p.most_tokens) {
-        if (loud) report(p, DA_ERR_STALE_PLAN);
-        return a;
-    }
+    if (old < 0 || old > p.most_tokens || fresh > p.most_tokens) return a;
     const int64_t round = ((int64_t)1 << p.page_shift) - 1;
     const int64_t held = (old + round) >> p.page_shift, holds = (fresh + round) >> p.page_shift;
     a.old = old;
@@ -204,7 +201,7 @@ __global__ void __launch_bounds__(kScanThreads) decode_attn_tables_kernel(const 
     int32_t* const sm_old = sm_pages + p.batch + 1;
     const bool keep = FILL && p.shared;
     const int64_t count = *p.free_count;
-    Ask ask = ask_of(p, tid, false);                          // of the first nt sequences, asked for beside the count
+    Ask ask = ask_of(p, tid);                          // of the first nt sequences, asked for beside the count
     const bool sane = count >= 0 && count <= p.free_capacity;
     if (!sane && tid == 0) report(p, DA_ERR_STALE_PLAN);
     const Ask none = {-1, -1, 0, 0, 0};
@@ -217,7 +214,7 @@ __global__ void __launch_bounds__(kScanThreads) decode_attn_tables_kernel(const 
     bool full = false;                                        // some of what is given back does not fit
     if (__syncthreads_or(any_back && sane)) {
         for (int b0 = 0; b0 < p.batch && !full; b0 += nt) {
-            const Ask a = b0 == 0 ? ask : sane ? ask_of(p, b0 + tid, false) : none;
+            const Ask a = b0 == 0 ? ask : sane ? ask_of(p, b0 + tid) : none;
             uint32_t at = sat(a.back), zero = 0;
             block_scan2(at, zero, all, sm);
             const bool fits = count + pushed + at + a.back <= p.free_capacity;
@@ -249,7 +246,7 @@ __global__ void __launch_bounds__(kScanThreads) decode_attn_tables_kernel(const 
     bool refused = false;
     for (int b0 = 0; b0 < p.batch; b0 += nt) {
         const int b = b0 + tid;
-        const Ask a = sane ? (b0 == 0 ? ask : ask_of(p, b, false)) : none;
+        const Ask a = sane ? (b0 == 0 ? ask : ask_of(p, b)) : none;
         if (sane && b < p.batch && a.old < 0) report(p, DA_ERR_STALE_PLAN);
         uint32_t lack = sat(a.lack), row = sat(a.rows);
         block_scan2(lack, row, all, sm);
