@@ -46,13 +46,9 @@ constexpr int kRowsPerThread = 4;
 constexpr int kSharedBatch = 2048;                // sequences whose sums are kept in shared memory
 
 // Sums saturate above every limit that they are held against (INT32_MAX rows or pages), which keeps them associative.  (Two that
-// have saturated are 2^32, which 32 bits do not hold.)
+// have saturated are 2^32, which 32 bits do not hold: what is added is cut off ahead of the addition.)
 constexpr uint32_t kSaturated = 0x80000000u;
-__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b)
-{
-    const uint32_t sum = a + b;
-    return sum < a ? kSaturated : min(sum, kSaturated);
-}
+__device__ __forceinline__ uint32_t sat_add(uint32_t a, uint32_t b) { return a + min(b, kSaturated - a); }
 __device__ __forceinline__ uint32_t sat(int64_t x) { return x > kSaturated ? kSaturated : (uint32_t)x; }
 
 // Exclusive prefix sums of two values over the block's threads; the totals in `all`.
