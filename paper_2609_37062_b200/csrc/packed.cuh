@@ -25,8 +25,8 @@ __device__ __forceinline__ void packed_unpack(uint32_t w, uint32_t (&r)[4])
 // scale 10,920 and be held as 65,520, which fp16 (of expanded pages, of the operands of V) rounds to infinity: its scale is 10,912.
 __device__ __forceinline__ __half packed_scale(float amax)
 {
-    const float s = __half2float(__float2half_rn(fminf(__fdiv_rn(amax, 6.0f), 65504.0f)));
-    return __float2half_rn(s == 10920.0f ? 10912.0f : s);
+    const float s = fminf(__fdiv_rn(amax, 6.0f), 65504.0f);
+    return __float2half_rn(fabsf(s - 10920.0f) < 4.0f ? 10912.0f : s);          // (what rounds to 10,920: half a step of 8 to either side)
 }
 
 // Two codes from a value's quotients: nearest, ties to the even code, at most 6.
