@@ -479,10 +479,11 @@ int decode_attn_prompt_last_device_status(const decode_attn_prompt_plan_t *plan,
  * K are exact up to fp32 sums, but for dims of a query below 2^-14 of its
  * head's largest magnitude max|q|: these are rounded to steps of 2^-24 of it, so
  * a logit is off by up to 2^-25 max|q| sum|k| times the softmax scale.  Weights
- * and values are rounded to fp16 ahead of the product with V, each by 2^-11 of
- * itself at most, weights below 2^-14 of the largest by 2^-25 of that (weights
- * of fp16 inputs keep twice the bits); V beyond 65,536 in magnitude (which bf16
- * rows can hold) makes what attends it infinite or NaN.
+ * and values are rounded to fp16 ahead of the product with V, off by 2^-11 of
+ * themselves at most: values below 2^-14 by 2^-25, weights below 2^-14 of the
+ * largest by 2^-25 of that (weights of fp16 inputs keep twice the bits).  V
+ * beyond 65,536 in magnitude (which bf16 rows can hold) makes what attends it
+ * infinite or NaN.
  * ------------------------------------------------------------------------- */
 
 /* Bytes of one KV head of one page of a cache in 4 bits; 0 for a head_dim or

@@ -6,7 +6,9 @@
 // are 144 bytes at head_dim 128 instead of 512, so at the same DRAM rate 3.6 times as many values have to be unpacked and
 // multiplied, and the kernel is bound by issued instructions as much as by memory: 263 of them a tile and warp, issued at
 // 0.62 a cycle and scheduler, of which the conversions from e2m1 and the half-precision products take a pipe two cycles each.
-// 64 sequences of 28,000 to 32,768 tokens, 32 / 8 heads of 128: 2.2 GB in 372 us, 5.96 TB/s (405 to 436 us where the same step
+// (At head_dim 128 these include spills: 64 to 80 bytes a thread stored and 44 to 52 loaded, more in the forms for windows and for groups
+// of more than 8, up to 444 and 292.)
+// 64 sequences of 28,000 to 32,768 tokens, 32 / 8 heads of 128: 2.2 GB in 372 us, 5.96 TB/s (405 to 450 us where the same step
 // runs without a pause and the power limit lowers the clock).
 //
 // A block is W warps, 4 or 8.  Every warp has a ring of its own and works in steps of two tiles (32 tokens): step w of

@@ -39,6 +39,7 @@ rows_kernel_t kernel_for(bool f16, bool packed, bool halves, bool all)
 // about one and a half to begin.  Where rows are more than half of the warps, another number may fill the last round of warps
 // better.  (32 + 8 + 8 heads of 128, us: 256 rows 5.3 with shares for a little more than the resident warps, 4.0 so; 600 rows 7.2
 // and 5.2; 1,777 rows 12.8 and 11.2; 1,200 rows 10.1 whole and 9.1 in three shares, 3,000 rows 19.5 whole and 18.0 in two.)
+// (Of a B200's 148 SMs; on another number the results are the same.)
 constexpr int kRowsWarps = 148 * kRowsBlocks * (kRowsThreads / 32);
 
 int split_of(int rows, int tasks)
